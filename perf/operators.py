@@ -1,0 +1,264 @@
+"""The gate of the gated MLP with an 8-bit checkpoint of its input, and the scaled embedding lookup with its gradient.
+
+Gate (GatedMLP, one row z = core | gate of 2 d values):
+    phi = SiLU(LN(core) g_c + b_c) * sigmoid(LN(gate) g_g + b_g)
+The forward pass of a training step keeps z in 8 bits, each half of a row with its least value and its step; the backward
+pass forms dz and the LayerNorm gradients from that. Inference keeps nothing.
+
+Embedding: out[i] = scale * table[token[i] - first], zero where that is no row of the table; its gradient sums the rows of
+equal tokens.
+
+Sizes are those of the crystals of this repository's workloads (edges, angles and atoms of one 8-atom cell up to 128
+crystals of width 128), and generic ones: wider rows, 16-bit types, larger tables, a million tokens.
+"""
+import math
+
+import torch
+
+own = False
+
+LN_EPS = 1e-5
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+STEP_OF_RANGE = float(torch.tensor(1.0 / 255.0, dtype=torch.float32))  # fp32's 1/255
+LEAST_STEP = 2.0 ** -100
+
+
+def listed():
+    return [
+        # inference of one 8-atom cell: the gates of its 1,354 angles, where only latency counts
+        dict(name="gate_infer_cell8", kind="gate_infer", rows=1354, d=64, dtype="fp32"),
+        # inference of 128 crystals at width 128: a layer's 397,934 angles
+        dict(name="gate_infer_wide128", kind="gate_infer", rows=397934, d=128, dtype="fp32"),
+        # training step of one 8-atom cell: the gates of its 920 edges
+        dict(name="gate_train_cell8", kind="gate_train", rows=920, d=64, dtype="fp32"),
+        # training step of 40 crystals: a layer's 85,274 edges
+        dict(name="gate_train_tri40", kind="gate_train", rows=85274, d=64, dtype="fp32"),
+        # training step of 128 crystals at width 128: a layer's 397,934 angles, the largest
+        dict(name="gate_train_wide128", kind="gate_train", rows=397934, d=128, dtype="fp32"),
+        # wider rows of odd width in 16 bits
+        dict(name="gate_train_odd", kind="gate_train", rows=20011, d=333, dtype="bf16"),
+        # atoms of one 8-atom cell
+        dict(name="embed_cell8", kind="embed", n=8, vocab=94, d=64, dtype="fp32", first=1, scale=1.0, pad=0.0, zipf=0.7),
+        # a large table in 16 bits, scaled to unit variance, padded batch
+        dict(name="embed_table50k", kind="embed", n=524288, vocab=50000, d=256, dtype="bf16", first=0, scale=16.0, pad=0.1,
+             zipf=1.0),
+        # element table of 40 crystals, 1,076 atoms
+        dict(name="embed_grad_tri40", kind="embed_grad", n=1076, vocab=94, d=64, dtype="fp32", first=1, scale=1.0, pad=0.0,
+             zipf=0.7),
+        # element table of 128 crystals at width 128, 5,844 atoms
+        dict(name="embed_grad_wide128", kind="embed_grad", n=5844, vocab=94, d=128, dtype="fp32", first=1, scale=1.0,
+             pad=0.0, zipf=0.7),
+        # a million atoms (large cells, or batches put together), oxygen the most frequent
+        dict(name="embed_grad_1m", kind="embed_grad", n=1000003, vocab=94, d=128, dtype="fp32", first=1, scale=1.0, pad=0.0,
+             zipf=1.3),
+        # a large table in 16 bits: few tokens a row, most rows without any, padded batch
+        dict(name="embed_grad_table50k", kind="embed_grad", n=262144, vocab=50000, d=512, dtype="bf16", first=0, scale=16.0,
+             pad=0.1, zipf=1.0),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["gate_infer", "gate_train", "gate_train", "embed", "embed_grad", "embed_grad"])
+    dtype = rng.choice(["fp32", "fp32", "bf16", "fp16"])
+    if kind.startswith("gate"):
+        d = rng.choice([64, 64, 128, 128, 256, 512, rng.randint(16, 1024)])
+        return dict(kind=kind, rows=_log(rng, 1, min(397934, 397934 * 128 // d)), d=d, dtype=dtype)
+    d = rng.choice([64, 64, 128, 256, 512, rng.randint(16, 1024)])
+    vocab = rng.choice([94, 94, _log(rng, 10, 130000)])
+    vocab = min(vocab, 50000 * 512 // d)
+    return dict(kind=kind, n=_log(rng, 1, min(1000000, 1000003 * 128 // d)), vocab=vocab, d=d, dtype=dtype,
+                first=rng.choice([0, 1]), scale=rng.choice([1.0, 0.5, float(d) ** 0.5]), pad=rng.choice([0.0, 0.0, 0.1]),
+                zipf=rng.choice([0.0, 0.7, 1.0, 1.3]))
+
+
+def prepare(case, seed):
+    c = case
+    dev = torch.device("cuda")
+    g = torch.Generator(device=dev)
+    g.manual_seed(int(seed))
+    t = TYPES[c["dtype"]]
+    randn = lambda *s: torch.randn(*s, device=dev, generator=g)
+    s = {"case": dict(c)}
+    if c["kind"].startswith("gate"):
+        R, d = c["rows"], c["d"]
+        # pre-activations: a column part that all rows share (the bias and the mean of the inputs), rows of their own scale
+        z = randn(R, 2 * d) * torch.exp(0.4 * randn(R, 1)) + 0.5 * randn(1, 2 * d)
+        s["z"] = z.to(t)
+        s["ln"] = torch.stack([1 + 0.1 * randn(d), 0.1 * randn(d), 1 + 0.1 * randn(d), 0.1 * randn(d)])
+        if c["kind"] == "gate_train":
+            # upstream gradients, small where a bond is near the cutoff (none at all in one row of eight)
+            w = torch.rand(R, 1, device=dev, generator=g)
+            s["dphi"] = (1e-2 * randn(R, d) * torch.where(w < 0.125, torch.zeros_like(w), w)).to(t)
+        return s
+    n, V, d = c["n"], c["vocab"], c["d"]
+    p = (torch.arange(V, device=dev) + 1.5).double() ** -c["zipf"]
+    p = torch.cumsum(p, 0) / p.sum()
+    row = torch.searchsorted(p, torch.rand(n, device=dev, generator=g, dtype=torch.float64)).clamp_(max=V - 1)
+    row = torch.randperm(V, device=dev, generator=g)[row]
+    tok = row + c["first"]
+    if c["pad"] > 0:
+        # the ends of short sequences
+        tok = torch.where(torch.rand(n, device=dev, generator=g) < c["pad"], torch.full_like(tok, -1), tok)
+    s["tok"] = tok.to(torch.int32)
+    if c["kind"] == "embed":
+        s["table"] = randn(V, d).to(t)
+    else:
+        s["dout"] = (1e-2 * randn(n, d)).to(t)
+    return s
+
+
+# --- plain forms -----------------------------------------------------------------------------------------------------------
+
+def _checkpoint(x):
+    """x [rows, 2, d] in fp32 as 8-bit codes with the least value and the step of each half row."""
+    lo, hi = x.amin(2, keepdim=True), x.amax(2, keepdim=True)
+    step = ((hi - lo) * STEP_OF_RANGE).clamp(min=LEAST_STEP)
+    inv = (1.0 / step.double()).float()
+    # in 64 bits: a product next to a half must not be rounded before it is rounded to a whole number
+    q = torch.round((x - lo).double() * inv.double()).to(torch.uint8)
+    return q, lo, step
+
+
+def _normed(x):
+    m = x.mean(2, keepdim=True)
+    x = x - m
+    r = torch.rsqrt((x * x).mean(2, keepdim=True) + LN_EPS)
+    return x * r, r
+
+
+def _gate_forward(z, ln):
+    x = z.float().reshape(z.shape[0], 2, -1)
+    xh, _ = _normed(x)
+    yc, yg = ln[0] * xh[:, 0] + ln[1], ln[2] * xh[:, 1] + ln[3]
+    return yc / (1 + torch.exp(-yc)) / (1 + torch.exp(-yg)), x
+
+
+def _gate_backward(q, lo, step, ln, dphi):
+    xh, r = _normed(lo + q.float() * step)
+    yc, yg = ln[0] * xh[:, 0] + ln[1], ln[2] * xh[:, 1] + ln[3]
+    sc, sg = 1 / (1 + torch.exp(-yc)), 1 / (1 + torch.exp(-yg))
+    up = dphi.float()
+    gy = torch.stack([up * sg * sc * (1 + yc * (1 - sc)), up * yc * sc * sg * (1 - sg)], 1)
+    dln = torch.stack([(gy * xh).sum(0), gy.sum(0)], 1).reshape(4, -1)
+    dy = gy * ln[0::2]
+    dz = r * (dy - dy.mean(2, keepdim=True) - xh * (dy * xh).mean(2, keepdim=True))
+    return dz.reshape(dz.shape[0], -1), dln
+
+
+def run(state):
+    s, c = state, state["case"]
+    if own:
+        from paper_2412_20796_amd import ops
+
+        if c["kind"] == "gate_infer":
+            return ops.gate_forward(s["z"], s["ln"], save=False)
+        if c["kind"] == "gate_train":
+            phi, kept = ops.gate_forward(s["z"], s["ln"])
+            dz, dln = ops.gate_backward(kept, s["ln"], s["dphi"])
+            return {"phi": phi, "dz": dz, "dln": dln}
+        if c["kind"] == "embed":
+            return ops.embed_forward(s["table"], s["tok"], scale=c["scale"], first=c["first"])
+        return ops.embed_backward(s["tok"], s["dout"], c["vocab"], scale=c["scale"], first=c["first"])
+    t = TYPES[c["dtype"]]
+    if c["kind"].startswith("gate"):
+        phi, x = _gate_forward(s["z"], s["ln"])
+        if c["kind"] == "gate_infer":
+            return phi.to(t)
+        kept = _checkpoint(x)
+        del x
+        dz, dln = _gate_backward(*kept, s["ln"], s["dphi"])
+        return {"phi": phi.to(t), "dz": dz.to(t), "dln": dln}
+    row = s["tok"].long() - c["first"]
+    there = (row >= 0) & (row < c["vocab"])
+    if c["kind"] == "embed":
+        return torch.where(there[:, None], s["table"][row.clamp(0, c["vocab"] - 1)].float() * c["scale"], 0.0).to(t)
+    # long sums (an element of every second atom) in parts, so that 32 bits hold them
+    n, V = row.numel(), c["vocab"] + 1
+    parts = min(64, max(1, n // (16 * V)))
+    out = torch.zeros(parts * V, c["d"], device=row.device)
+    part = torch.arange(n, device=row.device) % parts
+    out.index_add_(0, part * V + torch.where(there, row, c["vocab"]), s["dout"].float())
+    return out.reshape(parts, V, -1).sum(0)[:c["vocab"]] * c["scale"]
+
+
+def work(case):
+    """Inputs and outputs once each. The checkpoint is the first call's output and the second one's input."""
+    c = case
+    es = 4 if c["dtype"] == "fp32" else 2
+    if c["kind"].startswith("gate"):
+        R, d = c["rows"], c["d"]
+        fwd = {"bytes": 3 * R * d * es + 16 * d, "flops": 30 * R * d}
+        if c["kind"] == "gate_infer":
+            return fwd
+        kept = R * (2 * d + 16)
+        return {"bytes": fwd["bytes"] + 2 * kept + 3 * R * d * es + 32 * d, "flops": fwd["flops"] + 8 * R * d + 60 * R * d}
+    n, V, d = c["n"], c["vocab"], c["d"]
+    real = n * (1 - c["pad"])
+    if c["kind"] == "embed":
+        return {"bytes": 4 * n + n * d * es + min(V, real) * d * es, "flops": real * d}
+    return {"bytes": 4 * n + real * d * es + 4 * V * d, "flops": real * d + V * d}
+
+
+# --- the same in 64 bits ---------------------------------------------------------------------------------------------------
+
+def _r32(x):
+    return x.to(torch.float32).to(torch.float64)
+
+
+def exact(case, seed):
+    c, s = case, prepare(case, seed)
+    if c["kind"] == "embed":
+        W = torch.cat([s["table"].double(), torch.zeros(1, c["d"], dtype=torch.float64, device="cuda")])
+        k = s["tok"].long() - c["first"]
+        return c["scale"] * W[torch.where((k < 0) | (k >= c["vocab"]), c["vocab"], k)]
+    if c["kind"] == "embed_grad":
+        k = s["tok"].long() - c["first"]
+        keep = ((k >= 0) & (k < c["vocab"])).nonzero()[:, 0]
+        # rows in order of their tokens; sums of runs as differences are not exact enough, so runs are halved until each is one row
+        order = keep[torch.argsort(k[keep], stable=True)]
+        key, val = k[order], s["dout"][order].double()
+        while key.numel():
+            n = key.numel()
+            at = torch.arange(n, device=key.device)
+            start = torch.ones(n, dtype=torch.bool, device=key.device)
+            start[1:] = key[1:] != key[:-1]
+            if bool(start.all()):
+                break
+            head = torch.cummax(torch.where(start, at, 0), 0).values
+            odd = ((at - head) & 1).bool()  # joins the row before it
+            val[at[odd] - 1] += val[odd]
+            key, val = key[~odd], val[~odd]
+        out = torch.zeros(c["vocab"], c["d"], dtype=torch.float64, device="cuda")
+        out[key] = val
+        return out * c["scale"]
+    d = c["d"]
+    g = s["ln"].double()
+
+    def phi(core, gate):
+        def ln(x, a, b):
+            v, m = torch.var_mean(x, dim=1, unbiased=False, keepdim=True)
+            return a * ((x - m) / torch.sqrt(v + LN_EPS)) + b
+        y = ln(core, p[0], p[1])
+        return y * torch.sigmoid(y) * torch.sigmoid(ln(gate, p[2], p[3]))
+
+    z = s["z"].double()
+    p = [g[k] for k in range(4)]
+    with torch.no_grad():
+        f = phi(z[:, :d], z[:, d:])
+    if c["kind"] == "gate_infer":
+        return f
+    # the derivative at what the checkpoint holds; its steps are fp32 numbers by definition
+    held = []
+    for x in (z[:, :d], z[:, d:]):
+        lo, hi = torch.aminmax(x, dim=1, keepdim=True)
+        step = torch.clamp(_r32(_r32(hi - lo) * STEP_OF_RANGE), min=LEAST_STEP)
+        held.append((lo + step * torch.round(_r32(x - lo) * _r32(1.0 / step))).requires_grad_(True))
+    del z
+    p = [q.clone().requires_grad_(True) for q in p]
+    with torch.enable_grad():
+        grads = torch.autograd.grad(phi(*held), held + p, s["dphi"].double())
+    return {"phi": f, "dz": torch.cat(grads[:2], 1), "dln": torch.stack(grads[2:])}
