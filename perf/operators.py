@@ -2,7 +2,7 @@
 
 Gate (GatedMLP, one row z = core | gate of 2 d values):
     phi = SiLU(LN(core) g_c + b_c) * sigmoid(LN(gate) g_g + b_g)
-The forward pass of a training step keeps z in 8 bits, each half of a row with its least value and its step; the backward
+The forward pass of a training step keeps z in 8 bits, as steps above the least value of each half of a row; the backward
 pass forms dz and the LayerNorm gradients from that. Inference keeps nothing.
 
 Embedding: out[i] = scale * table[token[i] - first], zero where that is no row of the table; its gradient sums the rows of
@@ -194,7 +194,7 @@ def work(case):
         fwd = {"bytes": 3 * R * d * es + 16 * d, "flops": 30 * R * d}
         if c["kind"] == "gate_infer":
             return fwd
-        kept = R * (2 * d + 16)
+        kept = R * (2 * d + 8)
         return {"bytes": fwd["bytes"] + 2 * kept + 3 * R * d * es + 32 * d, "flops": fwd["flops"] + 8 * R * d + 60 * R * d}
     n, V, d = c["n"], c["vocab"], c["d"]
     real = n * (1 - c["pad"])
