@@ -6,6 +6,7 @@
 #include <string>
 #include <vector>
 
+#include "chgnet_ops.h"
 #include "common.hpp"
 
 namespace chg {
@@ -28,6 +29,19 @@ int step_entry(const chgnet_hparams* hp, const chgnet_batch* batch, chgnet_graph
 int md_entry(const chgnet_hparams* hp, const chgnet_batch* batch, chgnet_graph* graph, const float* params,
              chgnet_md_state* s, float dt, int n_steps, int forces_valid, int* steps_done, void* ws,
              size_t ws_bytes, hipStream_t st);
+
+int gate_forward_entry(int64_t rows, int32_t d, int32_t dtype, const void* z, int64_t ldz, const float* ln, void* phi,
+                       int64_t ldphi, uint8_t* codes, float* step, hipStream_t st);
+int gate_backward_workspace_entry(int64_t rows, int32_t d, size_t* bytes);
+int gate_backward_entry(int64_t rows, int32_t d, int32_t dtype, const uint8_t* codes, const float* step,
+                        const float* ln, const void* dphi, int64_t lddphi, void* dz, int64_t lddz, float* dln,
+                        int accumulate, void* ws, size_t ws_bytes, hipStream_t st);
+int embed_forward_entry(int64_t n, int32_t d, int64_t vocab, int32_t dtype, const int32_t* tok, int32_t first,
+                        const void* table, int64_t ldtable, float scale, void* out, int64_t ldout, hipStream_t st);
+int embed_backward_workspace_entry(int64_t n, int32_t d, int64_t vocab, size_t* bytes);
+int embed_backward_entry(int64_t n, int32_t d, int64_t vocab, int32_t dtype, const int32_t* tok, int32_t first,
+                         const void* dout, int64_t lddout, float scale, float* dtable, int64_t lddtable,
+                         int accumulate, void* ws, size_t ws_bytes, hipStream_t st);
 
 namespace {
 thread_local std::string g_last_error;
@@ -200,6 +214,40 @@ int chgnet_md(const chgnet_hparams* hp, const chgnet_batch* batch, chgnet_graph*
               size_t ws_bytes, void* stream) {
   return chg::md_entry(hp, batch, graph, params, state, dt, n_steps, forces_valid, steps_done, ws, ws_bytes,
                        static_cast<hipStream_t>(stream));
+}
+
+int chgnet_gate_forward(int64_t rows, int32_t d, int32_t dtype, const void* z, int64_t ldz, const float* ln,
+                        void* phi, int64_t ldphi, uint8_t* codes, float* step, void* stream) {
+  return chg::gate_forward_entry(rows, d, dtype, z, ldz, ln, phi, ldphi, codes, step,
+                                 static_cast<hipStream_t>(stream));
+}
+
+int chgnet_gate_backward_workspace(int64_t rows, int32_t d, size_t* bytes) {
+  return chg::gate_backward_workspace_entry(rows, d, bytes);
+}
+
+int chgnet_gate_backward(int64_t rows, int32_t d, int32_t dtype, const uint8_t* codes, const float* step,
+                         const float* ln, const void* dphi, int64_t lddphi, void* dz, int64_t lddz, float* dln,
+                         int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  return chg::gate_backward_entry(rows, d, dtype, codes, step, ln, dphi, lddphi, dz, lddz, dln, accumulate, ws,
+                                  ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+int chgnet_embed_forward(int64_t n, int32_t d, int64_t vocab, int32_t dtype, const int32_t* tok, int32_t first,
+                         const void* table, int64_t ldtable, float scale, void* out, int64_t ldout, void* stream) {
+  return chg::embed_forward_entry(n, d, vocab, dtype, tok, first, table, ldtable, scale, out, ldout,
+                                  static_cast<hipStream_t>(stream));
+}
+
+int chgnet_embed_backward_workspace(int64_t n, int32_t d, int64_t vocab, size_t* bytes) {
+  return chg::embed_backward_workspace_entry(n, d, vocab, bytes);
+}
+
+int chgnet_embed_backward(int64_t n, int32_t d, int64_t vocab, int32_t dtype, const int32_t* tok, int32_t first,
+                          const void* dout, int64_t lddout, float scale, float* dtable, int64_t lddtable,
+                          int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  return chg::embed_backward_entry(n, d, vocab, dtype, tok, first, dout, lddout, scale, dtable, lddtable, accumulate,
+                                   ws, ws_bytes, static_cast<hipStream_t>(stream));
 }
 
 const char* chgnet_last_error_string(void) { return chg::g_last_error.c_str(); }

@@ -1,0 +1,42 @@
+// Element types of the operators (chgnet_ops.h): fp32 arithmetic on values held
+// in fp32, bf16 or fp16, rounded once where they are stored.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "chgnet_ops.h"
+
+namespace chg {
+
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+// V consecutive values (V = 1 or 4), aligned to their total size
+template <int V, class T>
+__device__ __forceinline__ void load_v(const T* p, float (&v)[V]) {
+  typedef T vec __attribute__((ext_vector_type(V)));
+  const vec t = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = (float)t[k];
+}
+template <int V, class T>
+__device__ __forceinline__ void store_v(T* p, const float (&v)[V]) {
+  typedef T vec __attribute__((ext_vector_type(V)));
+  vec t;
+#pragma unroll
+  for (int k = 0; k < V; ++k) t[k] = (T)v[k];
+  *reinterpret_cast<vec*>(p) = t;
+}
+
+inline int elem_size(int32_t dtype) { return dtype == CHGNET_F32 ? 4 : dtype == CHGNET_BF16 || dtype == CHGNET_F16 ? 2 : 0; }
+// calls f with a value of the (valid) type
+template <class F>
+int with_type(int32_t dtype, F&& f) {
+  if (dtype == CHGNET_F32) return f(float{});
+  if (dtype == CHGNET_BF16) return f(bf16_t{});
+  return f(f16_t{});
+}
+inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+}  // namespace chg

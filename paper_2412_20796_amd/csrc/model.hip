@@ -20,6 +20,7 @@
 
 #include "common.hpp"
 #include "gemm.hpp"
+#include "rowops.hpp"
 #include "split.hpp"
 
 namespace chg {
@@ -31,13 +32,9 @@ int validate_batch(const chgnet_batch* b);
 
 namespace {
 
-constexpr float kLnEps = 1e-5f;
 constexpr int kFreqRowsPerBlock = 64;  // rows per block in frequency-gradient kernel
 constexpr int kReduceGroups = 32;      // first-level groups of the ordered partial-sum reduction
 constexpr int64_t kTnPartFloats = 64ll << 20;
-
-// logistic sigmoid; the hardware reciprocal (about 1 ulp) instead of an IEEE division
-__device__ __forceinline__ float sigm(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 
 __device__ __forceinline__ float wsum(float v) {
 #pragma unroll
@@ -285,21 +282,6 @@ __global__ void __launch_bounds__(256) k_geom(GeomArgs g) {
 // sums over the LPR lanes by DPP permutes (no LDS traffic). A wavefront works
 // on 64/LPR rows at a time.
 // ---------------------------------------------------------------------------
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, false));
-}
-
-template <int LPR>
-__device__ __forceinline__ float rowsum(float v) {
-  static_assert(LPR == 4 || LPR == 8 || LPR == 16, "row of 4, 8 or 16 lanes");
-  v += dpp<0xB1>(v);  // quad_perm [1,0,3,2]
-  v += dpp<0x4E>(v);  // quad_perm [2,3,0,1]
-  if (LPR >= 8) v += dpp<0x141>(v);   // row_half_mirror: pairs the two quads of 8 lanes
-  if (LPR == 16) v += dpp<0x140>(v);  // row_mirror: pairs the two halves of 16 lanes
-  return v;
-}
-
 template <int D, int CPL>
 struct Lanes {
   static constexpr int LPR = D / CPL;   // lanes per row
@@ -1097,14 +1079,6 @@ __device__ __forceinline__ void bwd_mm_index(const GateBwdJob& J, int row, BwdMm
 // rotate by 8 within a row of 16); afterwards lane (j, b3, b4, b5) holds sum
 // a of column 32 b3 + 4 j + 2 b4 + b5 for a = 0..3, and is that slot's only
 // writer (fixed order, no atomics race).
-__device__ __forceinline__ float pl_sum32(float a, float b) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float pl_sum16(float a, float b) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 __device__ __forceinline__ void bwd_mm_ln_add(const float (&p)[32], float* wsum) {
   const int lane = threadIdx.x & 63;
   float w[16], x[8];
