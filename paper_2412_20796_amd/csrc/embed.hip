@@ -7,7 +7,7 @@
 // once and writes every row of dW once; what it must not do is depend on how
 // the tokens are spread, from a table of which most rows have no token to an
 // element that is every second atom. So the positions are ordered by token
-// first (stable, so that the sums have one order), the ordered positions are
+// first (stably, so that the sums have one order), the ordered positions are
 // cut into chunks of equal length, each summed by one group of lanes run by
 // run, and the runs that cross a chunk's end are joined from the chunks' partial
 // sums, in order. Few tokens skip the ordering: a block a token finds the
@@ -140,10 +140,16 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_place(SortPass s) {
     // four threads a digit, each a quarter of the stretches
     const int digit = t & (kDigits - 1), q = t / kDigits;
     int before = 0, all = 0;
-    for (int b = nb * q / 4; b < nb * (q + 1) / 4; ++b) {
-      const int c = s.counts[b * kDigits + digit];
-      before += b < (int)blockIdx.x ? c : 0;
-      all += c;
+    const int b1 = nb * (q + 1) / 4;
+    for (int b0 = nb * q / 4; b0 < b1; b0 += 16) {
+      int c[16];  // loads in flight together: one at a time they took 30 us of 1,000,003 tokens
+#pragma unroll
+      for (int u = 0; u < 16; ++u) c[u] = b0 + u < b1 ? s.counts[(b0 + u) * kDigits + digit] : 0;
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        before += b0 + u < (int)blockIdx.x ? c[u] : 0;
+        all += c[u];
+      }
     }
     wcnt[q][digit] = before;
     wcnt[4 + q][digit] = all;
@@ -267,14 +273,24 @@ __global__ void __launch_bounds__(256) k_embed_runs(RunSums s, const T* __restri
       }
     }
   };
+  int nr[U], no[U];  // the next step's rows and positions, loaded a step ahead
+  auto load_index = [&](int p) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = min(p + u, p1 - 1);
+      nr[u] = s.row[x];
+      no[u] = s.pos[x];
+    }
+  };
+  load_index(p0);
   for (int p = p0; p < p1; p += U) {
     int r[U], o[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int x = min(p + u, p1 - 1);
-      r[u] = s.row[x];
-      o[u] = s.pos[x];
+      r[u] = nr[u];
+      o[u] = no[u];
     }
+    if (p + U < p1) load_index(p + U);
     float v[U][CPL];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -304,10 +320,14 @@ __global__ void __launch_bounds__(256) k_embed_runs(RunSums s, const T* __restri
 
 // Joins the runs that cross chunks: the block of the chunk in which a run
 // begins adds that chunk's slot 1 and slot 0 of the chunks up to the run's end.
-// 64 columns a block, 16 lanes a row; the 16 groups take the partial rows in
-// turn and are added in order.
-__global__ void __launch_bounds__(256) k_embed_join(RunSums s) {
-  __shared__ float red[16][64];
+// 64 columns a block, 16 lanes a row; the groups of lanes take the partial rows
+// in turn, eight loads in flight, and are added in order.
+constexpr int kJoinThreads = 512;
+
+template <int VEC>
+__global__ void __launch_bounds__(kJoinThreads) k_embed_join(RunSums s) {
+  constexpr int G = kJoinThreads / 16, U = 8, C = 16 * VEC;
+  __shared__ float red[G][C];
   const int c = blockIdx.x;
   const int p0 = c * s.chunk, p1 = p0 + s.chunk;
   if (p1 >= s.n) return;
@@ -320,86 +340,107 @@ __global__ void __launch_bounds__(256) k_embed_join(RunSums s) {
     if (s.row[mid * s.chunk] == v) lo = mid;
     else hi = mid;
   }
-  const int m = lo - c;  // chunks after c
-  const int g = threadIdx.x >> 4, col = blockIdx.y * 64 + (threadIdx.x & 15) * 4;
-  float acc[4] = {};
-  if (g == 0) {
-    const float* w = s.part + ((int64_t)2 * c + 1) * s.d;
+  const int m = lo - c + 1;  // partial rows
+  const int g = threadIdx.x >> 4, j = threadIdx.x & 15, col = blockIdx.y * C + j * VEC;
+  float acc[VEC] = {};
+  for (int q0 = g; q0 < m; q0 += G * U) {
+    float x[U][VEC];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (col + k < s.d) acc[k] = w[col + k];
+    for (int u = 0; u < U; ++u) {
+      const int q = q0 + u * G;
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) x[u][k] = 0.f;
+      if (q < m && col < s.d) load_v<VEC>(s.part + ((int64_t)2 * (c + q) + (q == 0)) * s.d + col, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) acc[k] += x[u][k];
   }
-#pragma unroll 8
-  for (int q = g; q < m; q += 16) {
-    const float* w = s.part + (int64_t)2 * (c + 1 + q) * s.d;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (col + k < s.d) acc[k] += w[col + k];
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) red[g][(threadIdx.x & 15) * 4 + k] = acc[k];
+  for (int k = 0; k < VEC; ++k) red[g][j * VEC + k] = acc[k];
   __syncthreads();
-  const int x = threadIdx.x, cx = blockIdx.y * 64 + x;
-  if (x >= 64 || cx >= s.d) return;
+  const int x = threadIdx.x, cx = blockIdx.y * C + x, used = min(m, G);
+  if (x >= C || cx >= s.d) return;
   float t = red[0][x];
-  for (int k = 1; k < 16; ++k) t += red[k][x];
+  for (int k = 1; k < used; ++k) t += red[k][x];
   float* w = s.dw + v * s.ldw + cx;
   *w = s.add ? *w + s.scale * t : s.scale * t;
 }
 
 // ---------------------------------------------------------------------------
-// Few tokens: block b < n sums the rows like token b if b is the first of its
-// kind; the blocks after them write zeros to the table rows without a token.
+// Few tokens: one launch, in which a block finds the tokens of one table row by
+// looking at all of them and sums their rows. By row, block v takes row v (and
+// writes its zeros if it has no token). By token, for tables with more rows than
+// tokens, block b < n takes the row of token b if b is the first of its kind,
+// and the blocks after them write the zeros of the other rows.
 // ---------------------------------------------------------------------------
-constexpr int kFewTokens = 1024, kFewThreads = 512, kFewZeroRows = 512;
+constexpr int kFewTokens = 8192, kFewThreads = 1024, kFewZeroRows = 512;
+constexpr int kFewEach = kFewTokens / kFewThreads;  // tokens a thread looks at, at most
 
 template <class T, int VEC, int LPR>
 __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int vocab, const int* __restrict__ tok,
                                                            int first, const T* __restrict__ dout, int64_t ldo,
-                                                           float scale, float* __restrict__ dw, int64_t ldw, int add) {
+                                                           float scale, float* __restrict__ dw, int64_t ldw, int add,
+                                                           int by_row) {
   constexpr int W = kFewThreads / 64, G = kFewThreads / LPR, U = 8;
   __shared__ int list[kFewTokens];
   __shared__ int wtot[W], has[kFewZeroRows];
   __shared__ float red[G][LPR * VEC];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  if ((int)blockIdx.x >= n) {
-    const int64_t v0 = (int64_t)(blockIdx.x - n) * kFewZeroRows;
-    for (int k = t; k < kFewZeroRows; k += kFewThreads) has[k] = 0;
-    __syncthreads();
-    for (int i = t; i < n; i += kFewThreads) {
-      const int64_t r = table_row(tok[i], first, vocab) - v0;
-      if (r >= 0 && r < kFewZeroRows) has[r] = 1;
-    }
-    __syncthreads();
-    const int rows = (int)min((int64_t)kFewZeroRows, vocab - v0);
-    for (int r = wave; r < rows; r += W) {
-      if (has[r]) continue;
-      float* w = dw + (v0 + r) * ldw;
-      const float none[VEC] = {};
-      for (int c = lane * VEC; c < d; c += 64 * VEC) store_v<VEC>(w + c, none);
+  if (!by_row && (int)blockIdx.x >= n) {
+    const int64_t step = (int64_t)(gridDim.x - n) * kFewZeroRows;
+    for (int64_t v0 = (int64_t)(blockIdx.x - n) * kFewZeroRows; v0 < vocab; v0 += step) {
+      for (int k = t; k < kFewZeroRows; k += kFewThreads) has[k] = 0;
+      __syncthreads();
+      for (int i = t; i < n; i += kFewThreads) {
+        const int row = table_row(tok[i], first, vocab);
+        if (row < vocab && row >= v0 && row < v0 + kFewZeroRows) has[row - v0] = 1;
+      }
+      __syncthreads();
+      const int rows = (int)min((int64_t)kFewZeroRows, vocab - v0);
+      for (int r = wave; r < rows; r += W) {
+        if (has[r]) continue;
+        float* w = dw + (v0 + r) * ldw;
+        const float none[VEC] = {};
+        for (int c = lane * VEC; c < d; c += 64 * VEC) store_v<VEC>(w + c, none);
+      }
+      __syncthreads();
     }
     return;
   }
-  const int b = blockIdx.x, v = table_row(tok[b], first, vocab);
+  const int b = blockIdx.x, v = by_row ? b : table_row(tok[b], first, vocab);
   if (v == vocab) return;
-  int m = 0;
-  for (int base = 0; base < n; base += kFewThreads) {
-    const int i = base + t;
-    const bool hit = i < n && table_row(tok[i], first, vocab) == v;
-    const unsigned long long w = __ballot(hit);
-    if (lane == 0) wtot[wave] = __popcll(w);
-    __syncthreads();
-    int at = m;
-    for (int k = 0; k < W; ++k) {
-      if (k < wave) at += wtot[k];
-      m += wtot[k];
-    }
-    if (hit) list[at + __popcll(w & ((1ull << lane) - 1))] = i;
-    __syncthreads();
-    if (m && list[0] != b) return;  // not the first of its kind
+  // the list of the row's tokens in order: each thread looks at `each`
+  // consecutive tokens, and a scan over the threads places its hits
+  const int each = (n + kFewThreads - 1) / kFewThreads;
+  unsigned hits = 0;
+#pragma unroll
+  for (int k = 0; k < kFewEach; ++k) {
+    const int i = t * each + k;
+    if (k < each && i < n && table_row(tok[i], first, vocab) == v) hits |= 1u << k;
   }
-  const int j = t % LPR, g = t / LPR;
-  const int q0 = (int)((int64_t)m * g / G), q1 = (int)((int64_t)m * (g + 1) / G);
+  const int mine = __popc(hits);
+  int incl = mine;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int x = __shfl_up(incl, off);
+    if (lane >= off) incl += x;
+  }
+  if (lane == 63) wtot[wave] = incl;
+  __syncthreads();
+  int at = incl - mine, m = 0;
+  for (int k = 0; k < W; ++k) {
+    if (k < wave) at += wtot[k];
+    m += wtot[k];
+  }
+  for (; hits; hits &= hits - 1) list[at++] = t * each + __ffs(hits) - 1;
+  __syncthreads();
+  if (!by_row && list[0] != b) return;  // not the first of its kind
+  if (add && m == 0) return;
+  const int j = t % LPR, g = t / LPR, groups = min(G, (m + U - 1) / U);
+  // a group's share of the list, at least U rows if there are as many
+  const int q0 = g < groups ? (int)((int64_t)m * g / groups) : 0, q1 = g < groups ? (int)((int64_t)m * (g + 1) / groups) : 0;
   for (int c0 = 0; c0 < d; c0 += LPR * VEC) {
     const int c = c0 + j * VEC;
     float acc[VEC] = {};
@@ -421,12 +462,17 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int voc
     __syncthreads();
     for (int x = t; x < LPR * VEC && c0 + x < d; x += kFewThreads) {
       float sum = red[0][x];
-      for (int k = 1; k < G; ++k) sum += red[k][x];
+      for (int k = 1; k < groups; ++k) sum += red[k][x];
       float* w = dw + v * ldw + c0 + x;
       *w = add ? *w + scale * sum : scale * sum;
     }
     __syncthreads();
   }
+}
+
+// Whether a call takes the one launch: what its blocks look at must stay small.
+bool few_tokens(int64_t n, int64_t vocab) {
+  return n <= kFewTokens && std::min(n, vocab) * n <= (1 << 20);
 }
 
 // Lanes a row: the fewest of 16, 32 and 64 that hold d values, 4 each.
@@ -449,9 +495,9 @@ int check_embed(const char* who, int64_t n, int32_t d, int64_t vocab, int32_t dt
   return CHGNET_OK;
 }
 
-// Length of a chunk of the ordered positions: about 4,096 chunks, whose rows in
+// Length of a chunk of the ordered positions: about 8,192 chunks, whose rows in
 // flight fill the chip, of 16 to 256 positions.
-int chunk_of(int64_t n) { return (int)std::min<int64_t>(256, std::max<int64_t>(16, cdiv(n, 4096))); }
+int chunk_of(int64_t n) { return (int)std::min<int64_t>(256, std::max<int64_t>(16, cdiv(n, 8192))); }
 
 constexpr int64_t kMaxTokens = 1 << 30;  // positions and the ends of chunks are 32-bit
 
@@ -459,8 +505,8 @@ struct EmbedWs {
   int *row[2], *pos[2], *counts;
   float* part;
 };
-void carve_embed(Arena& ar, int64_t n, int32_t d, EmbedWs& w) {
-  if (n <= kFewTokens) return;
+void carve_embed(Arena& ar, int64_t n, int32_t d, int64_t vocab, EmbedWs& w) {
+  if (few_tokens(n, vocab)) return;
   for (int k = 0; k < 2; ++k) {
     w.row[k] = ar.take<int>(n);
     w.pos[k] = ar.take<int>(n);
@@ -500,8 +546,8 @@ int embed_backward_workspace_entry(int64_t n, int32_t d, int64_t vocab, size_t* 
   if (!bytes) return fail(CHGNET_EINVAL, "embed_backward_workspace: bytes is NULL");
   Arena ar;
   EmbedWs w;
-  carve_embed(ar, n, d, w);
-  *bytes = align_up(ar.used + 256, 256);  // (with room to align the first array)
+  carve_embed(ar, n, d, vocab, w);
+  *bytes = ar.used;
   return CHGNET_OK;
 }
 
@@ -518,15 +564,16 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
   const int n = (int)n64, vocab = (int)vocab64;
   const int add = accumulate != 0;
   const bool vec = d % 4 == 0 && ldo % 4 == 0 && ldw % 4 == 0 && aligned_to(dout, 4 * es) && aligned_to(dtable, 16);
-  if (n <= kFewTokens) {
-    const unsigned zero = add ? 0 : (unsigned)cdiv(vocab, kFewZeroRows);
-    if (n + zero == 0) return CHGNET_OK;
+  if (few_tokens(n, vocab)) {
+    if (n == 0 && add) return CHGNET_OK;
+    const bool by_row = vocab <= n;
+    const unsigned blocks = (unsigned)(by_row ? vocab : n + (add ? 0 : std::min<int64_t>(4096, cdiv(vocab, kFewZeroRows))));
     return with_type(dtype, [&](auto t) {
       using T = decltype(t);
       return with_lanes(d, vec, [&](auto V, auto L) -> int {
         KLAUNCH(st, "k_embed_few",
-                k_embed_few<T, V.value, L.value><<<n + zero, kFewThreads, 0, st>>>(
-                    n, d, vocab, tok, first, static_cast<const T*>(dout), ldo, scale, dtable, ldw, add));
+                k_embed_few<T, V.value, L.value><<<blocks, kFewThreads, 0, st>>>(
+                    n, d, vocab, tok, first, static_cast<const T*>(dout), ldo, scale, dtable, ldw, add, by_row));
         return CHGNET_OK;
       });
     });
@@ -538,7 +585,7 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
   if (!aligned_to(ws, 16)) return fail(CHGNET_EINVAL, "embed_backward: ws is not 16-byte aligned");
   Arena ar{static_cast<char*>(ws), ws_bytes, 0};
   EmbedWs w{};
-  carve_embed(ar, n, d, w);
+  carve_embed(ar, n, d, vocab, w);
   // digits of the rows 0 .. vocab (vocab: no row), split evenly over the passes
   int bits = 1;
   while (bits < 31 && (vocab >> bits) != 0) ++bits;
@@ -586,8 +633,13 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
       return CHGNET_OK;
     });
   }));
-  if (r.nchunks > 1)
-    KLAUNCH(st, "k_embed_join", k_embed_join<<<dim3(r.nchunks - 1, (unsigned)cdiv(d, 64)), 256, 0, st>>>(r));
+  if (r.nchunks > 1) {
+    // the partial rows are dense: 16-byte loads where their width allows
+    if (d % 4 == 0)
+      KLAUNCH(st, "k_embed_join", k_embed_join<4><<<dim3(r.nchunks - 1, (unsigned)cdiv(d, 64)), kJoinThreads, 0, st>>>(r));
+    else
+      KLAUNCH(st, "k_embed_join", k_embed_join<1><<<dim3(r.nchunks - 1, (unsigned)cdiv(d, 16)), kJoinThreads, 0, st>>>(r));
+  }
   return CHGNET_OK;
 }
 

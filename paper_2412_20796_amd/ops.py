@@ -7,11 +7,13 @@ device memory and the stream (the current one of the tensors' device), and a
 missing library raises. Every tensor of a call is on one GPU; rows may have a
 stride, columns are contiguous. Inputs are not differentiated by autograd: a
 ``torch.autograd.Function`` of the caller's calls the two passes.
+
+The calls on few rows take as long as their launches, about 4 us each; the checks
+are written so that they add little to that (a dozen attribute reads).
 """
 from __future__ import annotations
 
 import ctypes
-from dataclasses import dataclass
 
 import torch
 
@@ -45,63 +47,70 @@ def _bad(msg):
     raise bd.ChgnetError(bd.CHGNET_EINVAL, msg)
 
 
-def _matrix(name, t, rows, cols, dtypes, device):
-    """Row stride of a [rows, cols] tensor of one of `dtypes` on `device`."""
-    if t.dim() != 2 or t.dtype not in dtypes or t.device != device or tuple(t.shape) != (rows, cols):
-        _bad("%s must be [%d, %d] of %s on %s, not %s %s on %s"
-             % (name, rows, cols, " or ".join(map(str, dtypes)), device, list(t.shape), t.dtype, t.device))
-    if cols > 1 and t.stride(1) != 1:
+def _wrong(name, t, shape, what, gpu):
+    _bad("%s must be %s of %s on GPU %d, not %s %s on %s" % (name, list(shape), what, gpu, list(t.shape), t.dtype, t.device))
+
+
+def _rows(name, t, rows, cols, dtype, gpu):
+    """Row stride of a [rows, cols] tensor of `dtype` on GPU `gpu`."""
+    if t.dtype is not dtype or t.get_device() != gpu or t.shape != (rows, cols):
+        _wrong(name, t, (rows, cols), dtype, gpu)
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         _bad("%s must have contiguous columns" % name)
-    ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
     if ld < cols:
-        _bad("%s has overlapping rows" % name)
+        if rows > 1:
+            _bad("%s has overlapping rows" % name)
+        ld = cols
     return ld
 
 
-def _packed(name, t, shape, dtype, device):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        _bad("%s must be contiguous %s of %s on %s, not %s %s on %s"
-             % (name, list(shape), dtype, device, list(t.shape), t.dtype, t.device))
+def _packed(name, t, shape, dtype, gpu):
+    if t.dtype is not dtype or t.get_device() != gpu or t.shape != shape or not t.is_contiguous():
+        _wrong(name, t, shape, "contiguous %s" % dtype, gpu)
 
 
-def _gpu(name, t):
-    if not t.is_cuda:
+def _start(name, t):
+    """(rows, columns, type code, GPU) of a call's first tensor."""
+    code = DTYPES.get(t.dtype)
+    if code is None or t.dim() != 2:
+        _bad("%s must be a matrix of fp32, bf16 or fp16, not %s %s" % (name, list(t.shape), t.dtype))
+    gpu = t.get_device()
+    if gpu < 0:
         _bad("%s must be on a GPU" % name)
-    return t.device
+    return *t.shape, code, gpu
 
 
-class _On:
-    """The tensors' device as the current one for a call, and its current stream."""
-
-    def __init__(self, device):
-        self.index = device.index
-
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream(self.index).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
+def _call(fn, gpu, args):
+    """The call on the GPU's current stream, with the GPU as the current device."""
+    before = torch.cuda.current_device()
+    if before == gpu:
+        code = fn(*args, torch._C._cuda_getCurrentRawStream(gpu))
+    else:
+        with torch.cuda.device(gpu):
+            code = fn(*args, torch._C._cuda_getCurrentRawStream(gpu))
+    if code:
+        bd._check(code)
 
 
-def _workspace(ws, nbytes, device):
+def _workspace(ws, nbytes, gpu, like):
     """(pointer, size, owner) of the caller's Workspace grown to nbytes, or of memory for this call."""
-    if ws is not None:
-        if torch.device(ws.device).type != "cuda" or ws.ensure(nbytes).device != device:
-            _bad("the workspace must be on %s" % device)
-        return ws.buf.data_ptr(), ws.nbytes, ws
-    buf = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+    if ws is None:
+        buf = torch.empty(nbytes or 1, dtype=torch.uint8, device=like.device)
+    else:
+        buf = ws.ensure(nbytes)
+        if buf.get_device() != gpu:
+            _bad("the workspace must be on GPU %d" % gpu)
     return buf.data_ptr(), buf.numel(), buf
 
 
-@dataclass
 class GateCheckpoint:
     """8-bit checkpoint of a gate's input: codes [rows, 2d] uint8 and step [rows, 2] fp32 (core, gate)."""
-    codes: torch.Tensor
-    step: torch.Tensor
+
+    __slots__ = ("codes", "step")
+
+    def __init__(self, codes, step):
+        self.codes, self.step = codes, step
 
     @classmethod
     def empty(cls, rows, d, device="cuda"):
@@ -112,101 +121,97 @@ class GateCheckpoint:
     def nbytes(self):
         return self.codes.numel() + 4 * self.step.numel()
 
+    def _check(self, rows, d, gpu):
+        _packed("kept.codes", self.codes, (rows, 2 * d), torch.uint8, gpu)
+        _packed("kept.step", self.step, (rows, 2), torch.float32, gpu)
+
 
 def gate_forward(z, ln, save=True, phi=None, kept=None):
     """phi [rows, d] of z [rows, 2d] (core | gate) and ln [4, d] fp32 (g_c, b_c, g_g, b_g); z in fp32, bf16 or fp16.
     With `save` returns (phi, GateCheckpoint) for gate_backward, else phi. phi and kept: tensors to write into."""
-    if z.dim() != 2 or z.shape[1] % 2 or z.shape[1] == 0 or z.dtype not in DTYPES:
-        _bad("z must be [rows, 2d] in fp32, bf16 or fp16, not %s %s" % (list(z.shape), z.dtype))
-    dev = _gpu("z", z)
-    rows, d = z.shape[0], z.shape[1] // 2
-    ldz = _matrix("z", z, rows, 2 * d, (z.dtype,), dev)
-    _packed("ln", ln, (4, d), torch.float32, dev)
+    rows, cols, code, gpu = _start("z", z)
+    d = cols // 2
+    if cols != 2 * d:
+        _bad("z must have an even number of columns, core | gate")
+    ldz = _rows("z", z, rows, cols, z.dtype, gpu)
+    _packed("ln", ln, (4, d), torch.float32, gpu)
     if phi is None:
-        phi = torch.empty(rows, d, dtype=z.dtype, device=dev)
-    ldp = _matrix("phi", phi, rows, d, (z.dtype,), dev)
+        phi, ldp = torch.empty((rows, d), dtype=z.dtype, device=z.device), d
+    else:
+        ldp = _rows("phi", phi, rows, d, z.dtype, gpu)
     if not save:
         if kept is not None:
             _bad("a checkpoint is given but not to be kept")
-    elif kept is None:
-        kept = GateCheckpoint.empty(rows, d, dev)
+        _call(lib().chgnet_gate_forward, gpu, (rows, d, code, z.data_ptr(), ldz, ln.data_ptr(), phi.data_ptr(), ldp,
+                                               None, None))
+        return phi
+    if kept is None:
+        kept = GateCheckpoint.empty(rows, d, z.device)
     else:
-        _packed("kept.codes", kept.codes, (rows, 2 * d), torch.uint8, dev)
-        _packed("kept.step", kept.step, (rows, 2), torch.float32, dev)
-    with _On(dev) as stream:
-        bd._check(lib().chgnet_gate_forward(rows, d, DTYPES[z.dtype], z.data_ptr(), ldz, ln.data_ptr(), phi.data_ptr(),
-                                            ldp, kept.codes.data_ptr() or None if save else None,
-                                            kept.step.data_ptr() or None if save else None, stream))
-    return (phi, kept) if save else phi
+        kept._check(rows, d, gpu)
+    _call(lib().chgnet_gate_forward, gpu, (rows, d, code, z.data_ptr(), ldz, ln.data_ptr(), phi.data_ptr(), ldp,
+                                           kept.codes.data_ptr() or None, kept.step.data_ptr() or None))
+    return phi, kept
 
 
 def gate_backward(kept, ln, dphi, dz=None, dln=None, accumulate=False, ws=None):
     """(dz [rows, 2d], dln [4, d]) from the checkpoint of gate_forward and dphi [rows, d]; dln is fp32 and added to what
     it holds with `accumulate`. ws: a Workspace of the caller's (one for each call that may run at the same time)."""
-    if dphi.dim() != 2 or dphi.dtype not in DTYPES:
-        _bad("dphi must be [rows, d] in fp32, bf16 or fp16, not %s %s" % (list(dphi.shape), dphi.dtype))
-    dev = _gpu("dphi", dphi)
-    rows, d = dphi.shape
-    ldp = _matrix("dphi", dphi, rows, d, (dphi.dtype,), dev)
-    _packed("kept.codes", kept.codes, (rows, 2 * d), torch.uint8, dev)
-    _packed("kept.step", kept.step, (rows, 2), torch.float32, dev)
-    _packed("ln", ln, (4, d), torch.float32, dev)
+    rows, d, code, gpu = _start("dphi", dphi)
+    ldp = _rows("dphi", dphi, rows, d, dphi.dtype, gpu)
+    kept._check(rows, d, gpu)
+    _packed("ln", ln, (4, d), torch.float32, gpu)
     if dz is None:
-        dz = torch.empty(rows, 2 * d, dtype=dphi.dtype, device=dev)
-    ldz = _matrix("dz", dz, rows, 2 * d, (dphi.dtype,), dev)
+        dz, ldz = torch.empty((rows, 2 * d), dtype=dphi.dtype, device=dphi.device), 2 * d
+    else:
+        ldz = _rows("dz", dz, rows, 2 * d, dphi.dtype, gpu)
     if dln is None:
         if accumulate:
             _bad("accumulate needs a dln to add to")
-        dln = torch.empty(4, d, dtype=torch.float32, device=dev)
-    _packed("dln", dln, (4, d), torch.float32, dev)
-    need = ctypes.c_size_t()
-    bd._check(lib().chgnet_gate_backward_workspace(rows, d, ctypes.byref(need)))
-    with _On(dev) as stream:
-        p, nbytes, _keep = _workspace(ws, need.value, dev)
-        bd._check(lib().chgnet_gate_backward(rows, d, DTYPES[dphi.dtype], kept.codes.data_ptr(), kept.step.data_ptr(),
-                                             ln.data_ptr(), dphi.data_ptr(), ldp, dz.data_ptr(), ldz, dln.data_ptr(),
-                                             int(accumulate), p, nbytes, stream))
+        dln = torch.empty((4, d), dtype=torch.float32, device=dphi.device)
+    else:
+        _packed("dln", dln, (4, d), torch.float32, gpu)
+    L, need = lib(), ctypes.c_size_t()
+    bd._check(L.chgnet_gate_backward_workspace(rows, d, ctypes.byref(need)))
+    p, nbytes, _keep = _workspace(ws, need.value, gpu, dphi)
+    _call(L.chgnet_gate_backward, gpu, (rows, d, code, kept.codes.data_ptr(), kept.step.data_ptr(), ln.data_ptr(),
+                                        dphi.data_ptr(), ldp, dz.data_ptr(), ldz, dln.data_ptr(), bool(accumulate), p,
+                                        nbytes))
     return dz, dln
 
 
 def embed_forward(table, tok, scale=1.0, first=0, out=None):
     """out [n, d] = scale * table[tok - first] for int32 tokens [n]; zeros for tokens outside the table [vocab, d]."""
-    if table.dim() != 2 or table.dtype not in DTYPES:
-        _bad("table must be [vocab, d] in fp32, bf16 or fp16, not %s %s" % (list(table.shape), table.dtype))
-    dev = _gpu("table", table)
-    vocab, d = table.shape
-    ldt = _matrix("table", table, vocab, d, (table.dtype,), dev)
+    vocab, d, code, gpu = _start("table", table)
+    ldt = _rows("table", table, vocab, d, table.dtype, gpu)
     n = tok.numel()
-    _packed("tok", tok, (n,), torch.int32, dev)
+    _packed("tok", tok, (n,), torch.int32, gpu)
     if out is None:
-        out = torch.empty(n, d, dtype=table.dtype, device=dev)
-    ldo = _matrix("out", out, n, d, (table.dtype,), dev)
-    with _On(dev) as stream:
-        bd._check(lib().chgnet_embed_forward(n, d, vocab, DTYPES[table.dtype], tok.data_ptr(), first, table.data_ptr(),
-                                             ldt, scale, out.data_ptr(), ldo, stream))
+        out, ldo = torch.empty((n, d), dtype=table.dtype, device=table.device), d
+    else:
+        ldo = _rows("out", out, n, d, table.dtype, gpu)
+    _call(lib().chgnet_embed_forward, gpu, (n, d, vocab, code, tok.data_ptr(), first, table.data_ptr(), ldt, scale,
+                                            out.data_ptr(), ldo))
     return out
 
 
 def embed_backward(tok, dout, vocab, scale=1.0, first=0, dtable=None, accumulate=False, ws=None):
     """dtable [vocab, d] fp32: row v = scale * the sum of dout [n, d] over the tokens with tok - first = v, added to what
     it holds with `accumulate`. ws: a Workspace of the caller's (one for each call that may run at the same time)."""
-    if dout.dim() != 2 or dout.dtype not in DTYPES:
-        _bad("dout must be [n, d] in fp32, bf16 or fp16, not %s %s" % (list(dout.shape), dout.dtype))
-    dev = _gpu("dout", dout)
+    n, d, code, gpu = _start("dout", dout)
     if vocab < 1:
         _bad("vocab must be at least 1")
-    n, d = dout.shape
-    ldo = _matrix("dout", dout, n, d, (dout.dtype,), dev)
-    _packed("tok", tok, (n,), torch.int32, dev)
+    ldo = _rows("dout", dout, n, d, dout.dtype, gpu)
+    _packed("tok", tok, (n,), torch.int32, gpu)
     if dtable is None:
         if accumulate:
             _bad("accumulate needs a dtable to add to")
-        dtable = torch.empty(vocab, d, dtype=torch.float32, device=dev)
-    ldw = _matrix("dtable", dtable, vocab, d, (torch.float32,), dev)
-    need = ctypes.c_size_t()
-    bd._check(lib().chgnet_embed_backward_workspace(n, d, vocab, ctypes.byref(need)))
-    with _On(dev) as stream:
-        p, nbytes, _keep = _workspace(ws, need.value, dev)
-        bd._check(lib().chgnet_embed_backward(n, d, vocab, DTYPES[dout.dtype], tok.data_ptr(), first, dout.data_ptr(),
-                                              ldo, scale, dtable.data_ptr(), ldw, int(accumulate), p, nbytes, stream))
+        dtable, ldw = torch.empty((vocab, d), dtype=torch.float32, device=dout.device), d
+    else:
+        ldw = _rows("dtable", dtable, vocab, d, torch.float32, gpu)
+    L, need = lib(), ctypes.c_size_t()
+    bd._check(L.chgnet_embed_backward_workspace(n, d, vocab, ctypes.byref(need)))
+    p, nbytes, _keep = _workspace(ws, need.value, gpu, dout) if need.value else (None, 0, None)
+    _call(L.chgnet_embed_backward, gpu, (n, d, vocab, code, tok.data_ptr(), first, dout.data_ptr(), ldo, scale,
+                                         dtable.data_ptr(), ldw, bool(accumulate), p, nbytes))
     return dtable

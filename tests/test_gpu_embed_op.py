@@ -76,12 +76,13 @@ def test_lookup_strides():
             assert bool((out[37:] == 7).all()) and bool((out[:, d:] == 7).all())
 
 
-# sizes below and above the switch to the ordering (1,024 tokens), around its stretches of 1,024 tokens a block, its
-# chunks of 16 and more, digits of one to three passes, and widths of one and several column blocks
+# sizes below and above the switch to the ordering (8,192 tokens, 2^20 tokens looked at), around its stretches of 1,024
+# tokens a block, its chunks of 16 and more, digits of one to three passes, widths of one and several column blocks
 @pytest.mark.parametrize("how", ["random", "one", "two ends", "in order", "outside", "none", "skewed"])
 @pytest.mark.parametrize("n,vocab,d", [(1, 1, 1), (1, 94, 64), (63, 94, 64), (513, 94, 128), (1023, 3000, 20),
                                        (1024, 94, 128), (1025, 94, 128), (1040, 1, 64), (2047, 2, 64), (2048, 255, 130),
-                                       (2049, 256, 65), (5844, 94, 128), (9999, 70000, 33), (16400, 300, 512),
+                                       (2049, 256, 65), (5844, 94, 128), (8192, 128, 64), (8192, 129, 64),
+                                       (8193, 94, 64), (9999, 70000, 33), (16400, 300, 512),
                                        (40000, 1000, 9), (300007, 94, 64)])
 def test_gradient(n, vocab, d, how):
     first = n % 2
@@ -91,7 +92,8 @@ def test_gradient(n, vocab, d, how):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n,vocab,d", [(700, 94, 64), (3000, 94, 128), (3000, 500, 256), (2000, 50, 77), (5000, 40, 1024)])
+@pytest.mark.parametrize("n,vocab,d", [(700, 94, 64), (3000, 94, 128), (3000, 500, 256), (2000, 50, 77), (9000, 50, 77), (5000, 40, 1024),
+                                       (12000, 40, 1024)])
 def test_gradient_types(n, vocab, d, dtype):
     tok, dout = _tokens(n, vocab, 0, "skewed"), _rand(n, d, dtype)
     r, b = ref.embed_grad(tok, dout, vocab, d ** 0.5, 0)
@@ -116,7 +118,7 @@ def test_gradient_is_the_adjoint_of_the_lookup():
         ref.embed_grad(tok, y, vocab, scale, 1)[1][7, 9]) + scale * ref.U * float(y[:, 9].abs().sum())
 
 
-@pytest.mark.parametrize("n", [0, 40, 1024, 1025, 6000])
+@pytest.mark.parametrize("n", [0, 40, 1024, 1025, 6000, 20000])
 def test_accumulate(n):
     vocab, d = 94, 64
     tok, dout = _tokens(n, vocab, 0, "skewed"), _rand(n, d, torch.float32)
@@ -132,7 +134,7 @@ def test_accumulate(n):
         assert not bool(once.any())
 
 
-@pytest.mark.parametrize("n", [200, 3000])
+@pytest.mark.parametrize("n", [200, 3000, 9000])
 def test_gradient_strides(n):
     vocab = 94
     for dtype in TYPES:
@@ -147,7 +149,7 @@ def test_gradient_strides(n):
             assert bool((out[:, d:] == 7).all()) and bool((out[0] == 7).all()) and bool((out[vocab + 1] == 7).all())
 
 
-@pytest.mark.parametrize("n", [500, 4000])
+@pytest.mark.parametrize("n", [500, 4000, 9000])
 def test_gradient_of_values_that_are_not_finite(n):
     tok, dout = _tokens(n, 94, 0, "random"), _rand(n, 64, torch.float32)
     tok[n // 2] = 17

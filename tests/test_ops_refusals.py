@@ -25,7 +25,7 @@ GATE_F = dict(rows=8, d=64, dtype=0, z=P, ldz=128, ln=P, phi=P, ldphi=64, codes=
 GATE_B = dict(rows=8, d=64, dtype=0, codes=P, step=P, ln=P, dphi=P, lddphi=64, dz=P, lddz=128, dln=P, accumulate=0, ws=P,
               ws_bytes=1 << 20, stream=None)
 EMB_F = dict(n=8, d=64, vocab=94, dtype=0, tok=P, first=1, table=P, ldtable=64, scale=1.0, out=P, ldout=64, stream=None)
-EMB_B = dict(n=8192, d=64, vocab=94, dtype=0, tok=P, first=1, dout=P, lddout=64, scale=1.0, dtable=P, lddtable=64,
+EMB_B = dict(n=20000, d=64, vocab=94, dtype=0, tok=P, first=1, dout=P, lddout=64, scale=1.0, dtable=P, lddtable=64,
              accumulate=0, ws=P, ws_bytes=1 << 26, stream=None)
 BAD = [
     ("chgnet_gate_forward", GATE_F, dict(rows=-1)),
