@@ -12,21 +12,40 @@ namespace chg {
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
 
-// V consecutive values (V = 1 or 4), aligned to their total size
+// V consecutive values (V = 1, 4 or 8), aligned to their total size, at most 16 bytes
 template <int V, class T>
 __device__ __forceinline__ void load_v(const T* p, float (&v)[V]) {
-  typedef T vec __attribute__((ext_vector_type(V)));
-  const vec t = *reinterpret_cast<const vec*>(p);
+  if constexpr (V * sizeof(T) > 16) {
+    float a[V / 2], b[V / 2];
+    load_v<V / 2>(p, a);
+    load_v<V / 2>(p + V / 2, b);
 #pragma unroll
-  for (int k = 0; k < V; ++k) v[k] = (float)t[k];
+    for (int k = 0; k < V; ++k) v[k] = k < V / 2 ? a[k % (V / 2)] : b[k % (V / 2)];
+  } else {
+    typedef T vec __attribute__((ext_vector_type(V)));
+    const vec t = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = (float)t[k];
+  }
 }
 template <int V, class T>
 __device__ __forceinline__ void store_v(T* p, const float (&v)[V]) {
-  typedef T vec __attribute__((ext_vector_type(V)));
-  vec t;
+  if constexpr (V * sizeof(T) > 16) {
+    float a[V / 2], b[V / 2];
 #pragma unroll
-  for (int k = 0; k < V; ++k) t[k] = (T)v[k];
-  *reinterpret_cast<vec*>(p) = t;
+    for (int k = 0; k < V / 2; ++k) {
+      a[k] = v[k];
+      b[k] = v[V / 2 + k];
+    }
+    store_v<V / 2>(p, a);
+    store_v<V / 2>(p + V / 2, b);
+  } else {
+    typedef T vec __attribute__((ext_vector_type(V)));
+    vec t;
+#pragma unroll
+    for (int k = 0; k < V; ++k) t[k] = (T)v[k];
+    *reinterpret_cast<vec*>(p) = t;
+  }
 }
 
 inline int elem_size(int32_t dtype) { return dtype == CHGNET_F32 ? 4 : dtype == CHGNET_BF16 || dtype == CHGNET_F16 ? 2 : 0; }

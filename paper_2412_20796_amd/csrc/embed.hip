@@ -68,8 +68,7 @@ __global__ void __launch_bounds__(256) k_embed_fwd(int64_t n, int d, int vocab, 
 // ---------------------------------------------------------------------------
 // Ordering of the positions by table row: passes over digits of at most 8 bits,
 // least significant first, each stable. A pass is two launches over at most
-// kSortBlocks blocks, each with a contiguous stretch of the tokens, taken 1,024
-// at a time: the counts of every digit in every stretch, then the places. A
+// kSortBlocks blocks, each with a contiguous stretch of the tokens: the counts of every digit in every stretch, then the places. A
 // block of the second launch adds up the counts of the stretches before its own
 // and of the lower digits itself (at most 256 x 256 numbers, in L2), so that no
 // scan stands between the two.
@@ -100,22 +99,9 @@ __device__ __forceinline__ unsigned long long same_digit(int digit, int bits, bo
   return m;
 }
 
-// Counts of the digits, and (fill blocks, after the counting ones) zeros in the
-// table rows: a row's sums overwrite them later.
-__global__ void __launch_bounds__(kSortThreads) k_embed_count(SortPass s, int nsort, int64_t zrows, int d, float* zero,
-                                                              int64_t ldz) {
+__global__ void __launch_bounds__(kSortThreads) k_embed_count(SortPass s) {
   __shared__ int cnt[kDigits];
   const int t = threadIdx.x;
-  if ((int)blockIdx.x >= nsort) {
-    const int64_t total = zrows * d, step = (int64_t)(gridDim.x - nsort) * kSortThreads;
-    int64_t i = (int64_t)(blockIdx.x - nsort) * kSortThreads + t;
-    if (ldz == d && total % 4 == 0 && reinterpret_cast<uintptr_t>(zero) % 16 == 0) {
-      for (; i < total / 4; i += step) reinterpret_cast<float4*>(zero)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    } else {
-      for (; i < total; i += step) zero[i / d * ldz + i % d] = 0.f;
-    }
-    return;
-  }
   if (t < kDigits) cnt[t] = 0;
   __syncthreads();
   const int64_t i0 = (int64_t)blockIdx.x * s.len, i1 = min(i0 + s.len, (int64_t)s.n);
@@ -130,7 +116,9 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_count(SortPass s, int ns
   if (t < kDigits) s.counts[blockIdx.x * kDigits + t] = cnt[t];
 }
 
+template <int kRounds>
 __global__ void __launch_bounds__(kSortThreads) k_embed_place(SortPass s) {
+  const int mask = (1 << s.bits) - 1;
   constexpr int W = kSortThreads / 64;
   __shared__ int place[kDigits];     // next place of each digit
   __shared__ int wcnt[W][kDigits];   // counts, then first places, of each wavefront's digits
@@ -179,18 +167,32 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_place(SortPass s) {
       at += c[k];
     }
   }
+  // kRounds tokens a thread and turn: a wavefront takes kRounds x 64 consecutive
+  // tokens in rounds of 64 and counts its digits as it goes, so that the block
+  // meets three times for all of them
   const int64_t i0 = (int64_t)blockIdx.x * s.len, i1 = min(i0 + s.len, (int64_t)s.n);
-  for (int64_t base = i0; base < i1; base += kSortThreads) {
+  for (int64_t base = i0; base < i1; base += kSortThreads * kRounds) {
     __syncthreads();
     for (int k = t; k < W * kDigits; k += kSortThreads) (&wcnt[0][0])[k] = 0;
     __syncthreads();
-    const int64_t i = base + t;
-    const bool valid = i < i1;
-    const int row = valid ? sort_row(s, (int)i) : 0;
-    const int digit = (row >> s.shift) & ((1 << s.bits) - 1);
-    const unsigned long long m = same_digit(digit, s.bits, valid);
-    const int rank = __popcll(m & ((1ull << lane) - 1));
-    if (valid && rank == 0) wcnt[wave][digit] = __popcll(m);
+    int row[kRounds], rank[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      const int64_t i = base + (wave * kRounds + r) * 64 + lane;
+      row[r] = i < i1 ? sort_row(s, (int)i) : -1;
+    }
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      const bool valid = row[r] >= 0;
+      const int digit = (row[r] >> s.shift) & mask;
+      const unsigned long long m = same_digit(digit, s.bits, valid);
+      const int before = __popcll(m & ((1ull << lane) - 1));
+      rank[r] = before + wcnt[wave][digit];
+      // (a wavefront's LDS accesses stay in order)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (valid && before == 0) wcnt[wave][digit] += __popcll(m);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
     __syncthreads();
     if (t < kDigits) {
       int at = place[t];
@@ -203,10 +205,13 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_place(SortPass s) {
       place[t] = at;
     }
     __syncthreads();
-    if (valid) {
-      const int to = wcnt[wave][digit] + rank;
-      s.row_out[to] = row;
-      s.pos_out[to] = s.tok ? (int)i : s.pos[i];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      if (row[r] < 0) continue;
+      const int i = (int)base + (wave * kRounds + r) * 64 + lane;
+      const int to = wcnt[wave][(row[r] >> s.shift) & mask] + rank[r];
+      s.row_out[to] = row[r];
+      s.pos_out[to] = s.tok ? i : s.pos[i];
     }
   }
 }
@@ -215,41 +220,90 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_place(SortPass s) {
 // Sums of the ordered rows. Groups of LPR lanes (VEC NQ values a lane; the
 // launch's y blocks take further columns) each add the rows of one chunk, eight
 // loads in flight, and write a run's sum when it ends. A run that began in an
-// earlier chunk or goes on in the next is a partial sum instead: slot 0 of the
-// chunk for a run that began before it, slot 1 for one that begins in it and
-// goes on.
+// earlier chunk or goes on in the next is a partial sum in LDS instead: slot 0 of
+// the chunk for a run that began before it, slot 1 for one that begins in it and
+// goes on. The block then joins its chunks' partial sums in order, and what
+// crosses the block's stretch is one partial row of slot 0 and one of slot 1 in
+// the workspace. The launch's first `nzero` blocks look up 512 table rows each
+// among the ordered ones and write the zeros of those that no token has.
 // ---------------------------------------------------------------------------
 struct RunSums {
-  int n, vocab, chunk, nchunks, d;
+  int n, vocab, chunk, stretch, nstretch, d;  // stretch: positions of a block
   const int *row, *pos;
   int64_t ldo, ldw;
   float scale;
   float* dw;
   int add;
-  float* part;  // [nchunks][2][d]
+  float* part;  // [nstretch][2][d]
+  int nzero;
 };
+constexpr int kRunThreads = 512;
+
+// zeros in the rows of v0 .. v0 + kRunThreads - 1 without a token, columns [col0, col1)
+template <int VEC>
+__device__ __forceinline__ void zero_rows(const RunSums& s, int64_t v0, int col0, int col1) {
+  __shared__ int none[kRunThreads];
+  const int t = threadIdx.x, lane = t & 63;
+  const int64_t v = v0 + t;
+  if (v < s.vocab) {
+    int lo = -1, hi = s.n;  // first position whose row is v or later: hi
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (s.row[mid] < v) lo = mid;
+      else hi = mid;
+    }
+    none[t] = hi == s.n || s.row[hi] != v;
+  }
+  __syncthreads();
+  const int rows = (int)min((int64_t)kRunThreads, s.vocab - v0);
+  for (int r = t >> 6; r < rows; r += kRunThreads / 64) {
+    if (!none[r]) continue;
+    float* w = s.dw + (v0 + r) * s.ldw;
+    const float zero[VEC] = {};
+    for (int c = col0 + lane * VEC; c < col1; c += 64 * VEC) store_v<VEC>(w + c, zero);
+  }
+}
 
 template <class T, int VEC, int LPR, int NQ>
-__global__ void __launch_bounds__(256) k_embed_runs(RunSums s, const T* __restrict__ dout) {
-  constexpr int G = 256 / LPR, U = 8, CPL = VEC * NQ;
-  const int j = threadIdx.x % LPR;
-  const int c = blockIdx.x * G + threadIdx.x / LPR;
-  if (c >= s.nchunks) return;
-  const int col0 = blockIdx.y * LPR * CPL;
-  const int p0 = c * s.chunk, p1 = min(p0 + s.chunk, s.n);
-  float acc[CPL];
+__global__ void __launch_bounds__(kRunThreads) k_embed_runs(RunSums s, const T* __restrict__ dout) {
+  constexpr int G = kRunThreads / LPR, U = 8, CPL = VEC * NQ, C = LPR * CPL;
+  __shared__ float part[G][2][C];
+  __shared__ int first[G], kind[G];  // kind bits: 1 slot 0 used, 2 slot 1 used, 4 slot 0's run goes on
+  const int j = threadIdx.x % LPR, g = threadIdx.x / LPR;
+  const int col0 = blockIdx.y * C;
+  const int blk = (int)blockIdx.x - s.nzero;
+  if (blk < 0) {
+    zero_rows<VEC < 4 ? VEC : 4>(s, (int64_t)blockIdx.x * kRunThreads, col0, min(col0 + C, s.d));
+    return;
+  }
+  const int b0 = blk * s.stretch, b1 = min(b0 + s.stretch, s.n);
+  const int p0 = b0 + g * s.chunk, p1 = min(p0 + s.chunk, b1);
+  auto column = [&](int q) { return (q * LPR + j) * VEC; };  // within the block's columns
+  if (j == 0) kind[g] = 0;
+  if (p0 < p1) {
+    float acc[CPL];
 #pragma unroll
-  for (int k = 0; k < CPL; ++k) acc[k] = 0.f;
-  int cur = s.row[p0];
-  bool began = p0 == 0 || s.row[p0 - 1] != cur;  // the run starts in this chunk
-  auto column = [&](int q) { return col0 + (q * LPR + j) * VEC; };
-  auto flush = [&](bool goes_on) {
-    if (cur >= s.vocab) return;
-    if (began && !goes_on) {
-      float* w = s.dw + cur * s.ldw;
+    for (int k = 0; k < CPL; ++k) acc[k] = 0.f;
+    int cur = s.row[p0];
+    if (j == 0) first[g] = cur;
+    bool began = p0 == 0 || s.row[p0 - 1] != cur;  // the run starts in this chunk
+    auto keep = [&](int slot) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) part[g][slot][column(q) + k] = acc[q * VEC + k];
+    };
+    auto flush = [&]() {
+      if (cur >= s.vocab) return;
+      if (!began) {
+        keep(0);
+        if (j == 0) kind[g] = 1;
+        return;
+      }
+      float* w = s.dw + cur * s.ldw + col0;
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
-        if (column(q) >= s.d) continue;
+        if (col0 + column(q) >= s.d) continue;
         float v[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k) v[k] = acc[q * VEC + k] * s.scale;
@@ -261,67 +315,88 @@ __global__ void __launch_bounds__(256) k_embed_runs(RunSums s, const T* __restri
         }
         store_v<VEC>(w + column(q), v);
       }
+    };
+    int nr[U], no[U];  // the next step's rows and positions, loaded a step ahead
+    auto load_index = [&](int p) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = min(p + u, p1 - 1);
+        nr[u] = s.row[x];
+        no[u] = s.pos[x];
+      }
+    };
+    load_index(p0);
+    for (int p = p0; p < p1; p += U) {
+      int r[U], o[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        r[u] = nr[u];
+        o[u] = no[u];
+      }
+      if (p + U < p1) load_index(p + U);
+      float v[U][CPL];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          float x[VEC] = {};
+          if (p + u < p1 && r[u] < s.vocab && col0 + column(q) < s.d) load_v<VEC>(dout + o[u] * s.ldo + col0 + column(q), x);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) v[u][q * VEC + k] = x[k];
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p + u >= p1) break;
+        if (r[u] != cur) {
+          flush();
+          cur = r[u];
+          began = true;
+#pragma unroll
+          for (int k = 0; k < CPL; ++k) acc[k] = 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) acc[k] += v[u][k];
+      }
+    }
+    if (p1 < s.n && s.row[p1] == cur && cur < s.vocab) {
+      keep(began ? 1 : 0);
+      if (j == 0) kind[g] |= began ? 2 : 5;
     } else {
-      float* w = s.part + ((int64_t)2 * c + (began ? 1 : 0)) * s.d;
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        if (column(q) >= s.d) continue;
-        float v[VEC];
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) v[k] = acc[q * VEC + k];
-        store_v<VEC>(w + column(q), v);
-      }
-    }
-  };
-  int nr[U], no[U];  // the next step's rows and positions, loaded a step ahead
-  auto load_index = [&](int p) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int x = min(p + u, p1 - 1);
-      nr[u] = s.row[x];
-      no[u] = s.pos[x];
-    }
-  };
-  load_index(p0);
-  for (int p = p0; p < p1; p += U) {
-    int r[U], o[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      r[u] = nr[u];
-      o[u] = no[u];
-    }
-    if (p + U < p1) load_index(p + U);
-    float v[U][CPL];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        float x[VEC] = {};
-        if (p + u < p1 && r[u] < s.vocab && column(q) < s.d) load_v<VEC>(dout + o[u] * s.ldo + column(q), x);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) v[u][q * VEC + k] = x[k];
-      }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (p + u >= p1) break;
-      if (r[u] != cur) {
-        flush(false);
-        cur = r[u];
-        began = true;
-#pragma unroll
-        for (int k = 0; k < CPL; ++k) acc[k] = 0.f;
-      }
-#pragma unroll
-      for (int k = 0; k < CPL; ++k) acc[k] += v[u][k];
+      flush();
     }
   }
-  flush(p1 < s.n && s.row[p1] == cur);
+  __syncthreads();
+  for (int x = threadIdx.x; x < C && col0 + x < s.d; x += kRunThreads) {
+    float acc = 0.f;
+    bool open = false, inside = false;  // a run goes on; it began in this block
+    for (int k = 0; k < G; ++k) {
+      const int kd = kind[k];
+      if (kd & 1) {
+        acc = open ? acc + part[k][0][x] : part[k][0][x];
+        open = true;
+        if (!(kd & 4)) {
+          if (inside) {
+            float* w = s.dw + first[k] * s.ldw + col0 + x;
+            *w = s.add ? *w + s.scale * acc : s.scale * acc;
+          } else {
+            s.part[(int64_t)2 * blk * s.d + col0 + x] = acc;
+          }
+          open = inside = false;
+        }
+      }
+      if (kd & 2) {
+        acc = part[k][1][x];
+        open = inside = true;
+      }
+    }
+    if (open) s.part[((int64_t)2 * blk + (inside ? 1 : 0)) * s.d + col0 + x] = acc;
+  }
 }
 
-// Joins the runs that cross chunks: the block of the chunk in which a run
-// begins adds that chunk's slot 1 and slot 0 of the chunks up to the run's end.
-// 64 columns a block, 16 lanes a row; the groups of lanes take the partial rows
-// in turn, eight loads in flight, and are added in order.
+// Joins the runs that cross stretches: the block of the stretch in which a run
+// begins adds that stretch's slot 1 and slot 0 of the stretches up to the run's
+// end. 64 columns a block, 16 lanes a row; the groups of lanes take the partial
+// rows in turn, eight loads in flight, and are added in order.
 constexpr int kJoinThreads = 512;
 
 template <int VEC>
@@ -329,15 +404,18 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(RunSums s) {
   constexpr int G = kJoinThreads / 16, U = 8, C = 16 * VEC;
   __shared__ float red[G][C];
   const int c = blockIdx.x;
-  const int p0 = c * s.chunk, p1 = p0 + s.chunk;
-  if (p1 >= s.n) return;
-  const int v = s.row[p1];
-  if (v >= s.vocab || s.row[p1 - 1] != v) return;
-  if (s.row[p0] == v && p0 > 0 && s.row[p0 - 1] == v) return;  // begins earlier
-  int lo = c + 1, hi = s.nchunks;  // last chunk whose first row is v: lo has it, hi does not
+  const int p0 = c * s.stretch, p1 = p0 + s.stretch;  // p1 < n: one block fewer than stretches
+  const int v = s.row[p1], before = s.row[p1 - 1], first = s.row[p0], early = p0 > 0 ? s.row[p0 - 1] : -1;
+  if (v >= s.vocab || before != v || (first == v && early == v)) return;  // no run that begins here and goes on
+  // last stretch whose first row is v: lo has it, hi does not; most runs end in the next one
+  int lo = c + 1, hi = lo + 1;
+  while (hi < s.nstretch && s.row[hi * s.stretch] == v) {
+    lo = hi;
+    hi = min(s.nstretch, hi + 2 * (hi - c));
+  }
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
-    if (s.row[mid * s.chunk] == v) lo = mid;
+    if (s.row[mid * s.stretch] == v) lo = mid;
     else hi = mid;
   }
   const int m = lo - c + 1;  // partial rows
@@ -475,13 +553,33 @@ bool few_tokens(int64_t n, int64_t vocab) {
   return n <= kFewTokens && std::min(n, vocab) * n <= (1 << 20);
 }
 
-// Lanes a row: the fewest of 16, 32 and 64 that hold d values, 4 each.
-template <class F>
-int with_lanes(int d, bool vec, F&& f) {
+// Values a lane: 16 bytes of the type, 4 values of 16 bits where 8 do not fit
+// the alignment, else 1. Lanes a row: the fewest of 16, 32 and 64 that hold d
+// values (64 lanes take further columns in turn).
+int vec_of(int32_t dtype, int32_t d, int64_t lda, int64_t ldb, const void* a, const void* b, size_t bsize) {
+  const size_t es = elem_size(dtype);
+  for (int v = es == 2 ? 8 : 4; v >= 4; v -= 4)
+    if (d % v == 0 && lda % v == 0 && ldb % 4 == 0 && aligned_to(a, v * es) && aligned_to(b, std::min<size_t>(16, v * bsize)) &&
+        (bsize == 4 || ldb % v == 0))
+      return v;
+  return 1;
+}
+int lanes_of(int32_t d, int vec) { return vec == 1 || d > 32 * vec ? 64 : d > 16 * vec ? 32 : 16; }
+
+template <class T, class F>
+int with_lanes(int d, int vec, F&& f) {
   using std::integral_constant;
-  if (!vec) return f(integral_constant<int, 1>{}, integral_constant<int, 64>{});
-  if (d <= 64) return f(integral_constant<int, 4>{}, integral_constant<int, 16>{});
-  if (d <= 128) return f(integral_constant<int, 4>{}, integral_constant<int, 32>{});
+  const int lanes = lanes_of(d, vec);
+  if constexpr (sizeof(T) == 2) {
+    if (vec == 8) {
+      if (lanes == 16) return f(integral_constant<int, 8>{}, integral_constant<int, 16>{});
+      if (lanes == 32) return f(integral_constant<int, 8>{}, integral_constant<int, 32>{});
+      return f(integral_constant<int, 8>{}, integral_constant<int, 64>{});
+    }
+  }
+  if (vec == 1) return f(integral_constant<int, 1>{}, integral_constant<int, 64>{});
+  if (lanes == 16) return f(integral_constant<int, 4>{}, integral_constant<int, 16>{});
+  if (lanes == 32) return f(integral_constant<int, 4>{}, integral_constant<int, 32>{});
   return f(integral_constant<int, 4>{}, integral_constant<int, 64>{});
 }
 
@@ -499,6 +597,9 @@ int check_embed(const char* who, int64_t n, int32_t d, int64_t vocab, int32_t dt
 // flight fill the chip, of 16 to 256 positions.
 int chunk_of(int64_t n) { return (int)std::min<int64_t>(256, std::max<int64_t>(16, cdiv(n, 8192))); }
 
+// Positions of a block of k_embed_runs: a chunk for each of its groups of lanes.
+int stretch_of(int64_t n, int lanes) { return chunk_of(n) * (kRunThreads / lanes); }
+
 constexpr int64_t kMaxTokens = 1 << 30;  // positions and the ends of chunks are 32-bit
 
 struct EmbedWs {
@@ -512,7 +613,7 @@ void carve_embed(Arena& ar, int64_t n, int32_t d, int64_t vocab, EmbedWs& w) {
     w.pos[k] = ar.take<int>(n);
   }
   w.counts = ar.take<int>((int64_t)kSortBlocks * kDigits);
-  w.part = ar.take<float>(2 * cdiv(n, chunk_of(n)) * d);
+  w.part = ar.take<float>(2 * cdiv(n, stretch_of(n, 64)) * d);  // (the shortest stretches are those of 64 lanes)
 }
 
 }  // namespace
@@ -526,10 +627,10 @@ int embed_forward_entry(int64_t n, int32_t d, int64_t vocab, int32_t dtype, cons
   const size_t es = elem_size(dtype);
   if (!aligned_to(tok, 4) || !aligned_to(table, es) || !aligned_to(out, es))
     return fail(CHGNET_EINVAL, "embed_forward: an array is not aligned to its values");
-  const bool vec = d % 4 == 0 && ldt % 4 == 0 && ldo % 4 == 0 && aligned_to(table, 4 * es) && aligned_to(out, 4 * es);
+  const int vec = vec_of(dtype, d, ldt, ldo, table, out, es);
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    return with_lanes(d, vec, [&](auto V, auto L) -> int {
+    return with_lanes<T>(d, vec, [&](auto V, auto L) -> int {
       const unsigned blocks = (unsigned)std::min<int64_t>(4096, cdiv(n, 256 / L.value * kFwdRows));
       KLAUNCH(st, "k_embed_fwd",
               k_embed_fwd<T, V.value, L.value><<<blocks, 256, 0, st>>>(n, d, (int)vocab, tok, first,
@@ -563,14 +664,14 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
     return fail(CHGNET_EINVAL, "embed_backward: an array is not aligned to its values");
   const int n = (int)n64, vocab = (int)vocab64;
   const int add = accumulate != 0;
-  const bool vec = d % 4 == 0 && ldo % 4 == 0 && ldw % 4 == 0 && aligned_to(dout, 4 * es) && aligned_to(dtable, 16);
+  const int vec = vec_of(dtype, d, ldo, ldw, dout, dtable, 4);
   if (few_tokens(n, vocab)) {
     if (n == 0 && add) return CHGNET_OK;
     const bool by_row = vocab <= n;
     const unsigned blocks = (unsigned)(by_row ? vocab : n + (add ? 0 : std::min<int64_t>(4096, cdiv(vocab, kFewZeroRows))));
     return with_type(dtype, [&](auto t) {
       using T = decltype(t);
-      return with_lanes(d, vec, [&](auto V, auto L) -> int {
+      return with_lanes<T>(d, vec, [&](auto V, auto L) -> int {
         KLAUNCH(st, "k_embed_few",
                 k_embed_few<T, V.value, L.value><<<blocks, kFewThreads, 0, st>>>(
                     n, d, vocab, tok, first, static_cast<const T*>(dout), ldo, scale, dtable, ldw, add, by_row));
@@ -594,7 +695,9 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
   s.n = n;
   s.vocab = vocab;
   s.first = first;
-  s.len = cdiv(cdiv(n, kSortBlocks), kSortThreads) * kSortThreads;
+  // (kSortBlocks stretches of one round, or as many rounds as that takes)
+  const int rounds = n <= kSortBlocks * kSortThreads ? 1 : 4;
+  s.len = cdiv(cdiv(n, kSortBlocks), kSortThreads * rounds) * kSortThreads * rounds;
   const int nb = (int)cdiv(n, s.len);
   s.counts = w.counts;
   for (int p = 0; p < passes; ++p) {
@@ -605,16 +708,16 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
     s.pos = w.pos[(p + 1) & 1];
     s.row_out = w.row[p & 1];
     s.pos_out = w.pos[p & 1];
-    const int64_t zrows = p == 0 && !add ? vocab : 0;
-    const int zb = (int)std::min<int64_t>(512, cdiv(zrows * d, 4 * kSortThreads));
-    KLAUNCH(st, "k_embed_count", k_embed_count<<<nb + zb, kSortThreads, 0, st>>>(s, nb, zrows, d, dtable, ldw));
-    KLAUNCH(st, "k_embed_place", k_embed_place<<<nb, kSortThreads, 0, st>>>(s));
+    KLAUNCH(st, "k_embed_count", k_embed_count<<<nb, kSortThreads, 0, st>>>(s));
+    if (rounds == 1) KLAUNCH(st, "k_embed_place", k_embed_place<1><<<nb, kSortThreads, 0, st>>>(s));
+    else KLAUNCH(st, "k_embed_place", k_embed_place<4><<<nb, kSortThreads, 0, st>>>(s));
   }
   RunSums r{};
   r.n = n;
   r.vocab = vocab;
   r.chunk = chunk_of(n);
-  r.nchunks = (int)cdiv(n, r.chunk);
+  r.stretch = stretch_of(n, lanes_of(d, vec));
+  r.nstretch = (int)cdiv(n, r.stretch);
   r.d = d;
   r.row = w.row[(passes + 1) & 1];
   r.pos = w.pos[(passes + 1) & 1];
@@ -624,21 +727,23 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
   r.dw = dtable;
   r.add = add;
   r.part = w.part;
+  r.nzero = add ? 0 : (int)cdiv(vocab, kRunThreads);
   CHG_TRY(with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    return with_lanes(d, vec, [&](auto V, auto L) -> int {
+    return with_lanes<T>(d, vec, [&](auto V, auto L) -> int {
       constexpr int NQ = V.value == 1 ? 4 : 1;
-      const dim3 grid((unsigned)cdiv(r.nchunks, 256 / L.value), (unsigned)cdiv(d, L.value * V.value * NQ));
-      KLAUNCH(st, "k_embed_runs", k_embed_runs<T, V.value, L.value, NQ><<<grid, 256, 0, st>>>(r, static_cast<const T*>(dout)));
+      const dim3 grid((unsigned)(r.nzero + r.nstretch), (unsigned)cdiv(d, L.value * V.value * NQ));
+      KLAUNCH(st, "k_embed_runs",
+              k_embed_runs<T, V.value, L.value, NQ><<<grid, kRunThreads, 0, st>>>(r, static_cast<const T*>(dout)));
       return CHGNET_OK;
     });
   }));
-  if (r.nchunks > 1) {
+  if (r.nstretch > 1) {
     // the partial rows are dense: 16-byte loads where their width allows
     if (d % 4 == 0)
-      KLAUNCH(st, "k_embed_join", k_embed_join<4><<<dim3(r.nchunks - 1, (unsigned)cdiv(d, 64)), kJoinThreads, 0, st>>>(r));
+      KLAUNCH(st, "k_embed_join", k_embed_join<4><<<dim3(r.nstretch - 1, (unsigned)cdiv(d, 64)), kJoinThreads, 0, st>>>(r));
     else
-      KLAUNCH(st, "k_embed_join", k_embed_join<1><<<dim3(r.nchunks - 1, (unsigned)cdiv(d, 16)), kJoinThreads, 0, st>>>(r));
+      KLAUNCH(st, "k_embed_join", k_embed_join<1><<<dim3(r.nstretch - 1, (unsigned)cdiv(d, 16)), kJoinThreads, 0, st>>>(r));
   }
   return CHGNET_OK;
 }
