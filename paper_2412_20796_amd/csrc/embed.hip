@@ -39,12 +39,21 @@ __global__ void __launch_bounds__(256) k_embed_fwd(int64_t n, int d, int vocab, 
                                                    const T* __restrict__ table, int64_t ldt, float scale,
                                                    T* __restrict__ out, int64_t ldo) {
   constexpr int G = 256 / LPR;
-  const int j = threadIdx.x % LPR, g = threadIdx.x / LPR;
+  const int j = threadIdx.x % LPR;
+  const int g = LPR == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / LPR) : threadIdx.x / LPR;
   const int64_t stride = (int64_t)gridDim.x * G * kFwdRows;
-  for (int64_t i0 = ((int64_t)blockIdx.x * G + g) * kFwdRows; i0 < n; i0 += stride) {
+  int64_t i0 = ((int64_t)blockIdx.x * G + g) * kFwdRows;
+  int next[kFwdRows];  // the next rows' tokens, loaded a turn ahead
+  auto load_tokens = [&](int64_t i) {
+#pragma unroll
+    for (int u = 0; u < kFwdRows; ++u) next[u] = i + u < n ? tok[i + u] : -1;
+  };
+  load_tokens(i0);
+  for (; i0 < n; i0 += stride) {
     int r[kFwdRows];
 #pragma unroll
-    for (int u = 0; u < kFwdRows; ++u) r[u] = i0 + u < n ? table_row(tok[i0 + u], first, vocab) : vocab;
+    for (int u = 0; u < kFwdRows; ++u) r[u] = table_row(next[u], first, vocab);
+    load_tokens(i0 + stride);
     for (int c = j * VEC; c < d; c += LPR * VEC) {
       float v[kFwdRows][VEC];
 #pragma unroll
@@ -265,11 +274,15 @@ __device__ __forceinline__ void zero_rows(const RunSums& s, int64_t v0, int col0
 }
 
 template <class T, int VEC, int LPR, int NQ>
-__global__ void __launch_bounds__(kRunThreads) k_embed_runs(RunSums s, const T* __restrict__ dout) {
+__global__ void __launch_bounds__(kRunThreads) k_embed_runs(RunSums s, const int* __restrict__ rows,
+                                                            const int* __restrict__ poss, const T* __restrict__ dout) {
   constexpr int G = kRunThreads / LPR, U = 8, CPL = VEC * NQ, C = LPR * CPL;
   __shared__ float part[G][2][C];
   __shared__ int first[G], kind[G];  // kind bits: 1 slot 0 used, 2 slot 1 used, 4 slot 0's run goes on
-  const int j = threadIdx.x % LPR, g = threadIdx.x / LPR;
+  // (a wavefront on one row: its chunk is uniform, so indices, comparisons and
+  // addresses are scalar)
+  const int j = threadIdx.x % LPR;
+  const int g = LPR == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / LPR) : threadIdx.x / LPR;
   const int col0 = blockIdx.y * C;
   const int blk = (int)blockIdx.x - s.nzero;
   if (blk < 0) {
@@ -284,9 +297,9 @@ __global__ void __launch_bounds__(kRunThreads) k_embed_runs(RunSums s, const T* 
     float acc[CPL];
 #pragma unroll
     for (int k = 0; k < CPL; ++k) acc[k] = 0.f;
-    int cur = s.row[p0];
+    int cur = rows[p0];
     if (j == 0) first[g] = cur;
-    bool began = p0 == 0 || s.row[p0 - 1] != cur;  // the run starts in this chunk
+    bool began = p0 == 0 || rows[p0 - 1] != cur;  // the run starts in this chunk
     auto keep = [&](int slot) {
 #pragma unroll
       for (int q = 0; q < NQ; ++q)
@@ -321,8 +334,8 @@ __global__ void __launch_bounds__(kRunThreads) k_embed_runs(RunSums s, const T* 
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int x = min(p + u, p1 - 1);
-        nr[u] = s.row[x];
-        no[u] = s.pos[x];
+        nr[u] = rows[x];
+        no[u] = poss[x];
       }
     };
     load_index(p0);
@@ -358,7 +371,7 @@ __global__ void __launch_bounds__(kRunThreads) k_embed_runs(RunSums s, const T* 
         for (int k = 0; k < CPL; ++k) acc[k] += v[u][k];
       }
     }
-    if (p1 < s.n && s.row[p1] == cur && cur < s.vocab) {
+    if (p1 < s.n && rows[p1] == cur && cur < s.vocab) {
       keep(began ? 1 : 0);
       if (j == 0) kind[g] |= began ? 2 : 5;
     } else {
@@ -734,7 +747,8 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
       constexpr int NQ = V.value == 1 ? 4 : 1;
       const dim3 grid((unsigned)(r.nzero + r.nstretch), (unsigned)cdiv(d, L.value * V.value * NQ));
       KLAUNCH(st, "k_embed_runs",
-              k_embed_runs<T, V.value, L.value, NQ><<<grid, kRunThreads, 0, st>>>(r, static_cast<const T*>(dout)));
+              k_embed_runs<T, V.value, L.value, NQ><<<grid, kRunThreads, 0, st>>>(r, r.row, r.pos,
+                                                                           static_cast<const T*>(dout)));
       return CHGNET_OK;
     });
   }));
