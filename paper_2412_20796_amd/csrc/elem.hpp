@@ -48,6 +48,32 @@ __device__ __forceinline__ void store_v(T* p, const float (&v)[V]) {
   }
 }
 
+// The same past the caches (nontemporal), for values that are read once and
+// results that others than this kernel read.
+template <int V, class T>
+__device__ __forceinline__ void load_nt(const T* p, float (&v)[V]) {
+  static_assert(V * sizeof(T) <= 16, "one access");
+  typedef T vec __attribute__((ext_vector_type(V)));
+  const vec t = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p));
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = (float)t[k];
+}
+template <int V, class T>
+__device__ __forceinline__ void store_nt(T* p, const float (&v)[V]) {
+  static_assert(V * sizeof(T) <= 16, "one access");
+  typedef T vec __attribute__((ext_vector_type(V)));
+  vec t;
+#pragma unroll
+  for (int k = 0; k < V; ++k) t[k] = (T)v[k];
+  __builtin_nontemporal_store(t, reinterpret_cast<vec*>(p));
+}
+
+// Input bytes of a call from which it loads them past the caches: half of the
+// last cache's 256 MB. (The gate: 154 MB of z after the product that wrote it: 121 -> 115
+// us with what comes before and after; 87 MB: the same; 44 MB that no kernel
+// has touched lately: 33 -> 40.)
+constexpr int64_t kFarBytes = 128 << 20;
+
 inline int elem_size(int32_t dtype) { return dtype == CHGNET_F32 ? 4 : dtype == CHGNET_BF16 || dtype == CHGNET_F16 ? 2 : 0; }
 // calls f with a value of the (valid) type
 template <class F>

@@ -27,19 +27,29 @@ namespace chg {
 namespace {
 
 // Row of d values in LPR lanes: lane j holds the NQ groups of VEC values at
-// columns (q LPR + j) VEC. FULL: d is exactly the LPR VEC NQ columns.
-template <int VEC, int LPR, int NQ, bool FULL>
+// columns (q LPR + j) VEC. MIN: d is greater, so that only the groups past it
+// are looked at for their end; FULL: d is exactly the LPR VEC NQ columns.
+// Results are stored past the caches (nontemporal), and with FAR the inputs are
+// loaded so: both are of use to others than this kernel only. Measured in fp32
+// on both passes of 85,274 rows of 64 and of 397,934 rows of 128: 38.7 and 287 us
+// with plain accesses, 32.7 and 274 with such stores, 40.2 and 240 with such
+// loads too, which pay where the inputs do not fit the last cache (kFarBytes);
+// a kernel that reads the results next takes no longer at any size.
+template <int VEC, int LPR, int NQ, int MIN, bool FULL, bool FAR>
 struct Cols {
   static constexpr int CPL = VEC * NQ, RPW = 64 / LPR;
   int j, d;
   __device__ __forceinline__ int col(int q) const { return (q * LPR + j) * VEC; }
-  __device__ __forceinline__ bool has(int q) const { return FULL || col(q) < d; }
+  __device__ __forceinline__ bool has(int q) const { return FULL || (q + 1) * LPR * VEC <= MIN || col(q) < d; }
   template <class T>
   __device__ __forceinline__ void load(const T* p, float (&v)[CPL]) const {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       float t[VEC] = {};
-      if (has(q)) load_v<VEC>(p + col(q), t);
+      if (has(q)) {
+        if constexpr (FAR) load_nt<VEC>(p + col(q), t);
+        else load_v<VEC>(p + col(q), t);
+      }
 #pragma unroll
       for (int k = 0; k < VEC; ++k) v[q * VEC + k] = t[k];
     }
@@ -51,7 +61,7 @@ struct Cols {
       float t[VEC];
 #pragma unroll
       for (int k = 0; k < VEC; ++k) t[k] = v[q * VEC + k];
-      if (has(q)) store_v<VEC>(p + col(q), t);
+      if (has(q)) store_nt<VEC>(p + col(q), t);
     }
   }
   // the LayerNorm parameters, which may sit at any float of the parameter vector
@@ -81,11 +91,11 @@ struct Cols {
   }
 };
 
-template <class T, int VEC, int LPR, int NQ, bool FULL>
+template <class T, int VEC, int LPR, int NQ, int MIN, bool FULL, bool FAR>
 __global__ void __launch_bounds__(256) k_gate_act_fwd(int64_t rows, int d, const T* __restrict__ z, int64_t ldz,
                                                       const float* __restrict__ ln, T* __restrict__ phi, int64_t ldphi,
                                                       uint8_t* __restrict__ codes, float2* __restrict__ step) {
-  using C = Cols<VEC, LPR, NQ, FULL>;
+  using C = Cols<VEC, LPR, NQ, MIN, FULL, FAR>;
   constexpr int CPL = C::CPL;
   const int lane = threadIdx.x & 63;
   const C cols{lane % LPR, FULL ? VEC * LPR * NQ : d};
@@ -161,13 +171,13 @@ constexpr int kBwdThreads = 512, kBwdBlocks = 512;
 
 // part: [gridDim.x][4 d] partial sums of the LayerNorm gradients, or with one
 // block their destination (`add`: to what it holds).
-template <class T, int VEC, int LPR, int NQ, bool FULL>
+template <class T, int VEC, int LPR, int NQ, int MIN, bool FULL, bool FAR>
 __global__ void __launch_bounds__(kBwdThreads) k_gate_act_bwd(int64_t rows, int d, const uint8_t* __restrict__ codes,
                                                               const float2* __restrict__ step,
                                                               const float* __restrict__ ln, const T* __restrict__ dphi,
                                                               int64_t lddphi, T* __restrict__ dz, int64_t lddz,
                                                               float* __restrict__ part, int add) {
-  using C = Cols<VEC, LPR, NQ, FULL>;
+  using C = Cols<VEC, LPR, NQ, MIN, FULL, FAR>;
   constexpr int CPL = C::CPL, W = kBwdThreads / 64;
   __shared__ float red[W][VEC * LPR * NQ];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -312,32 +322,39 @@ __global__ void __launch_bounds__(256) k_gate_ln_zero(int n, float* __restrict__
   if (i < n) p[i] = 0.f;
 }
 
-// Calls f with the layout of rows of width d. Four values a lane where
-// alignment allows 16-byte (8-byte) accesses, with as few lanes a row as 16
-// values a lane of each half allow; else one value a lane.
+// Calls f with the layout of rows of width d: four values a lane where alignment
+// allows 16-byte (8-byte) accesses, with as few lanes a row as 16 values a lane
+// of each half allow; else one value a lane.
 template <class F>
-int with_layout(int d, bool vec, F&& f) {
-#define CHG_ROW(VEC, LPR, NQ)                                                        \
-  if (d <= VEC * LPR * NQ) {                                                         \
-    if constexpr (VEC == 4) {                                                        \
-      if (d == VEC * LPR * NQ) return f(std::integral_constant<int, VEC>{}, std::integral_constant<int, LPR>{}, \
-                                        std::integral_constant<int, NQ>{}, std::true_type{});                   \
-    }                                                                                \
-    return f(std::integral_constant<int, VEC>{}, std::integral_constant<int, LPR>{}, \
-             std::integral_constant<int, NQ>{}, std::false_type{});                  \
+int with_layout(int d, bool vec, bool far, F&& f) {
+  using std::integral_constant;
+#define CHG_ROW(VEC, LPR, NQ, MIN)                                                                 \
+  if (d <= VEC * LPR * NQ) {                                                                      \
+    const integral_constant<int, VEC> v;                                                          \
+    const integral_constant<int, LPR> l;                                                          \
+    const integral_constant<int, NQ> n;                                                           \
+    const integral_constant<int, MIN> m;                                                          \
+    if constexpr (VEC == 4) {                                                                     \
+      if (d == VEC * LPR * NQ && far) return f(v, l, n, m, std::true_type{}, std::true_type{});   \
+      if (d == VEC * LPR * NQ) return f(v, l, n, m, std::true_type{}, std::false_type{});         \
+    }                                                                                             \
+    return f(v, l, n, m, std::false_type{}, std::false_type{});                                   \
   }
   if (vec) {
-    CHG_ROW(4, 16, 1)
-    CHG_ROW(4, 16, 2)
-    CHG_ROW(4, 32, 2)
-    CHG_ROW(4, 64, 2)
-    CHG_ROW(4, 64, 4)
+    CHG_ROW(4, 16, 1, 0)
+    CHG_ROW(4, 16, 2, 64)
+    CHG_ROW(4, 32, 2, 128)
+    CHG_ROW(4, 64, 2, 256)
+    CHG_ROW(4, 64, 4, 512)
   } else {
-    CHG_ROW(1, 16, 1)
-    CHG_ROW(1, 16, 4)
-    CHG_ROW(1, 64, 4)
-    CHG_ROW(1, 64, 8)
-    CHG_ROW(1, 64, 16)
+    CHG_ROW(1, 16, 1, 0)
+    CHG_ROW(1, 16, 4, 16)
+    CHG_ROW(1, 32, 4, 64)
+    CHG_ROW(1, 32, 8, 128)
+    CHG_ROW(1, 32, 12, 256)
+    CHG_ROW(1, 64, 8, 384)
+    CHG_ROW(1, 64, 12, 512)
+    CHG_ROW(1, 64, 16, 768)
   }
 #undef CHG_ROW
   return fail(CHGNET_EINVAL, "gate: d must be in 1..1024");
@@ -372,12 +389,12 @@ int gate_forward_entry(int64_t rows, int32_t d, int32_t dtype, const void* z, in
                    aligned_to(codes, 4);
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    return with_layout(d, vec, [&](auto V, auto L, auto N, auto full) -> int {
+    return with_layout(d, vec, rows * 2 * d * (int64_t)es >= kFarBytes, [&](auto V, auto L, auto N, auto M, auto full, auto far) -> int {
       constexpr int rpw = 64 / L.value;
       // 8 blocks of 256 threads a compute unit walk the rows
       const unsigned blocks = (unsigned)std::min<int64_t>(2048, cdiv(rows, 4 * rpw));
       KLAUNCH(st, "k_gate_act_fwd",
-              k_gate_act_fwd<T, V.value, L.value, N.value, full.value><<<blocks, 256, 0, st>>>(
+              k_gate_act_fwd<T, V.value, L.value, N.value, M.value, full.value, far.value><<<blocks, 256, 0, st>>>(
                   rows, d, static_cast<const T*>(z), ldz, ln, static_cast<T*>(phi), ldphi, codes,
                   reinterpret_cast<float2*>(step)));
       return CHGNET_OK;
@@ -419,11 +436,11 @@ int gate_backward_entry(int64_t rows, int32_t d, int32_t dtype, const uint8_t* c
   int blocks = 1;
   CHG_TRY(with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    return with_layout(d, vec, [&](auto V, auto L, auto N, auto full) -> int {
+    return with_layout(d, vec, rows * d * (int64_t)(es + 2) >= kFarBytes, [&](auto V, auto L, auto N, auto M, auto full, auto far) -> int {
       constexpr int rpw = 64 / L.value;
       blocks = bwd_blocks(rows, rpw);
       KLAUNCH(st, "k_gate_act_bwd",
-              k_gate_act_bwd<T, V.value, L.value, N.value, full.value><<<blocks, kBwdThreads, 0, st>>>(
+              k_gate_act_bwd<T, V.value, L.value, N.value, M.value, full.value, far.value><<<blocks, kBwdThreads, 0, st>>>(
                   rows, d, codes, reinterpret_cast<const float2*>(step), ln, static_cast<const T*>(dphi), lddphi,
                   static_cast<T*>(dz), lddz, blocks == 1 ? dln : part, blocks == 1 && accumulate));
       return CHGNET_OK;
