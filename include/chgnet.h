@@ -36,7 +36,8 @@
  * 31 radial and 31 angular basis functions, envelope exponent p = 8, atom
  * graph cutoff 6 A, bond graph cutoff 3 A. Supported: d in {64, 128},
  * 1 <= T <= 16, 1 <= n_rbf <= 64, n_fourier odd in [1, 63], p in [2, 16],
- * 0 < r_bond <= r_atom <= 20, magmom, sequential and conservative in {0, 1}.
+ * 0 < r_bond <= r_atom <= 20, magmom, sequential and conservative in {0, 1},
+ * act_bits in {0, 8}.
  */
 #ifndef CHGNET_H
 #define CHGNET_H
@@ -80,6 +81,15 @@ typedef struct {
                          numbers), with either block. The workspace then
                          holds the dual-number buffers
                          as well (chgnet_workspace_size includes them).     */
+  int32_t act_bits;   /* 0: the gates' pre-activations, most of what a
+                         forward pass keeps for the backward pass, are kept
+                         in fp32; 8: in 8 bits, each half row in steps of
+                         (max - min) / 255 (the checkpoint of chgnet_ops.h),
+                         2 d + 8 bytes a gate row in place of 8 d. Energies,
+                         forces, stresses and the loss are the same bits; the
+                         gates' derivatives are those at the kept values.
+                         The same value for every call on a workspace. Not
+                         with the conservative readout.                      */
 } chgnet_hparams;
 
 /* Loss of chgnet_step (Sec. IV, "Parameters Setting"), host memory. Each term

@@ -92,6 +92,9 @@ int validate_hparams(const chgnet_hparams* hp) {
   if ((hp->magmom != 0 && hp->magmom != 1) || (hp->sequential != 0 && hp->sequential != 1) ||
       (hp->conservative != 0 && hp->conservative != 1))
     return fail(CHGNET_EINVAL, "magmom, sequential and conservative must be 0 or 1");
+  if (hp->act_bits != 0 && hp->act_bits != 8) return fail(CHGNET_EINVAL, "act_bits must be 0 or 8");
+  if (hp->act_bits == 8 && hp->conservative)
+    return fail(CHGNET_EINVAL, "act_bits = 8 needs the direct heads: the conservative readout differentiates the kept pre-activations again");
   return CHGNET_OK;
 }
 

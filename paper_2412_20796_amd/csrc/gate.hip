@@ -184,11 +184,24 @@ __global__ void __launch_bounds__(kBwdThreads) k_gate_act_bwd(int64_t rows, int 
   const C cols{lane % LPR, FULL ? VEC * LPR * NQ : d};
   d = cols.d;
   const float inv_d = 1.0f / (float)d;
+  // LayerNorm parameters in registers; at 16 columns a lane with an end to look
+  // for, where there is no
+  // room for them (70 registers spilled), in LDS
+  constexpr bool kLnInLds = CPL == 16 && !FULL;
+  __shared__ float lnS[kLnInLds ? 4 * VEC * LPR * NQ : 1];
   float gc[CPL], bc[CPL], gg[CPL], bg[CPL];
-  cols.load_any(ln, gc);
-  cols.load_any(ln + d, bc);
-  cols.load_any(ln + 2 * d, gg);
-  cols.load_any(ln + 3 * d, bg);
+  if constexpr (kLnInLds) {
+    for (int t = threadIdx.x; t < 4 * VEC * LPR * NQ; t += kBwdThreads) {
+      const int a = t / (VEC * LPR * NQ), c = t % (VEC * LPR * NQ);
+      lnS[t] = c < d ? ln[a * d + c] : 0.f;
+    }
+    __syncthreads();
+  } else {
+    cols.load_any(ln, gc);
+    cols.load_any(ln + d, bc);
+    cols.load_any(ln + 2 * d, gg);
+    cols.load_any(ln + 3 * d, bg);
+  }
   float acc[4][CPL];
 #pragma unroll
   for (int a = 0; a < 4; ++a)
@@ -241,6 +254,20 @@ __global__ void __launch_bounds__(kBwdThreads) k_gate_act_bwd(int64_t rows, int 
 #pragma unroll
     for (int k = 0; k < CPL; ++k) up[k] = in.up[k];
     if (row + stride < rows) load(row + stride, in);
+    if constexpr (kLnInLds) {
+      int at = 0;
+      asm volatile("" : "+v"(at));  // read for each row: kept from moving out of the loop into registers
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+          const float* p = lnS + at + cols.col(q) + k;
+          gc[q * VEC + k] = p[0];
+          bc[q * VEC + k] = p[VEC * LPR * NQ];
+          gg[q * VEC + k] = p[2 * VEC * LPR * NQ];
+          bg[q * VEC + k] = p[3 * VEC * LPR * NQ];
+        }
+    }
     const float rc = cols.center(xc, uc), rg = cols.center(xg, ug);
     const float fc = uc * rc, fg = ug * rg;
     float s1c = 0.f, s2c = 0.f, s1g = 0.f, s2g = 0.f;

@@ -365,6 +365,94 @@ __device__ __forceinline__ void ln_stats(float (&zc)[CPL], float (&zg)[CPL], flo
   }
 }
 
+// The same from the codes of a row's 8-bit checkpoint (rowops.hpp), in zc and zg:
+// the least value that they count from drops out with the mean, and their sums
+// are exact.
+template <int D, int CPL>
+__device__ __forceinline__ void ln_stats_codes(float (&zc)[CPL], float (&zg)[CPL], float2 step, float& rc, float& rg) {
+  constexpr int LPR = Lanes<D, CPL>::LPR;
+  float sc = 0.f, sg = 0.f;
+#pragma unroll
+  for (int k = 0; k < CPL; ++k) {
+    sc += zc[k];
+    sg += zg[k];
+  }
+  const float mc = rowsum<LPR>(sc) * (1.0f / D), mg = rowsum<LPR>(sg) * (1.0f / D);
+  float vc = 0.f, vg = 0.f;
+#pragma unroll
+  for (int k = 0; k < CPL; ++k) {
+    zc[k] -= mc;
+    zg[k] -= mg;
+    vc += zc[k] * zc[k];
+    vg += zg[k] * zg[k];
+  }
+  rc = __builtin_amdgcn_rsqf(rowsum<LPR>(vc) * (1.0f / D) * (step.x * step.x) + kLnEps);
+  rg = __builtin_amdgcn_rsqf(rowsum<LPR>(vg) * (1.0f / D) * (step.y * step.y) + kLnEps);
+  const float fc = rc * step.x, fg = rg * step.y;
+#pragma unroll
+  for (int k = 0; k < CPL; ++k) {
+    zc[k] *= fc;
+    zg[k] *= fg;
+  }
+}
+
+// 8-bit checkpoint of a gate's pre-activations in the workspace (act_bits = 8):
+// per row the 16-byte pieces of its lanes (the codes of a lane's 8 core and 8
+// gate columns, so that a lane writes and reads its part of a row in one
+// access), and the steps of both halves.
+struct ZCodes {
+  uint4* q;      // piece j of row r: q[r * ldq + j]
+  float2* step;  // step[r * lds]
+  int ldq, lds;
+};
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+
+template <int D, int CPL>
+__device__ __forceinline__ void store_codes(const ZCodes& k, int row, int j, const float (&zc)[CPL],
+                                            const float (&zg)[CPL]) {
+  static_assert(CPL == 8, "16 codes a lane");
+  constexpr int LPR = Lanes<D, CPL>::LPR;
+  v4u w;
+  float2 st;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float(&x)[CPL] = h ? zg : zc;
+    float lo = x[0], hi = x[0], inv;
+#pragma unroll
+    for (int c = 1; c < CPL; ++c) {
+      lo = __builtin_elementwise_minimum(lo, x[c]);
+      hi = __builtin_elementwise_maximum(hi, x[c]);
+    }
+    lo = rowmin<LPR>(lo);
+    hi = rowmax<LPR>(hi);
+    code_step(lo, hi, h ? st.y : st.x, inv);
+    unsigned u[CPL];
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) u[c] = code_of(x[c], lo, inv);
+    w[2 * h] = pack_codes(u[0], u[1], u[2], u[3]);
+    w[2 * h + 1] = pack_codes(u[4], u[5], u[6], u[7]);
+  }
+  __builtin_nontemporal_store(w, reinterpret_cast<v4u*>(k.q + (int64_t)row * k.ldq + j));
+  if (j == 0) k.step[(int64_t)row * k.lds] = st;
+}
+template <int CPL>
+__device__ __forceinline__ float2 load_codes(const ZCodes& k, int row, int j, float (&zc)[CPL], float (&zg)[CPL]) {
+  const v4u w = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(k.q + (int64_t)row * k.ldq + j));
+  const float2 st = k.step[(int64_t)row * k.lds];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    zc[4 * q] = code_value<0>(w[q]);
+    zc[4 * q + 1] = code_value<1>(w[q]);
+    zc[4 * q + 2] = code_value<2>(w[q]);
+    zc[4 * q + 3] = code_value<3>(w[q]);
+    zg[4 * q] = code_value<0>(w[2 + q]);
+    zg[4 * q + 1] = code_value<1>(w[2 + q]);
+    zg[4 * q + 2] = code_value<2>(w[2 + q]);
+    zg[4 * q + 3] = code_value<3>(w[2 + q]);
+  }
+  return st;
+}
+
 struct LnPtrs {
   const float *gc, *bc, *gg, *bg;
 };
@@ -432,6 +520,7 @@ struct GateMmJob {
   float* out;
   float* zsave;  // optional [rows, ldzs]: the whole pre-activation z, kept for the backward pass
   int ldzs;
+  ZCodes zcodes;  // the same in 8 bits (kernels with Q8; q == nullptr: not kept)
   float* xcopy;  // optional [rows, d]: a copy of x (the residual part of e^{t+1})
 };
 struct GateMmJobs {
@@ -579,7 +668,7 @@ struct GateLnRegs {
 // on 4,096 atoms (d = 64) 157 MB of messages were written and read back a
 // layer, and the segmented sum goes from 93 to 68 us a launch; on wide128 from
 // 112 to 91 us on average, with the gate 3 % faster.
-template <int D, int MODE>
+template <int D, int MODE, bool Q8>
 __device__ __forceinline__ void gate_mm_row(const GateMmJob& J, int row, int lr, float* Zs, const GateRowIn& in,
                                             const GateLnRegs& ln) {
   constexpr int CPL = kMmCpl;
@@ -617,7 +706,9 @@ __device__ __forceinline__ void gate_mm_row(const GateMmJob& J, int row, int lr,
       zg[k] += in.ag[q][k];
     }
   }
-  if (J.zsave && row < J.rows) {
+  if (Q8) {
+    if (J.zcodes.q && row < J.rows) store_codes<D, CPL>(J.zcodes, row, j, zc, zg);
+  } else if (J.zsave && row < J.rows) {
     store_cols_nt<D, CPL>(J.zsave + (int64_t)row * J.ldzs, j, zc);
     store_cols_nt<D, CPL>(J.zsave + (int64_t)row * J.ldzs + D, j, zg);
   }
@@ -755,7 +846,8 @@ __device__ __forceinline__ void mm_tile(const float* X, float* Z, const float (&
 }
 
 // One block per compute unit, walking its share of the jobs' tiles (XcdTiles).
-template <int D, int R>
+// Q8: what is kept for the backward pass is the 8-bit checkpoint.
+template <int D, int R, bool Q8>
 __global__ void __launch_bounds__((MmCfg<D, R>::Threads), 1) k_gate_fwd_mm(GateMmJobs J) {
   using C = MmCfg<D, R>;
   __shared__ __attribute__((aligned(16))) float Xs[2][C::Rows * C::Xld];
@@ -849,9 +941,9 @@ __global__ void __launch_bounds__((MmCfg<D, R>::Threads), 1) k_gate_fwd_mm(GateM
         }
         const int row = tile * C::Rows + lr;
         float* Z = Zs[(i - 1) & 1];
-        if (jb.mode == FWD_ATOM) gate_mm_row<D, FWD_ATOM>(jb, row, lr, Z, in, lnr);
-        else if (jb.mode == FWD_BOND) gate_mm_row<D, FWD_BOND>(jb, row, lr, Z, in, lnr);
-        else gate_mm_row<D, FWD_ANGLE>(jb, row, lr, Z, in, lnr);
+        if (jb.mode == FWD_ATOM) gate_mm_row<D, FWD_ATOM, Q8>(jb, row, lr, Z, in, lnr);
+        else if (jb.mode == FWD_BOND) gate_mm_row<D, FWD_BOND, Q8>(jb, row, lr, Z, in, lnr);
+        else gate_mm_row<D, FWD_ANGLE, Q8>(jb, row, lr, Z, in, lnr);
         // (issued before the rows are computed, or as soon as this tile's are
         // added to z, the gathers made the launch 12-14 % slower at d = 64
         // and spill at d = 128)
@@ -877,6 +969,7 @@ constexpr int kGateRows = 128;
 struct GateBwdJob {
   int mode, rows, ldz, lddz, block0;
   const float* z;  // the saved pre-activations [rows, ldz]
+  ZCodes zcodes;   // the same in 8 bits (kernels with Q8)
   LnPtrs ln;
   const float *up, *eb;
   const int *up_idx, *b2_idx;
@@ -897,7 +990,7 @@ struct GateBwdLds {
   static constexpr int FLOATS = 4 * 4 * RPW * LD;
 };
 
-template <int D, int MODE>
+template <int D, int MODE, bool Q8>
 __device__ __forceinline__ void gate_bwd_rows(int blk, const GateBwdJob& J, float* red) {
   const int rows = J.rows, ldz = J.ldz, lddz = J.lddz;
   const float* __restrict__ z = J.z;
@@ -922,8 +1015,13 @@ __device__ __forceinline__ void gate_bwd_rows(int blk, const GateBwdJob& J, floa
     const int row = blk * kGateRows + (it * 4 + wave) * RPW + slot;
     if (row >= rows) continue;
     float zc[CPL], zg[CPL], rc, rg;
-    load_z<D, CPL>(z, ldz, row, j, zc, zg);
-    ln_stats<D, CPL>(zc, zg, rc, rg);
+    if (Q8) {
+      const float2 step = load_codes<CPL>(J.zcodes, row, j, zc, zg);
+      ln_stats_codes<D, CPL>(zc, zg, step, rc, rg);
+    } else {
+      load_z<D, CPL>(z, ldz, row, j, zc, zg);
+      ln_stats<D, CPL>(zc, zg, rc, rg);
+    }
     float u[CPL], w[CPL], dphi[CPL];
     if (MODE == BWD_ANGLE) {
       load_cols<D, CPL>(up + (int64_t)row * D, j, dphi);
@@ -1017,16 +1115,16 @@ __device__ __forceinline__ void gate_bwd_rows(int blk, const GateBwdJob& J, floa
   }
 }
 
-template <int D>
+template <int D, bool Q8>
 __global__ void __launch_bounds__(256) k_gate_bwd(GateBwdJobs J) {
   int k = 0;
   while (k + 1 < J.n && (int)blockIdx.x >= J.j[k + 1].block0) ++k;
   const GateBwdJob& jb = J.j[k];
   const int blk = blockIdx.x - jb.block0;
   __shared__ __align__(16) float red[GateBwdLds<D>::FLOATS];
-  if (jb.mode == BWD_ATOM) gate_bwd_rows<D, BWD_ATOM>(blk, jb, red);
-  else if (jb.mode == BWD_BOND) gate_bwd_rows<D, BWD_BOND>(blk, jb, red);
-  else gate_bwd_rows<D, BWD_ANGLE>(blk, jb, red);
+  if (jb.mode == BWD_ATOM) gate_bwd_rows<D, BWD_ATOM, Q8>(blk, jb, red);
+  else if (jb.mode == BWD_BOND) gate_bwd_rows<D, BWD_BOND, Q8>(blk, jb, red);
+  else gate_bwd_rows<D, BWD_ANGLE, Q8>(blk, jb, red);
 }
 
 // ---------------------------------------------------------------------------
@@ -1096,14 +1194,19 @@ __device__ __forceinline__ void bwd_mm_ln_add(const float (&p)[32], float* wsum)
   }
 }
 
-template <int D, int MODE>
+template <int D, int MODE, bool Q8>
 __device__ __forceinline__ void gate_bwd_mm_row(const GateBwdJob& J, int row, const BwdMmIdx& x, int j,
                                                 const float* lnS, float (&lp)[4 * kMmCpl], float* zrow) {
   constexpr int CPL = kMmCpl;
   constexpr int LPR = Lanes<D, CPL>::LPR;
   float zc[CPL], zg[CPL], rc, rg;
-  load_cols_nt<D, CPL>(J.z + (int64_t)row * J.ldz, j, zc);
-  load_cols_nt<D, CPL>(J.z + (int64_t)row * J.ldz + D, j, zg);
+  float2 step;
+  if (Q8) {
+    step = load_codes<CPL>(J.zcodes, row, j, zc, zg);
+  } else {
+    load_cols_nt<D, CPL>(J.z + (int64_t)row * J.ldz, j, zc);
+    load_cols_nt<D, CPL>(J.z + (int64_t)row * J.ldz + D, j, zg);
+  }
   // the running sum d e^a of this edge, loaded with the row's other inputs
   // (after the dz stores the load could not be moved ahead of them)
   float de[CPL];
@@ -1129,7 +1232,8 @@ __device__ __forceinline__ void gate_bwd_mm_row(const GateBwdJob& J, int row, co
       }
     }
   }
-  ln_stats<D, CPL>(zc, zg, rc, rg);
+  if (Q8) ln_stats_codes<D, CPL>(zc, zg, step, rc, rg);
+  else ln_stats<D, CPL>(zc, zg, rc, rg);
   float gc[CPL], bc[CPL], gg[CPL], bg[CPL];
   load_cols<D, CPL>(lnS, j, gc);
   load_cols<D, CPL>(lnS + D, j, bc);
@@ -1199,6 +1303,7 @@ __device__ __forceinline__ void gate_bwd_mm_row(const GateBwdJob& J, int row, co
 // One block per compute unit, walking tiles blockIdx.x, blockIdx.x +
 // gridDim.x, ... of the concatenated jobs; consumers fill the dz tile of
 // tile i while producers multiply tile i - 1 (one block barrier per tile).
+template <bool Q8>
 __global__ void __launch_bounds__(kMmThreads, 1) k_gate_bwd_mm(GateBwdMmJobs J) {
   __shared__ __attribute__((aligned(16))) float Zs[2][kMmRows * kBmLd];
   __shared__ __attribute__((aligned(16))) float LnS[2][2][4][64];
@@ -1342,9 +1447,9 @@ __global__ void __launch_bounds__(kMmThreads, 1) k_gate_bwd_mm(GateBwdMmJobs J) 
           if (row < jb.rows) {
             const float* lnS = &LnS[k][g][0][0];
             float* zrow = Zs[i & 1] + lr * kBmLd + 128 * g;
-            if (gj.mode == BWD_ATOM) gate_bwd_mm_row<64, BWD_ATOM>(gj, row, xi[g], j, lnS, lp, zrow);
-            else if (gj.mode == BWD_BOND) gate_bwd_mm_row<64, BWD_BOND>(gj, row, xi[g], j, lnS, lp, zrow);
-            else gate_bwd_mm_row<64, BWD_ANGLE>(gj, row, xi[g], j, lnS, lp, zrow);
+            if (gj.mode == BWD_ATOM) gate_bwd_mm_row<64, BWD_ATOM, Q8>(gj, row, xi[g], j, lnS, lp, zrow);
+            else if (gj.mode == BWD_BOND) gate_bwd_mm_row<64, BWD_BOND, Q8>(gj, row, xi[g], j, lnS, lp, zrow);
+            else gate_bwd_mm_row<64, BWD_ANGLE, Q8>(gj, row, xi[g], j, lnS, lp, zrow);
           }
           bwd_mm_ln_add(lp, Wsum[jb.gid[g]][cw]);
         }
@@ -1410,6 +1515,7 @@ struct GateBwd128Jobs {
   float* lnpart[3];  // by slot: [gridDim.x][4 * 128], or nullptr
 };
 
+template <bool Q8>
 __global__ void __launch_bounds__(kBm2Threads, 1) k_gate_bwd_mm128(GateBwd128Jobs J) {
   constexpr int D = 128;
   __shared__ __attribute__((aligned(16))) float Zs[2][kBm2Rows * kBm2Ld];
@@ -1534,9 +1640,9 @@ __global__ void __launch_bounds__(kBm2Threads, 1) k_gate_bwd_mm128(GateBwd128Job
         const BwdMmIdx x = xcur;
         const float* lnS = &LnS[k][0][0];
         float* zrow = Zs[units & 1] + lr * kBm2Ld;
-        if (gj.mode == BWD_ATOM) gate_bwd_mm_row<D, BWD_ATOM>(gj, row, x, j, lnS, lp, zrow);
-        else if (gj.mode == BWD_BOND) gate_bwd_mm_row<D, BWD_BOND>(gj, row, x, j, lnS, lp, zrow);
-        else gate_bwd_mm_row<D, BWD_ANGLE>(gj, row, x, j, lnS, lp, zrow);
+        if (gj.mode == BWD_ATOM) gate_bwd_mm_row<D, BWD_ATOM, Q8>(gj, row, x, j, lnS, lp, zrow);
+        else if (gj.mode == BWD_BOND) gate_bwd_mm_row<D, BWD_BOND, Q8>(gj, row, x, j, lnS, lp, zrow);
+        else gate_bwd_mm_row<D, BWD_ANGLE, Q8>(gj, row, x, j, lnS, lp, zrow);
       }
       bwd_mm_ln_add128(lp, Wsum[jb.gid][cw]);
       xcur = xnext;
@@ -2464,6 +2570,7 @@ __global__ void k_md_kick_commit(int n3, const float* __restrict__ pos2, const f
 struct Dims {
   int64_t N, S, E, B, A;
   int D, T, R, K;
+  bool act8;  // pre-activations kept in 8 bits
 };
 
 struct Acts {
@@ -2473,6 +2580,8 @@ struct Acts {
   float* e[kMaxLayers + 1];
   float* a[kMaxLayers];
   float *zv[kMaxLayers], *zae[kMaxLayers], *m[kMaxLayers], *ssum[kMaxLayers], *mu[kMaxLayers];
+  // with act8, in place of zv and zae: atom conv, bond conv, angle update
+  ZCodes zq[kMaxLayers][3];
   float *msg, *msgb, *Xa[kMaxLayers], *Xb[kMaxLayers];
   float *hE1, *aE1, *hE2, *aE2, *hS1, *aS1, *hS2, *aS2, *hF1, *aF1, *hF2, *aF2, *oE, *oS, *oF, *oM, *gM;
   float* dvf;  // gradient of v^{t+1} including the sequential block's bond and angle inputs
@@ -2560,8 +2669,17 @@ void carve_acts(Arena& ar, const Dims& m, Acts& a, int64_t n_params_aligned) {
   }
   for (int t = 0; t < m.T; ++t) {
     a.a[t] = ar.take<float>(A * D);
-    a.zv[t] = ar.take<float>(E * 2 * D);
-    a.zae[t] = ar.take<float>(A * 4 * D);
+    if (m.act8) {
+      // 16 codes a piece; an angle's row holds those of both its gates
+      const int lpr = (int)(D / 8);
+      a.zv[t] = a.zae[t] = nullptr;
+      a.zq[t][0] = ZCodes{ar.take<uint4>(E * lpr), ar.take<float2>(E), lpr, 1};
+      a.zq[t][1] = ZCodes{ar.take<uint4>(A * 2 * lpr), ar.take<float2>(A * 2), 2 * lpr, 2};
+      a.zq[t][2] = ZCodes{a.zq[t][1].q + lpr, a.zq[t][1].step + 1, 2 * lpr, 2};
+    } else {
+      a.zv[t] = ar.take<float>(E * 2 * D);
+      a.zae[t] = ar.take<float>(A * 4 * D);
+    }
     a.m[t] = ar.take<float>(N * D);
     a.ssum[t] = ar.take<float>(B * D);
     a.mu[t] = ar.take<float>(B * D);
@@ -2838,7 +2956,7 @@ int pack_params(const ParamLayout& L, const ParamLayout& La, const PackTable& pk
 // Launch the gates of one layer (forward) as one multi-job kernel.
 // Launch the fused forward gates of one layer: a persistent grid of one
 // block per compute unit.
-int gate_fwd_mm_launch(int D, GateMmJobs J, hipStream_t st) {
+int gate_fwd_mm_launch(int D, GateMmJobs J, bool q8, hipStream_t st) {
   int64_t rows = 0;
   for (int i = 0; i < J.n; ++i) rows += J.j[i].rows;
   const int rows_per_tile = D == 128 ? 32 : rows >= kMmTallRows ? 96 : 64;
@@ -2852,12 +2970,15 @@ int gate_fwd_mm_launch(int D, GateMmJobs J, hipStream_t st) {
   }
   const int grid = xcd_grid(nt, K.n);
   if (grid == 0) return CHGNET_OK;
-  if (rows_per_tile == 96)
-    KLAUNCH(st, "k_gate_fwd", k_gate_fwd_mm<64, 96><<<grid, MmCfg<64, 96>::Threads, 0, st>>>(K));
-  else if (rows_per_tile == 64)
-    KLAUNCH(st, "k_gate_fwd", k_gate_fwd_mm<64, 64><<<grid, MmCfg<64, 64>::Threads, 0, st>>>(K));
-  else
-    KLAUNCH(st, "k_gate_fwd", k_gate_fwd_mm<128, 32><<<grid, MmCfg<128, 32>::Threads, 0, st>>>(K));
+#define GATE_FWD(DD, R)                                                                                            \
+  do {                                                                                                           \
+    if (q8) KLAUNCH(st, "k_gate_fwd", k_gate_fwd_mm<DD, R, true><<<grid, MmCfg<DD, R>::Threads, 0, st>>>(K));       \
+    else KLAUNCH(st, "k_gate_fwd", k_gate_fwd_mm<DD, R, false><<<grid, MmCfg<DD, R>::Threads, 0, st>>>(K));         \
+  } while (0)
+  if (rows_per_tile == 96) GATE_FWD(64, 96);
+  else if (rows_per_tile == 64) GATE_FWD(64, 64);
+  else GATE_FWD(128, 32);
+#undef GATE_FWD
   return CHGNET_OK;
 }
 
@@ -2903,7 +3024,7 @@ GateBwdJob bwd_job(int mode, int64_t rows, const float* z, int ldz, LnPtrs ln, c
 // Job i writes its LayerNorm parameter partials to slot[i] (lnpart slots of
 // 3 x T); with ln_grad their reductions into ln_grad[i] are appended to
 // `defer`, to run after the whole backward.
-int gate_bwd_launch(int D, GateBwdJobs J, float* const* ln_grad, const int* slot, const Acts& a,
+int gate_bwd_launch(int D, GateBwdJobs J, bool q8, float* const* ln_grad, const int* slot, const Acts& a,
                     std::vector<ReduceJob>& defer, hipStream_t st) {
   GateBwdJobs K{};
   int blocks = 0;
@@ -2918,8 +3039,10 @@ int gate_bwd_launch(int D, GateBwdJobs J, float* const* ln_grad, const int* slot
     K.n++;
   }
   if (blocks == 0) return CHGNET_OK;
-  if (D == 64) KLAUNCH(st, "k_gate_bwd", k_gate_bwd<64><<<blocks, 256, 0, st>>>(K));
-  else KLAUNCH(st, "k_gate_bwd", k_gate_bwd<128><<<blocks, 256, 0, st>>>(K));
+  if (D == 64 && q8) KLAUNCH(st, "k_gate_bwd", k_gate_bwd<64, true><<<blocks, 256, 0, st>>>(K));
+  else if (D == 64) KLAUNCH(st, "k_gate_bwd", k_gate_bwd<64, false><<<blocks, 256, 0, st>>>(K));
+  else if (q8) KLAUNCH(st, "k_gate_bwd", k_gate_bwd<128, true><<<blocks, 256, 0, st>>>(K));
+  else KLAUNCH(st, "k_gate_bwd", k_gate_bwd<128, false><<<blocks, 256, 0, st>>>(K));
   return CHGNET_OK;
 }
 
@@ -2928,7 +3051,7 @@ int gate_bwd_launch(int D, GateBwdJobs J, float* const* ln_grad, const int* slot
 // slot[gid] is the lnpart slot of gate id gid (0 atom conv, 1 bond conv, 2
 // angle update); with ln_grad, each used slot's reduction into ln_grad[gid]
 // is appended to `defer`.
-int gate_bwd_mm_launch(int D, GateBwdMmJobs J, float* const* ln_grad, const int* slot, const Acts& a,
+int gate_bwd_mm_launch(int D, GateBwdMmJobs J, bool q8, float* const* ln_grad, const int* slot, const Acts& a,
                        std::vector<ReduceJob>& defer, hipStream_t st) {
   bool used[3] = {false, false, false};
   auto ln_slots = [&](int grid, float** lnpart) -> int {
@@ -2966,7 +3089,8 @@ int gate_bwd_mm_launch(int D, GateBwdMmJobs J, float* const* ln_grad, const int*
     if (maxt == 0) return CHGNET_OK;
     const int grid = std::min(maxt, 256);
     if (int rc = ln_slots(grid, K.lnpart)) return rc;
-    KLAUNCH(st, "k_gate_bwd", k_gate_bwd_mm128<<<grid, kBm2Threads, 0, st>>>(K));
+    if (q8) KLAUNCH(st, "k_gate_bwd", k_gate_bwd_mm128<true><<<grid, kBm2Threads, 0, st>>>(K));
+    else KLAUNCH(st, "k_gate_bwd", k_gate_bwd_mm128<false><<<grid, kBm2Threads, 0, st>>>(K));
     return CHGNET_OK;
   }
   GateBwdMmJobs K{};
@@ -2983,7 +3107,8 @@ int gate_bwd_mm_launch(int D, GateBwdMmJobs J, float* const* ln_grad, const int*
   if (tiles == 0) return CHGNET_OK;
   const int grid = std::min(tiles, 256);
   if (int rc = ln_slots(grid, K.lnpart)) return rc;
-  KLAUNCH(st, "k_gate_bwd", k_gate_bwd_mm<<<grid, kMmThreads, 0, st>>>(K));
+  if (q8) KLAUNCH(st, "k_gate_bwd", k_gate_bwd_mm<true><<<grid, kMmThreads, 0, st>>>(K));
+  else KLAUNCH(st, "k_gate_bwd", k_gate_bwd_mm<false><<<grid, kMmThreads, 0, st>>>(K));
   return CHGNET_OK;
 }
 
@@ -3012,7 +3137,7 @@ int make_ctx(const chgnet_hparams* hp, const chgnet_batch* batch, const chgnet_g
   c.batch = batch;
   c.graph = graph;
   c.dm = Dims{batch->n_atoms, batch->n_struct, graph->n_edges, graph->n_bonds, graph->n_angles,
-              hp->d, hp->n_layers, hp->n_rbf, hp->n_fourier};
+              hp->d, hp->n_layers, hp->n_rbf, hp->n_fourier, hp->act_bits == 8};
   c.L = make_layout(*hp, 1);
   c.La = make_layout(*hp, 4);
   c.pk = pack_table(c.L, c.La, c.dm);
@@ -3138,19 +3263,27 @@ int forward_impl(Ctx& c, const float* Pflat, float* energy, float* forces, float
       GateMmJobs J{};
       float* zv = c.save_z ? a.zv[t] : nullptr;
       float* zae = c.save_z ? a.zae[t] : nullptr;
+      const bool q8 = c.save_z && m.act8;
       if (which & 1) {
         J.j[J.n] = mm_job(D, FWD_ATOM, E, a.e[t], Wx_av, P + lo.av.b, ad_av, ln_ptrs(P, lo.av), a.ea, nullptr, a.msg,
                           zv, 2 * D);
+        if (q8) J.j[J.n].zcodes = a.zq[t][0];
         // e^{t+1} = e^t outside G^b (the bond rows are updated after)
         J.j[J.n++].xcopy = bond && a.e[t + 1] != a.e[t] ? a.e[t + 1] : nullptr;
       }
-      if (which & 2)
-        J.j[J.n++] = mm_job(D, FWD_BOND, A, a.a[t], Wx_be, P + lo.be.b, ad_be, ln_ptrs(P, lo.be), a.eb, a.ang_b2,
-                            a.msgb, zae, 4 * D);
-      if (which & 4)
-        J.j[J.n++] = mm_job(D, FWD_ANGLE, A, a.a[t], Wx_an, P + lo.an.b, ad_an, ln_ptrs(P, lo.an), a.a[t], nullptr,
-                            a.a[t + 1], zae ? zae + 2 * D : nullptr, 4 * D);
-      return gate_fwd_mm_launch(D, J, st);
+      if (which & 2) {
+        J.j[J.n] = mm_job(D, FWD_BOND, A, a.a[t], Wx_be, P + lo.be.b, ad_be, ln_ptrs(P, lo.be), a.eb, a.ang_b2,
+                          a.msgb, zae, 4 * D);
+        if (q8) J.j[J.n].zcodes = a.zq[t][1];
+        J.n++;
+      }
+      if (which & 4) {
+        J.j[J.n] = mm_job(D, FWD_ANGLE, A, a.a[t], Wx_an, P + lo.an.b, ad_an, ln_ptrs(P, lo.an), a.a[t], nullptr,
+                          a.a[t + 1], zae ? zae + 2 * D : nullptr, 4 * D);
+        if (q8) J.j[J.n].zcodes = a.zq[t][2];
+        J.n++;
+      }
+      return gate_fwd_mm_launch(D, J, q8, st);
     };
     // messages: m_i = sum over out-edges of e^a * phi_v; mu_b = eb_b * sum over
     // angles (b, b2) of eb_b2 * phi_e
@@ -3513,21 +3646,24 @@ int backward_impl(Ctx& c, const float* Pflat, bool repack, const float* dE, cons
         lg_out[J.n] = G + lg.be.g_c;
         J.j[J.n++] = bwd_job(BWD_BOND, A, a.zae[t], 4 * D, ln_ptrs(P, lo.be), a.dmu, a.ang_b1, a.eb, a.ang_b2,
                              a.t2, a.dzae, 4 * D);
+        J.j[J.n - 1].zcodes = a.zq[t][1];
       }
       if (which & 1) {
         slot[J.n] = 3 * t + 1;
         lg_out[J.n] = G + lg.av.g_c;
         J.j[J.n++] = bwd_job(BWD_ATOM, E, a.zv[t], 2 * D, ln_ptrs(P, lo.av), a.dm, a.edge_src, a.ea, nullptr,
                              a.dea, a.dzv, 2 * D);
+        J.j[J.n - 1].zcodes = a.zq[t][0];
         J.j[J.n - 1].aux_acc = t < m.T - 1;  // the first layer of the backward starts d e^a
       }
       if (which & 4) {
         slot[J.n] = 3 * t + 2;
         lg_out[J.n] = G + lg.an.g_c;
-        J.j[J.n++] = bwd_job(BWD_ANGLE, A, a.zae[t] + 2 * D, 4 * D, ln_ptrs(P, lo.an), a.da[cur], nullptr,
-                             nullptr, nullptr, nullptr, a.dzae + 2 * D, 4 * D);
+        J.j[J.n++] = bwd_job(BWD_ANGLE, A, m.act8 ? nullptr : a.zae[t] + 2 * D, 4 * D, ln_ptrs(P, lo.an), a.da[cur],
+                             nullptr, nullptr, nullptr, nullptr, a.dzae + 2 * D, 4 * D);
+        J.j[J.n - 1].zcodes = a.zq[t][2];
       }
-      return gate_bwd_launch(D, J, wg ? lg_out : nullptr, slot, a, reduce_jobs, st);
+      return gate_bwd_launch(D, J, m.act8, wg ? lg_out : nullptr, slot, a, reduce_jobs, st);
     };
     // fused gate backward and edge/angle input gradients: edges
     // de(e^t) = de(e^{t+1}) + dz_v W_av,e^T; angles da(a^t) = da(a^{t+1}) +
@@ -3541,6 +3677,7 @@ int backward_impl(Ctx& c, const float* Pflat, bool repack, const float* dE, cons
         q.gid[0] = 0;
         q.g[0] = bwd_job(BWD_ATOM, E, a.zv[t], 2 * D, ln_ptrs(P, lo.av), a.dm, a.edge_src, a.ea, nullptr, a.dea,
                          a.dzv, 2 * D);
+        q.g[0].zcodes = a.zq[t][0];
         q.g[0].aux_acc = t < m.T - 1;  // the first layer of the backward starts d e^a
         q.W[0] = Wav + 2 * D * 2 * D;
         q.res = de_res;
@@ -3553,20 +3690,22 @@ int backward_impl(Ctx& c, const float* Pflat, bool repack, const float* dE, cons
         q.gid[0] = 1;
         q.g[0] = bwd_job(BWD_BOND, A, a.zae[t], 4 * D, ln_ptrs(P, lo.be), a.dmu, a.ang_b1, a.eb, a.ang_b2, a.t2,
                          a.dzae, 4 * D);
+        q.g[0].zcodes = a.zq[t][1];
         q.W[0] = Wbe + 3 * D * 2 * D;
         if (ang) {
           q.gid[1] = 2;
-          q.g[1] = bwd_job(BWD_ANGLE, A, a.zae[t] + 2 * D, 4 * D, ln_ptrs(P, lo.an), a.da[cur], nullptr, nullptr,
-                           nullptr, nullptr, a.dzae + 2 * D, 4 * D);
+          q.g[1] = bwd_job(BWD_ANGLE, A, m.act8 ? nullptr : a.zae[t] + 2 * D, 4 * D, ln_ptrs(P, lo.an), a.da[cur],
+                           nullptr, nullptr, nullptr, nullptr, a.dzae + 2 * D, 4 * D);
+          q.g[1].zcodes = a.zq[t][2];
           q.W[1] = Wan + 3 * D * 2 * D;
           q.res = a.da[cur];
         }
         q.dx = a.da[nx];
       }
       const int slot[3] = {3 * t + 1, 3 * t, 3 * t + 2};
-      if (!wg) return gate_bwd_mm_launch(D, J, nullptr, slot, a, reduce_jobs, st);
+      if (!wg) return gate_bwd_mm_launch(D, J, m.act8, nullptr, slot, a, reduce_jobs, st);
       float* lg_out[3] = {G + lg.av.g_c, G + lg.be.g_c, G + lg.an.g_c};
-      return gate_bwd_mm_launch(D, J, lg_out, slot, a, reduce_jobs, st);
+      return gate_bwd_mm_launch(D, J, m.act8, lg_out, slot, a, reduce_jobs, st);
     };
     // per-bond sums of dz over the bond's two angle roles (DZ12) from `ncols`
     // columns of dzae starting at col0; with_deb also forms d e^b
@@ -3882,7 +4021,7 @@ int forward_full(Ctx& c, const float* Pflat, float* energy, float* forces, float
 size_t acts_bytes(const chgnet_hparams& hp, int64_t N, int64_t E, int64_t B, int64_t A, int64_t S) {
   Arena ar;
   Acts a;
-  Dims m{N, S, E, B, A, hp.d, hp.n_layers, hp.n_rbf, hp.n_fourier};
+  Dims m{N, S, E, B, A, hp.d, hp.n_layers, hp.n_rbf, hp.n_fourier, hp.act_bits == 8};
   carve_acts(ar, m, a, make_layout(hp, 4).total);
   if (hp.conservative) {
     // dual-number buffers of the weight gradient through the conservative readout
@@ -3936,7 +4075,7 @@ int step_entry(const chgnet_hparams* hp, const chgnet_batch* batch, chgnet_graph
     Arena ar{static_cast<char*>(ws), ws_bytes, 0};
     ar.used = graph_scratch_bytes(batch->n_atoms, batch->n_struct);
     Acts a0;
-    Dims d0{batch->n_atoms, batch->n_struct, 0, 0, 0, hp->d, hp->n_layers, hp->n_rbf, hp->n_fourier};
+    Dims d0{batch->n_atoms, batch->n_struct, 0, 0, 0, hp->d, hp->n_layers, hp->n_rbf, hp->n_fourier, hp->act_bits == 8};
     const ParamLayout L1 = make_layout(*hp, 1), L4 = make_layout(*hp, 4);
     carve_acts(ar, d0, a0, L4.total);
     if (!ws || !ar.ok()) return fail(CHGNET_EWORKSPACE, "workspace too small (query chgnet_workspace_size)");
@@ -4046,7 +4185,7 @@ int md_entry(const chgnet_hparams* hp, const chgnet_batch* batch, chgnet_graph* 
     Arena ar{static_cast<char*>(ws), ws_bytes, 0};
     ar.used = graph_scratch_bytes(batch->n_atoms, batch->n_struct);
     Acts a;
-    Dims d0{batch->n_atoms, batch->n_struct, 0, 0, 0, hp->d, hp->n_layers, hp->n_rbf, hp->n_fourier};
+    Dims d0{batch->n_atoms, batch->n_struct, 0, 0, 0, hp->d, hp->n_layers, hp->n_rbf, hp->n_fourier, hp->act_bits == 8};
     carve_acts(ar, d0, a, make_layout(*hp, 4).total);
     if (!ws || !ar.ok()) return fail(CHGNET_EWORKSPACE, "workspace too small (query chgnet_workspace_size)");
     pos2 = a.md_pos;
