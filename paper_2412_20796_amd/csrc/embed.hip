@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(RunSums s) {
 // tokens, block b < n takes the row of token b if b is the first of its kind,
 // and the blocks after them write the zeros of the other rows.
 // ---------------------------------------------------------------------------
-constexpr int kFewTokens = 8192, kFewThreads = 1024, kFewZeroRows = 512;
+constexpr int kFewTokens = 16384, kFewThreads = 1024, kFewZeroRows = 512;
 constexpr int kFewEach = kFewTokens / kFewThreads;  // tokens a thread looks at, at most
 
 template <class T, int VEC, int LPR>
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int voc
                                                            float scale, float* __restrict__ dw, int64_t ldw, int add,
                                                            int by_row) {
   constexpr int W = kFewThreads / 64, G = kFewThreads / LPR, U = 8;
-  __shared__ int list[kFewTokens];
+  __shared__ unsigned short list[kFewTokens];
   __shared__ int wtot[W], has[kFewZeroRows];
   __shared__ float red[G][LPR * VEC];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -532,7 +532,7 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int voc
     if (k < wave) at += wtot[k];
     m += wtot[k];
   }
-  for (; hits; hits &= hits - 1) list[at++] = t * each + __ffs(hits) - 1;
+  for (; hits; hits &= hits - 1) list[at++] = (unsigned short)(t * each + __ffs(hits) - 1);
   __syncthreads();
   if (!by_row && list[0] != b) return;  // not the first of its kind
   if (add && m == 0) return;
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int voc
 
 // Whether a call takes the one launch: what its blocks look at must stay small.
 bool few_tokens(int64_t n, int64_t vocab) {
-  return n <= kFewTokens && std::min(n, vocab) * n <= (1 << 20);
+  return n <= kFewTokens && std::min(n, vocab) * n <= (1 << 21);
 }
 
 // Values a lane: 16 bytes of the type, 4 values of 16 bits where 8 do not fit
@@ -661,14 +661,18 @@ int embed_forward_entry(int64_t n, int32_t d, int64_t vocab, int32_t dtype, cons
   });
 }
 
+size_t embed_backward_bytes(int64_t n, int32_t d, int64_t vocab) {
+  Arena ar;
+  EmbedWs w;
+  carve_embed(ar, n, d, vocab, w);
+  return ar.used;
+}
+
 int embed_backward_workspace_entry(int64_t n, int32_t d, int64_t vocab, size_t* bytes) {
   CHG_TRY(check_embed("embed_backward_workspace", n, d, vocab, CHGNET_F32, 0));
   if (n > kMaxTokens) return fail(CHGNET_EINVAL, "embed_backward_workspace: n must be at most 2^30");
   if (!bytes) return fail(CHGNET_EINVAL, "embed_backward_workspace: bytes is NULL");
-  Arena ar;
-  EmbedWs w;
-  carve_embed(ar, n, d, vocab, w);
-  *bytes = ar.used;
+  *bytes = embed_backward_bytes(n, d, vocab);
   return CHGNET_OK;
 }
 

@@ -18,6 +18,7 @@
 #include <cmath>
 #include <vector>
 
+#include "chgnet_ops.h"
 #include "common.hpp"
 #include "gemm.hpp"
 #include "rowops.hpp"
@@ -29,6 +30,10 @@ size_t graph_scratch_bytes(int64_t N, int64_t S);
 int build_graph(const chgnet_hparams* hp, const chgnet_batch* batch, chgnet_graph* graph, void* ws, size_t ws_bytes,
                 hipStream_t st);
 int validate_batch(const chgnet_batch* b);
+size_t embed_backward_bytes(int64_t n, int32_t d, int64_t vocab);
+int embed_backward_entry(int64_t n, int32_t d, int64_t vocab, int32_t dtype, const int32_t* tok, int32_t first,
+                         const void* dout, int64_t lddout, float scale, float* dtable, int64_t lddtable,
+                         int accumulate, void* ws, size_t ws_bytes, hipStream_t st);
 
 namespace {
 
@@ -2287,6 +2292,12 @@ __global__ void k_seed_edges2(int E, const int* __restrict__ edge_rev, const flo
 // matches in atom order, up to 8 rows' loads issued together; the eight
 // partial sums are added in wavefront order.
 constexpr int kEmbZWaves = 8;
+// Batches of more atoms take the embedding operator's gradient (embed.hip),
+// whose time does not go with the most frequent element: of 8,632 atoms of
+// uniform elements 15 us here and 8 there, of 34,528 atoms 45 and 25, and where
+// every third atom is oxygen 40 and 14, and 157 and 25 (d = 64). Smaller batches
+// keep this kernel's order of the sum, at 7 to 14 us against 7 to 11.
+constexpr int64_t kEmbZAtoms = 8192;
 __global__ void __launch_bounds__(64 * kEmbZWaves) k_embed_bwd_Z(int N, int D, const int* __restrict__ Z,
                                                                  const float* __restrict__ dv0, float* __restrict__ gWZ) {
   __shared__ float red[kEmbZWaves][2][64];
@@ -2605,6 +2616,9 @@ struct Acts {
   float *md_pos, *md_vel;
   // conservative readout: dE/d FT [A,K], dE/dr_e [E,3], per-angle d theta terms [A,6]
   float *dft, *gvec, *pang;
+  // scratch of the element table's gradient on large batches
+  char* embz;
+  size_t embz_bytes;
 };
 
 // The weight matrices that products take as operands.
@@ -2752,6 +2766,8 @@ void carve_acts(Arena& ar, const Dims& m, Acts& a, int64_t n_params_aligned) {
   a.dft = ar.take<float>(A * K);
   a.gvec = ar.take<float>(3 * E);
   a.pang = ar.take<float>(6 * A);
+  a.embz_bytes = N > kEmbZAtoms ? embed_backward_bytes(N, (int32_t)D, 94) : 0;
+  a.embz = ar.take<char>((int64_t)a.embz_bytes);
 }
 
 // ---------------------------------------------------------------------------
@@ -3489,6 +3505,16 @@ int side_fork(SideStream& ss, hipStream_t st, hipEvent_t e) {
   return CHGNET_OK;
 }
 
+// gWZ += the sums of dv0 by element
+int element_table_grad(const Ctx& c, const float* dv0, float* gWZ, const char* tag, hipStream_t st) {
+  const int64_t N = c.dm.N;
+  const int D = c.dm.D;
+  if (N > kEmbZAtoms)
+    return embed_backward_entry(N, D, 94, CHGNET_F32, c.batch->Z, 1, dv0, D, 1.0f, gWZ, D, 1, c.a.embz, c.a.embz_bytes, st);
+  KLAUNCH(st, tag, k_embed_bwd_Z<<<94, 64 * kEmbZWaves, 0, st>>>((int)N, D, c.batch->Z, dv0, gWZ));
+  return CHGNET_OK;
+}
+
 // G == nullptr with dft_out: the conservative readout's pass, the input
 // gradients of the energy (no weight gradients; dE, dF, dS not read), and also
 // dE/d FT = da^0 W_th^T [A,K].
@@ -3919,7 +3945,7 @@ int backward_impl(Ctx& c, const float* Pflat, bool repack, const float* dE, cons
     CHG_TRY(fill(a.da[cur], A * D, 0.f, st));
   }
   // embeddings
-  if (wg) KLAUNCH(st, "k_embed_bwd_Z", k_embed_bwd_Z<<<94, 64 * kEmbZWaves, 0, st>>>((int)N, D, bt.Z, a.dv[cur], G + Lg.W_Z));
+  if (wg) CHG_TRY(element_table_grad(c, a.dv[cur], G + Lg.W_Z, "k_embed_bwd_Z", st));
   {
     std::vector<TnProblem> ts;
     ts.push_back(tp(E, m.R, D, a.rbf_a, m.R, 0, nullptr, a.de[ecur], D, 0, nullptr, G + Lg.W_e, 2 * D));

@@ -253,3 +253,24 @@ def test_operators_together(dtype):
     terms = torch.zeros(V, dtype=torch.float64).index_add_(0, Z.long() - 1, (dz.cpu().double().abs() @ Wt.double().abs().t()).amax(1))
     eps = torch.finfo(dtype).eps
     assert bool(((dtable.cpu().double() - T64.grad).abs() <= 4 * eps * scale * terms[:, None] + 1e-5).all())
+
+
+@gpu
+@pytest.mark.parametrize("k,kw", [(8, {}), (16, {}), (16, dict(act_bits=8)), (8, dict(conservative=True))])
+def test_element_table_of_a_large_batch(k, kw):
+    """8 and 16 copies of 40 crystals (8,632 and 17,264 atoms: the embedding operator's gradient with and without the
+    ordering of the atoms) give k times the element table's gradient of one."""
+    b = synth.make_batch("triclinic40")
+    d, T = 64, 1
+    params = synth.make_params(d, T, seed=(10, 1, 0))
+    targets = synth.make_targets(b, seed=(10, 2, 0))
+    hp, p = bd.hparams(d=d, n_layers=T, **kw), _dev(params)
+    g = []
+    for n in (1, k):
+        bb, tg = _copies(b, n), [_dev(np.concatenate([x] * n)) for x in targets]
+        loss, grad = bd.step(hp, bd.DeviceBatch.from_host(bb), bd.DeviceGraph(bb.n_atoms, 64, 16, 64), p, tg, bd.Workspace())
+        g.append(grad[:94 * d].cpu().double().numpy())
+    # the loss's means over k times as many values make the sums of k copies one copy's; sums of up to 16 x 20 rows round
+    # by 2^-24 of their terms each, and the rows themselves by a few 1e-7 from batch to batch (codes that turn: 1e-4)
+    scale = np.abs(g[0]).max()
+    assert np.abs(g[1] - g[0]).max() <= (1e-3 if kw.get("act_bits") else 2e-5) * scale
