@@ -251,13 +251,15 @@ struct RunSums {
 };
 constexpr int kRunThreads = 512;
 
-// zeros in the rows of v0 .. v0 + kRunThreads - 1 without a token, columns [col0, col1)
+constexpr int kZeroRows = kRunThreads;
+
+// zeros in the rows v0 .. v0 + kZeroRows - 1 without a token, columns [col0, col1)
 template <int VEC>
 __device__ __forceinline__ void zero_rows(const RunSums& s, int64_t v0, int col0, int col1) {
-  __shared__ int none[kRunThreads];
+  __shared__ int none[kZeroRows];
   const int t = threadIdx.x, lane = t & 63;
   const int64_t v = v0 + t;
-  if (v < s.vocab) {
+  if (t < kZeroRows && v < s.vocab) {
     int lo = -1, hi = s.n;  // first position whose row is v or later: hi
     while (hi - lo > 1) {
       const int mid = lo + (hi - lo) / 2;
@@ -267,7 +269,7 @@ __device__ __forceinline__ void zero_rows(const RunSums& s, int64_t v0, int col0
     none[t] = hi == s.n || s.row[hi] != v;
   }
   __syncthreads();
-  const int rows = (int)min((int64_t)kRunThreads, s.vocab - v0);
+  const int rows = (int)min((int64_t)kZeroRows, s.vocab - v0);
   for (int r = t >> 6; r < rows; r += kRunThreads / 64) {
     if (!none[r]) continue;
     float* w = s.dw + (v0 + r) * s.ldw;
@@ -289,7 +291,7 @@ __global__ void __launch_bounds__(kRunThreads) k_embed_runs(RunSums s, const int
   const int col0 = blockIdx.y * C;
   const int blk = (int)blockIdx.x - s.nzero;
   if (blk < 0) {
-    zero_rows<VEC < 4 ? VEC : 4>(s, (int64_t)blockIdx.x * kRunThreads, col0, min(col0 + C, s.d));
+    zero_rows<VEC < 4 ? VEC : 4>(s, (int64_t)blockIdx.x * kZeroRows, col0, min(col0 + C, s.d));
     return;
   }
   const int b0 = blk * s.stretch, b1 = min(b0 + s.stretch, s.n);
@@ -471,9 +473,10 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(RunSums s) {
 // looking at all of them and sums their rows. By row, block v takes row v (and
 // writes its zeros if it has no token). By token, for tables with more rows than
 // tokens, block b < n takes the row of token b if b is the first of its kind,
-// and the blocks after them write the zeros of the other rows.
+// and the blocks after them write the zeros of the other rows. Each of the
+// launch's y blocks takes LPR VEC columns.
 // ---------------------------------------------------------------------------
-constexpr int kFewTokens = 16384, kFewThreads = 1024, kFewZeroRows = 512;
+constexpr int kFewTokens = 16384, kFewThreads = 1024, kFewZeroRows = 128;
 constexpr int kFewEach = kFewTokens / kFewThreads;  // tokens a thread looks at, at most
 
 template <class T, int VEC, int LPR>
@@ -486,6 +489,7 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int voc
   __shared__ int wtot[W], has[kFewZeroRows];
   __shared__ float red[G][LPR * VEC];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int c0 = blockIdx.y * LPR * VEC, c = c0 + t % LPR * VEC;
   if (!by_row && (int)blockIdx.x >= n) {
     const int64_t step = (int64_t)(gridDim.x - n) * kFewZeroRows;
     for (int64_t v0 = (int64_t)(blockIdx.x - n) * kFewZeroRows; v0 < vocab; v0 += step) {
@@ -497,11 +501,10 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int voc
       }
       __syncthreads();
       const int rows = (int)min((int64_t)kFewZeroRows, vocab - v0);
-      for (int r = wave; r < rows; r += W) {
-        if (has[r]) continue;
-        float* w = dw + (v0 + r) * ldw;
+      for (int r = t / LPR; r < rows; r += G) {
+        if (has[r] || c >= d) continue;
         const float none[VEC] = {};
-        for (int c = lane * VEC; c < d; c += 64 * VEC) store_v<VEC>(w + c, none);
+        store_v<VEC>(dw + (v0 + r) * ldw + c, none);
       }
       __syncthreads();
     }
@@ -536,41 +539,42 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int voc
   __syncthreads();
   if (!by_row && list[0] != b) return;  // not the first of its kind
   if (add && m == 0) return;
-  const int j = t % LPR, g = t / LPR, groups = min(G, (m + U - 1) / U);
   // a group's share of the list, at least U rows if there are as many
+  const int g = t / LPR, groups = min(G, (m + U - 1) / U);
   const int q0 = g < groups ? (int)((int64_t)m * g / groups) : 0, q1 = g < groups ? (int)((int64_t)m * (g + 1) / groups) : 0;
-  for (int c0 = 0; c0 < d; c0 += LPR * VEC) {
-    const int c = c0 + j * VEC;
-    float acc[VEC] = {};
-    for (int q = q0; q < q1; q += U) {
-      float x[U][VEC];
+  float acc[VEC] = {};
+  for (int q = q0; q < q1; q += U) {
+    float x[U][VEC];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) x[u][k] = 0.f;
-        if (q + u < q1 && c < d) load_v<VEC>(dout + list[q + u] * ldo + c, x[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) acc[k] += x[u][k];
+      for (int k = 0; k < VEC; ++k) x[u][k] = 0.f;
+      if (q + u < q1 && c < d) load_v<VEC>(dout + list[q + u] * ldo + c, x[u]);
     }
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) red[g][j * VEC + k] = acc[k];
-    __syncthreads();
-    for (int x = t; x < LPR * VEC && c0 + x < d; x += kFewThreads) {
-      float sum = red[0][x];
-      for (int k = 1; k < groups; ++k) sum += red[k][x];
-      float* w = dw + v * ldw + c0 + x;
-      *w = add ? *w + scale * sum : scale * sum;
-    }
-    __syncthreads();
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) acc[k] += x[u][k];
+  }
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) red[g][t % LPR * VEC + k] = acc[k];
+  __syncthreads();
+  if (t < LPR * VEC && c0 + t < d) {
+    float sum = red[0][t];
+    for (int k = 1; k < groups; ++k) sum += red[k][t];
+    float* w = dw + v * ldw + c0 + t;
+    *w = add ? *w + scale * sum : scale * sum;
   }
 }
 
-// Whether a call takes the one launch: what its blocks look at must stay small.
-bool few_tokens(int64_t n, int64_t vocab) {
-  return n <= kFewTokens && std::min(n, vocab) * n <= (1 << 21);
+// Whether a call whose blocks take `cols` columns each is the one launch: what
+// its blocks look at must stay small, and so must the rows of a frequent token,
+// which one block adds up alone. Of 94 table rows, with tokens evenly spread and
+// with a third of them on one row, against the ordering's four launches, us a
+// call: 16,384 of 64 fp32 11 and 19 (20 and 22), 12,000 of 128 7 and 18 (18 and
+// 19), 16,384 of 128 11 and 29, 8,192 of 512 9 and 26 (17 and 18).
+bool few_tokens(int64_t n, int cols, int64_t vocab) {
+  return n <= kFewTokens && std::min(n, vocab) * n <= (1 << 21) && n * cols <= 3 << 19;
 }
 
 // Values a lane: 16 bytes of the type, 4 values of 16 bits where 8 do not fit
@@ -627,7 +631,7 @@ struct EmbedWs {
   float* part;
 };
 void carve_embed(Arena& ar, int64_t n, int32_t d, int64_t vocab, EmbedWs& w) {
-  if (few_tokens(n, vocab)) return;
+  if (few_tokens(n, std::min(d, 512), vocab)) return;  // whichever columns the call's blocks take
   for (int k = 0; k < 2; ++k) {
     w.row[k] = ar.take<int>(n);
     w.pos[k] = ar.take<int>(n);
@@ -689,7 +693,7 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
   const int n = (int)n64, vocab = (int)vocab64;
   const int add = accumulate != 0;
   const int vec = vec_of(dtype, d, ldo, ldw, dout, dtable, 4);
-  if (few_tokens(n, vocab)) {
+  if (few_tokens(n, std::min(d, lanes_of(d, vec) * vec), vocab)) {
     if (n == 0 && add) return CHGNET_OK;
     const bool by_row = vocab <= n;
     const unsigned blocks = (unsigned)(by_row ? vocab : n + (add ? 0 : std::min<int64_t>(4096, cdiv(vocab, kFewZeroRows))));
@@ -697,7 +701,7 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
       using T = decltype(t);
       return with_lanes<T>(d, vec, [&](auto V, auto L) -> int {
         KLAUNCH(st, "k_embed_few",
-                k_embed_few<T, V.value, L.value><<<blocks, kFewThreads, 0, st>>>(
+                k_embed_few<T, V.value, L.value><<<dim3(blocks, (unsigned)cdiv(d, L.value * V.value)), kFewThreads, 0, st>>>(
                     n, d, vocab, tok, first, static_cast<const T*>(dout), ldo, scale, dtable, ldw, add, by_row));
         return CHGNET_OK;
       });
@@ -751,7 +755,7 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
   r.dw = dtable;
   r.add = add;
   r.part = w.part;
-  r.nzero = add ? 0 : (int)cdiv(vocab, kRunThreads);
+  r.nzero = add ? 0 : (int)cdiv(vocab, kZeroRows);
   CHG_TRY(with_type(dtype, [&](auto t) {
     using T = decltype(t);
     return with_lanes<T>(d, vec, [&](auto V, auto L) -> int {

@@ -14,6 +14,7 @@ are written so that they add little to that (a dozen attribute reads).
 from __future__ import annotations
 
 import ctypes
+from functools import lru_cache
 
 import torch
 
@@ -93,6 +94,20 @@ def _call(fn, gpu, args):
         bd._check(code)
 
 
+@lru_cache(maxsize=4096)
+def _gate_bytes(rows, d):
+    need = ctypes.c_size_t()
+    bd._check(lib().chgnet_gate_backward_workspace(rows, d, ctypes.byref(need)))
+    return need.value
+
+
+@lru_cache(maxsize=4096)
+def _embed_bytes(n, d, vocab):
+    need = ctypes.c_size_t()
+    bd._check(lib().chgnet_embed_backward_workspace(n, d, vocab, ctypes.byref(need)))
+    return need.value
+
+
 def _workspace(ws, nbytes, gpu, like):
     """(pointer, size, owner) of the caller's Workspace grown to nbytes, or of memory for this call."""
     if ws is None:
@@ -105,25 +120,49 @@ def _workspace(ws, nbytes, gpu, like):
 
 
 class GateCheckpoint:
-    """8-bit checkpoint of a gate's input: codes [rows, 2d] uint8 and step [rows, 2] fp32 (core, gate)."""
+    """8-bit checkpoint of a gate's input: codes [rows, 2d] uint8 and step [rows, 2] fp32 (core, gate), two tensors of the
+    caller's or views of one allocation (`empty`)."""
 
-    __slots__ = ("codes", "step")
+    __slots__ = ("_codes", "_step", "_data", "_rows", "_d")
 
     def __init__(self, codes, step):
-        self.codes, self.step = codes, step
+        self._codes, self._step, self._data = codes, step, None
 
     @classmethod
     def empty(cls, rows, d, device="cuda"):
-        return cls(torch.empty(rows, 2 * d, dtype=torch.uint8, device=device),
-                   torch.empty(rows, 2, dtype=torch.float32, device=device))
+        self = cls(None, None)
+        self._data = torch.empty(rows * (2 * d + 8), dtype=torch.uint8, device=device)
+        self._rows, self._d = rows, d
+        return self
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._codes = self._data[8 * self._rows:].view(self._rows, 2 * self._d)
+        return self._codes
+
+    @property
+    def step(self):
+        if self._step is None:
+            self._step = self._data[:8 * self._rows].view(torch.float32).view(self._rows, 2)
+        return self._step
 
     @property
     def nbytes(self):
         return self.codes.numel() + 4 * self.step.numel()
 
-    def _check(self, rows, d, gpu):
-        _packed("kept.codes", self.codes, (rows, 2 * d), torch.uint8, gpu)
-        _packed("kept.step", self.step, (rows, 2), torch.float32, gpu)
+    def _pointers(self, rows, d, gpu):
+        """(codes, step) addresses of a checkpoint of [rows, 2d] on GPU `gpu`."""
+        t = self._data
+        if t is not None:
+            if self._rows != rows or self._d != d or t.get_device() != gpu:
+                _bad("the checkpoint is of [%d, %d] on %s, not of [%d, %d] on GPU %d"
+                     % (self._rows, 2 * self._d, t.device, rows, 2 * d, gpu))
+            p = t.data_ptr()
+            return (p + 8 * rows, p) if rows else (None, None)
+        _packed("kept.codes", self._codes, (rows, 2 * d), torch.uint8, gpu)
+        _packed("kept.step", self._step, (rows, 2), torch.float32, gpu)
+        return self._codes.data_ptr() or None, self._step.data_ptr() or None
 
 
 def gate_forward(z, ln, save=True, phi=None, kept=None):
@@ -147,10 +186,8 @@ def gate_forward(z, ln, save=True, phi=None, kept=None):
         return phi
     if kept is None:
         kept = GateCheckpoint.empty(rows, d, z.device)
-    else:
-        kept._check(rows, d, gpu)
     _call(lib().chgnet_gate_forward, gpu, (rows, d, code, z.data_ptr(), ldz, ln.data_ptr(), phi.data_ptr(), ldp,
-                                           kept.codes.data_ptr() or None, kept.step.data_ptr() or None))
+                                           *kept._pointers(rows, d, gpu)))
     return phi, kept
 
 
@@ -159,7 +196,7 @@ def gate_backward(kept, ln, dphi, dz=None, dln=None, accumulate=False, ws=None):
     it holds with `accumulate`. ws: a Workspace of the caller's (one for each call that may run at the same time)."""
     rows, d, code, gpu = _start("dphi", dphi)
     ldp = _rows("dphi", dphi, rows, d, dphi.dtype, gpu)
-    kept._check(rows, d, gpu)
+    codes, step = kept._pointers(rows, d, gpu)
     _packed("ln", ln, (4, d), torch.float32, gpu)
     if dz is None:
         dz, ldz = torch.empty((rows, 2 * d), dtype=dphi.dtype, device=dphi.device), 2 * d
@@ -171,12 +208,9 @@ def gate_backward(kept, ln, dphi, dz=None, dln=None, accumulate=False, ws=None):
         dln = torch.empty((4, d), dtype=torch.float32, device=dphi.device)
     else:
         _packed("dln", dln, (4, d), torch.float32, gpu)
-    L, need = lib(), ctypes.c_size_t()
-    bd._check(L.chgnet_gate_backward_workspace(rows, d, ctypes.byref(need)))
-    p, nbytes, _keep = _workspace(ws, need.value, gpu, dphi)
-    _call(L.chgnet_gate_backward, gpu, (rows, d, code, kept.codes.data_ptr(), kept.step.data_ptr(), ln.data_ptr(),
-                                        dphi.data_ptr(), ldp, dz.data_ptr(), ldz, dln.data_ptr(), bool(accumulate), p,
-                                        nbytes))
+    p, nbytes, _keep = _workspace(ws, _gate_bytes(rows, d), gpu, dphi)
+    _call(lib().chgnet_gate_backward, gpu, (rows, d, code, codes, step, ln.data_ptr(), dphi.data_ptr(), ldp,
+                                            dz.data_ptr(), ldz, dln.data_ptr(), bool(accumulate), p, nbytes))
     return dz, dln
 
 
@@ -209,9 +243,8 @@ def embed_backward(tok, dout, vocab, scale=1.0, first=0, dtable=None, accumulate
         dtable, ldw = torch.empty((vocab, d), dtype=torch.float32, device=dout.device), d
     else:
         ldw = _rows("dtable", dtable, vocab, d, torch.float32, gpu)
-    L, need = lib(), ctypes.c_size_t()
-    bd._check(L.chgnet_embed_backward_workspace(n, d, vocab, ctypes.byref(need)))
-    p, nbytes, _keep = _workspace(ws, need.value, gpu, dout) if need.value else (None, 0, None)
-    _call(L.chgnet_embed_backward, gpu, (n, d, vocab, code, tok.data_ptr(), first, dout.data_ptr(), ldo, scale,
-                                         dtable.data_ptr(), ldw, bool(accumulate), p, nbytes))
+    need = _embed_bytes(n, d, vocab)
+    p, nbytes, _keep = _workspace(ws, need, gpu, dout) if need else (None, 0, None)
+    _call(lib().chgnet_embed_backward, gpu, (n, d, vocab, code, tok.data_ptr(), first, dout.data_ptr(), ldo, scale,
+                                             dtable.data_ptr(), ldw, bool(accumulate), p, nbytes))
     return dtable
