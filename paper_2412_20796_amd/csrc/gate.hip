@@ -164,9 +164,12 @@ __global__ void __launch_bounds__(256) k_gate_act_fwd(int64_t rows, int d, const
   }
 }
 
-// Threads of a backward block, and the blocks of a launch: the LayerNorm
-// gradients of a block's rows are one partial row, and few blocks make few of
-// them, while 2 blocks of 512 threads a compute unit keep enough loads in flight.
+// Threads of a backward block, and the blocks of a launch, which walk the rows:
+// each ends in one partial row of the LayerNorm gradients. Two blocks a compute
+// unit at 4 columns a lane; wider rows have registers for one (512 against 256
+// blocks, forward and backward in us: 85,274 rows of 64 32.1 and 32.5, 397,934 of
+// 128 238 and 234, 20,011 of 333 in 16 bits 49 and 45). Blocks of 256 threads,
+// twice as many, take 251 us in place of 238.
 constexpr int kBwdThreads = 512, kBwdBlocks = 512;
 
 // part: [gridDim.x][4 d] partial sums of the LayerNorm gradients, or with one
@@ -394,13 +397,14 @@ int check_gate(const char* who, int64_t rows, int32_t d, int32_t dtype) {
   return CHGNET_OK;
 }
 
-// Blocks of a backward launch over `rows` rows, RPW a wavefront. What one block
+// Blocks of a backward launch over `rows` rows, rpw a wavefront, cpl columns a
+// lane. What one block
 // does in two turns needs no second launch to add partial rows: 8.0 us a call
 // against 10.7 (64 rows of 64 or 128); in four turns, 7.9 and 10.8 us a call, it
 // has the GPU as long as both launches.
-int bwd_blocks(int64_t rows, int rpw) {
+int bwd_blocks(int64_t rows, int rpw, int cpl) {
   const int64_t turns = cdiv(rows, rpw * (kBwdThreads / 64));
-  return turns <= 2 ? 1 : (int)std::min<int64_t>(kBwdBlocks, turns);
+  return turns <= 2 ? 1 : (int)std::min<int64_t>(cpl <= 4 ? kBwdBlocks : kBwdBlocks / 2, turns);
 }
 
 }  // namespace
@@ -469,7 +473,7 @@ int gate_backward_entry(int64_t rows, int32_t d, int32_t dtype, const uint8_t* c
     using T = decltype(t);
     return with_layout(d, vec, rows * d * (int64_t)(es + 2) >= kFarBytes, [&](auto V, auto L, auto N, auto M, auto full, auto far) -> int {
       constexpr int rpw = 64 / L.value;
-      blocks = bwd_blocks(rows, rpw);
+      blocks = bwd_blocks(rows, rpw, V.value * N.value);
       KLAUNCH(st, "k_gate_act_bwd",
               k_gate_act_bwd<T, V.value, L.value, N.value, M.value, full.value, far.value><<<blocks, kBwdThreads, 0, st>>>(
                   rows, d, codes, reinterpret_cast<const float2*>(step), ln, static_cast<const T*>(dphi), lddphi,
