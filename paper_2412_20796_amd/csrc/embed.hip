@@ -140,12 +140,12 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_place(SortPass s) {
     const int digit = t & (kDigits - 1), q = t / kDigits;
     int before = 0, all = 0;
     const int b1 = nb * (q + 1) / 4;
-    for (int b0 = nb * q / 4; b0 < b1; b0 += 16) {
-      int c[16];  // loads in flight together: one at a time they took 30 us of 1,000,003 tokens
+    for (int b0 = nb * q / 4; b0 < b1; b0 += 32) {
+      int c[32];  // loads in flight together: one at a time they took 30 us of 1,000,003 tokens
 #pragma unroll
-      for (int u = 0; u < 16; ++u) c[u] = b0 + u < b1 ? s.counts[(b0 + u) * kDigits + digit] : 0;
+      for (int u = 0; u < 32; ++u) c[u] = b0 + u < b1 ? s.counts[(b0 + u) * kDigits + digit] : 0;
 #pragma unroll
-      for (int u = 0; u < 16; ++u) {
+      for (int u = 0; u < 32; ++u) {
         before += b0 + u < (int)blockIdx.x ? c[u] : 0;
         all += c[u];
       }
@@ -417,14 +417,15 @@ __global__ void __launch_bounds__(kRunThreads) k_embed_runs(RunSums s, const int
 
 // Joins the runs that cross stretches: the block of the stretch in which a run
 // begins adds that stretch's slot 1 and slot 0 of the stretches up to the run's
-// end. 64 columns a block, 16 lanes a row; the groups of lanes take the partial
-// rows in turn, eight loads in flight, and are added in order.
+// end. `lanes` (a power of two) lanes a row of VEC columns each; the groups of
+// lanes take the partial rows in turn, eight loads in flight, and are added in
+// order. One block for all columns, since most have no run to join.
 constexpr int kJoinThreads = 512;
 
 template <int VEC>
-__global__ void __launch_bounds__(kJoinThreads) k_embed_join(RunSums s) {
-  constexpr int G = kJoinThreads / 16, U = 8, C = 16 * VEC;
-  __shared__ float red[G][C];
+__global__ void __launch_bounds__(kJoinThreads) k_embed_join(RunSums s, int lanes) {
+  constexpr int U = 8;
+  __shared__ float red[kJoinThreads * VEC];
   const int c = blockIdx.x;
   const int p0 = c * s.stretch, p1 = p0 + s.stretch;  // p1 < n: one block fewer than stretches
   const int v = s.row[p1], before = s.row[p1 - 1], first = s.row[p0], early = p0 > 0 ? s.row[p0 - 1] : -1;
@@ -441,31 +442,35 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(RunSums s) {
     else hi = mid;
   }
   const int m = lo - c + 1;  // partial rows
-  const int g = threadIdx.x >> 4, j = threadIdx.x & 15, col = blockIdx.y * C + j * VEC;
-  float acc[VEC] = {};
-  for (int q0 = g; q0 < m; q0 += G * U) {
-    float x[U][VEC];
+  const int G = kJoinThreads / lanes, g = threadIdx.x / lanes, j = threadIdx.x % lanes, used = min(m, G);
+  for (int col0 = 0; col0 < s.d; col0 += lanes * VEC) {
+    const int col = col0 + j * VEC;
+    float acc[VEC] = {};
+    for (int q0 = g; q0 < m; q0 += G * U) {
+      float x[U][VEC];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int q = q0 + u * G;
+      for (int u = 0; u < U; ++u) {
+        const int q = q0 + u * G;
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) x[u][k] = 0.f;
-      if (q < m && col < s.d) load_v<VEC>(s.part + ((int64_t)2 * (c + q) + (q == 0)) * s.d + col, x[u]);
+        for (int k = 0; k < VEC; ++k) x[u][k] = 0.f;
+        if (q < m && col < s.d) load_v<VEC>(s.part + ((int64_t)2 * (c + q) + (q == 0)) * s.d + col, x[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) acc[k] += x[u][k];
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) acc[k] += x[u][k];
+    for (int k = 0; k < VEC; ++k) red[threadIdx.x * VEC + k] = acc[k];
+    __syncthreads();
+    for (int x = threadIdx.x; x < lanes * VEC && col0 + x < s.d; x += kJoinThreads) {
+      float t = red[x];
+      for (int k = 1; k < used; ++k) t += red[k * lanes * VEC + x];
+      float* w = s.dw + v * s.ldw + col0 + x;
+      *w = s.add ? *w + s.scale * t : s.scale * t;
+    }
+    __syncthreads();
   }
-#pragma unroll
-  for (int k = 0; k < VEC; ++k) red[g][j * VEC + k] = acc[k];
-  __syncthreads();
-  const int x = threadIdx.x, cx = blockIdx.y * C + x, used = min(m, G);
-  if (x >= C || cx >= s.d) return;
-  float t = red[0][x];
-  for (int k = 1; k < used; ++k) t += red[k][x];
-  float* w = s.dw + v * s.ldw + cx;
-  *w = s.add ? *w + s.scale * t : s.scale * t;
 }
 
 // ---------------------------------------------------------------------------
@@ -773,10 +778,11 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
   }));
   if (r.nstretch > 1) {
     // the partial rows are dense: 16-byte loads where their width allows
-    if (d % 4 == 0)
-      KLAUNCH(st, "k_embed_join", k_embed_join<4><<<dim3(r.nstretch - 1, (unsigned)cdiv(d, 64)), kJoinThreads, 0, st>>>(r));
-    else
-      KLAUNCH(st, "k_embed_join", k_embed_join<1><<<dim3(r.nstretch - 1, (unsigned)cdiv(d, 16)), kJoinThreads, 0, st>>>(r));
+    const int v = d % 4 == 0 ? 4 : 1;
+    int lanes = 16;
+    while (lanes < kJoinThreads && lanes * v < d) lanes *= 2;
+    if (v == 4) KLAUNCH(st, "k_embed_join", k_embed_join<4><<<r.nstretch - 1, kJoinThreads, 0, st>>>(r, lanes));
+    else KLAUNCH(st, "k_embed_join", k_embed_join<1><<<r.nstretch - 1, kJoinThreads, 0, st>>>(r, lanes));
   }
   return CHGNET_OK;
 }
