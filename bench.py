@@ -37,6 +37,8 @@ def parse():
     ap.add_argument("--sequential", action="store_true", help="model variant: the Eq. (10) interaction block")
     ap.add_argument("--conservative", action="store_true",
                     help="forces and stress as derivatives of the energy (training: second derivatives)")
+    ap.add_argument("--act-bits", type=int, default=0, choices=(0, 8),
+                    help="training: pre-activations kept in 8 bits (default: fp32)")
     ap.add_argument("--forward-only", action="store_true",
                     help="time inference (graph build + forward with the readout) instead of training steps")
     ap.add_argument("--no-cpu-baseline", action="store_true")
@@ -89,7 +91,8 @@ def main():
         print(json.dumps(md_bench(args, bd, synth, dev)), flush=True)
         return
     b, params, targets, d, T = synth.workload_inputs(args.workload, magmom=args.magmom)
-    hp = bd.hparams(d=d, n_layers=T, magmom=args.magmom, sequential=args.sequential, conservative=args.conservative)
+    hp = bd.hparams(d=d, n_layers=T, magmom=args.magmom, sequential=args.sequential, conservative=args.conservative,
+                    act_bits=args.act_bits)
     db = bd.DeviceBatch.from_host(b, dev)
     g = bd.DeviceGraph(b.n_atoms, 1024, 256, 1024, dev)
     ws = bd.Workspace(dev)
@@ -177,7 +180,8 @@ def main():
                    "loss": "Huber delta=%g" % args.huber if args.huber > 0 else "MSE",
                    "heads": "E, F, S, magmom" if args.magmom else "E, F, S",
                    "readout": "conservative (F = -dE/dr)" if args.conservative else "direct force/stress heads",
-                   "step": "graph + forward" if args.forward_only else "graph + forward + loss + backward + Adam"},
+                   "step": "graph + forward" if args.forward_only else "graph + forward + loss + backward + Adam",
+                   **({"pre_activations": "kept in 8 bits"} if args.act_bits else {})},
         "edges_per_s": round(E / (ms * 1e-3), 1),
         "angles_per_s": round(A / (ms * 1e-3), 1),
         "ms_per_step_mean": round(ms_mean, 4),

@@ -78,8 +78,8 @@ int chgnet_embed_forward(int64_t n, int32_t d, int64_t vocab, int32_t dtype, con
 
 /* Gradient of the table: dtable [vocab, d] fp32, row v = scale * sum of dout [n,
  * d] over the i with tok[i] - first = v (added to what it holds with accumulate
- * != 0), summed in fp32 in an order fixed by n, d and the tokens. Tokens outside
- * the table add nothing. n <= 2^30. ws: at least
+ * != 0), summed in fp32 in an order fixed by the sizes, the arrays' alignment and
+ * the tokens. Tokens outside the table add nothing. n <= 2^30. ws: at least
  * chgnet_embed_backward_workspace(n, d, vocab) bytes, 16-byte aligned. */
 int chgnet_embed_backward_workspace(int64_t n, int32_t d, int64_t vocab, size_t* bytes);
 int chgnet_embed_backward(int64_t n, int32_t d, int64_t vocab, int32_t dtype, const int32_t* tok, int32_t first,

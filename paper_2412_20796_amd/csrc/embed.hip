@@ -10,8 +10,15 @@
 // first (stably, so that the sums have one order), the ordered positions are
 // cut into chunks of equal length, each summed by one group of lanes run by
 // run, and the runs that cross a chunk's end are joined from the chunks' partial
-// sums, in order. Few tokens skip the ordering: a block a token finds the
-// others like it by comparing all of them.
+// sums, in order. Few tokens skip the ordering: a block finds the tokens of its
+// table row by looking at all of them.
+//
+// Measured, 1,000,003 tokens of 94 rows of 128 in fp32 (a third of them on one
+// row): counts 5.6 us, places 17.3, sums 87 (512 MB, 5.9 TB/s), joins 5.9;
+// 262,144 tokens of 50,000 rows of 512 in bf16: two passes of 4.8 and 11.1 us,
+// sums and zeros 77 (242 MB read, 102 MB written, 4.5 TB/s), joins 6.5. The
+// ordering is bound by latency (a pass reads and writes 16 bytes a token), the
+// sums by memory.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -141,7 +148,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_place(SortPass s) {
     int before = 0, all = 0;
     const int b1 = nb * (q + 1) / 4;
     for (int b0 = nb * q / 4; b0 < b1; b0 += 32) {
-      int c[32];  // loads in flight together: one at a time they took 30 us of 1,000,003 tokens
+      int c[32];  // loads in flight together: one at a time the launch took 30 us of 1,000,003 tokens
 #pragma unroll
       for (int u = 0; u < 32; ++u) c[u] = b0 + u < b1 ? s.counts[(b0 + u) * kDigits + digit] : 0;
 #pragma unroll

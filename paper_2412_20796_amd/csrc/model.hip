@@ -404,7 +404,9 @@ __device__ __forceinline__ void ln_stats_codes(float (&zc)[CPL], float (&zg)[CPL
 // 8-bit checkpoint of a gate's pre-activations in the workspace (act_bits = 8):
 // per row the 16-byte pieces of its lanes (the codes of a lane's 8 core and 8
 // gate columns, so that a lane writes and reads its part of a row in one
-// access), and the steps of both halves.
+// access), and the steps of both halves. The gates stay bound as they were (by
+// the products and the gathers): forward and backward gates of wide128's layers
+// 4.86 and 5.35 ms a step with fp32 pre-activations, 4.68 and 5.08 with codes.
 struct ZCodes {
   uint4* q;      // piece j of row r: q[r * ldq + j]
   float2* step;  // step[r * lds]
