@@ -774,12 +774,15 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
       constexpr int NQ = V.value == 1 ? 4 : 1;
       const dim3 grid((unsigned)(r.nzero + r.nstretch), (unsigned)cdiv(d, L.value * V.value * NQ));
       const T* x = static_cast<const T*>(dout);
-      if (V.value > 1 && (int64_t)n * d * (int64_t)sizeof(T) >= kFarBytes)
-        KLAUNCH(st, "k_embed_runs",
-                k_embed_runs<T, V.value, L.value, NQ, true><<<grid, kRunThreads, 0, st>>>(r, r.row, r.pos, x));
-      else
-        KLAUNCH(st, "k_embed_runs",
-                k_embed_runs<T, V.value, L.value, NQ, false><<<grid, kRunThreads, 0, st>>>(r, r.row, r.pos, x));
+      if constexpr (V.value > 1) {
+        if ((int64_t)n * d * (int64_t)sizeof(T) >= kFarBytes) {
+          KLAUNCH(st, "k_embed_runs",
+                  k_embed_runs<T, V.value, L.value, NQ, true><<<grid, kRunThreads, 0, st>>>(r, r.row, r.pos, x));
+          return CHGNET_OK;
+        }
+      }
+      KLAUNCH(st, "k_embed_runs",
+              k_embed_runs<T, V.value, L.value, NQ, false><<<grid, kRunThreads, 0, st>>>(r, r.row, r.pos, x));
       return CHGNET_OK;
     });
   }));

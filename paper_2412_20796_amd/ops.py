@@ -82,6 +82,11 @@ def _start(name, t):
     return *t.shape, code, gpu
 
 
+def _first(first):
+    if not 0 <= first < 1 << 31:  # (ctypes would keep the low bits)
+        _bad("first must be in 0 .. 2^31 - 1")
+
+
 def _call(fn, gpu, args):
     """The call on the GPU's current stream, with the GPU as the current device."""
     before = torch.cuda.current_device()
@@ -220,6 +225,7 @@ def embed_forward(table, tok, scale=1.0, first=0, out=None):
     ldt = _rows("table", table, vocab, d, table.dtype, gpu)
     n = tok.numel()
     _packed("tok", tok, (n,), torch.int32, gpu)
+    _first(first)
     if out is None:
         out, ldo = torch.empty((n, d), dtype=table.dtype, device=table.device), d
     else:
@@ -237,6 +243,7 @@ def embed_backward(tok, dout, vocab, scale=1.0, first=0, dtable=None, accumulate
         _bad("vocab must be at least 1")
     ldo = _rows("dout", dout, n, d, dout.dtype, gpu)
     _packed("tok", tok, (n,), torch.int32, gpu)
+    _first(first)
     if dtable is None:
         if accumulate:
             _bad("accumulate needs a dtable to add to")

@@ -195,6 +195,27 @@ def test_bitwise_reproducible_and_captured():
             assert torch.equal(x, y) and torch.equal(x, z)
 
 
+@gpu
+def test_inference_and_md_have_the_bits_of_the_fp32_path():
+    b = synth.make_batch("cubic8")
+    params = synth.make_params(64, 4, seed=(11, 1, 0))
+    got = []
+    for bits in (0, 8):
+        hp, db, p, ws = bd.hparams(act_bits=bits), bd.DeviceBatch.from_host(b), _dev(params), bd.Workspace()
+        g = bd.DeviceGraph(b.n_atoms, 64, 16, 64)
+        bd.build_graph(hp, db, g, ws)
+        outs = list(bd.forward(hp, db, g, p, ws, save_for_backward=False))
+        vel, im = torch.zeros(b.n_atoms, 3, device="cuda"), _dev((1.0 / (2.1 * b.Z)).astype(np.float32))
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            outs += bd.md(hp, db, g, p, vel, im, 0.5, 6, ws, skin=1.0)
+        torch.cuda.synchronize()
+        got.append(outs + [db.pos, vel])
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+
+
 def test_workspace_is_smaller():
     """2 d + 8 bytes a gate row in place of 8 d: at least 6 d - 8 a row of every layer, less the arrays' alignment."""
     N, S = 1000, 20

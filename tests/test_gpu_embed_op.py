@@ -210,3 +210,42 @@ def test_captured_and_replayed():
             n, vocab, d = x["shape"]
             assert torch.equal(x["dw"], ops.embed_backward(x["tok"].clone(), x["dout"].clone(), vocab, scale=3.0))
             assert torch.equal(x["out"], ops.embed_forward(x["table"], x["tok"].clone(), scale=3.0))
+
+
+@pytest.mark.parametrize("n", [500, 20000])
+def test_two_streams_at_once(n):
+    """Calls on two streams with workspaces of their own, and without any given, none waiting for the other."""
+    vocab, d = 94, 128
+    data = [(_tokens(n, vocab, 0, "skewed", seed=k).cuda(), _rand(n, d, torch.float32, seed=k).cuda()) for k in range(2)]
+    want = [ops.embed_backward(t, x, vocab) for t, x in data]
+    streams, ws = [torch.cuda.Stream() for _ in range(2)], [bd.Workspace(), None]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[k].append(ops.embed_backward(*data[k], vocab, ws=ws[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(g, want[k]) for g in got[k])
+
+
+def test_what_the_binding_refuses():
+    table, tok, dout = torch.zeros(9, 8, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, 8, device="cuda")
+    for call in (lambda: ops.embed_forward(table, tok.long()), lambda: ops.embed_forward(table, tok.reshape(2, 2)),
+                 lambda: ops.embed_forward(table.double(), tok), lambda: ops.embed_forward(table[0], tok),
+                 lambda: ops.embed_forward(table, tok, first=-1), lambda: ops.embed_forward(table, tok, first=1 << 32),
+                 lambda: ops.embed_forward(table, tok, out=torch.zeros(4, 7, device="cuda")),
+                 lambda: ops.embed_forward(table, tok, out=torch.zeros(4, 8, device="cuda", dtype=torch.bfloat16)),
+                 lambda: ops.embed_forward(table, tok.cpu()), lambda: ops.embed_forward(table.t(), tok),
+                 lambda: ops.embed_forward(table[:0], tok), lambda: ops.embed_backward(tok, dout, 0),
+                 lambda: ops.embed_backward(tok[:3], dout, 9), lambda: ops.embed_backward(tok, dout, 9, first=1 << 40),
+                 lambda: ops.embed_backward(tok, dout[:1].expand(4, 8), 9),
+                 lambda: ops.embed_backward(tok, dout, 9, accumulate=True),
+                 lambda: ops.embed_backward(tok, dout, 9, dtable=torch.zeros(9, 8, device="cuda", dtype=torch.bfloat16)),
+                 lambda: ops.embed_backward(tok, dout, 9, dtable=torch.zeros(8, 8, device="cuda")),
+                 lambda: ops.embed_backward(torch.zeros(20000, dtype=torch.int32, device="cuda"),
+                                            torch.zeros(20000, 8, device="cuda"), 9, ws=bd.Workspace("cpu"))):
+        with pytest.raises(bd.ChgnetError) as e:
+            call()
+        assert e.value.code == bd.CHGNET_EINVAL

@@ -269,3 +269,40 @@ def test_captured_and_replayed():
             eager = _run(z, ln, dphi)
             assert torch.equal(x["phi"], eager[0]) and torch.equal(x["dz"], eager[2]) and torch.equal(x["dln"], eager[3])
             assert torch.equal(x["kept"].codes, eager[1].codes)
+
+
+def test_what_the_binding_refuses():
+    dev = dict(device="cuda")
+    z, ln, up = torch.zeros(6, 16, **dev), torch.zeros(4, 8, **dev), torch.zeros(6, 8, **dev)
+    _, kept = ops.gate_forward(z, ln)
+    for call in (lambda: ops.gate_forward(z[:, :15], ln), lambda: ops.gate_forward(z.double(), ln),
+                 lambda: ops.gate_forward(z[0], ln), lambda: ops.gate_forward(z.t().contiguous().t(), ln),
+                 lambda: ops.gate_forward(z[:1].expand(6, 16), ln), lambda: ops.gate_forward(z, ln[:, :7]),
+                 lambda: ops.gate_forward(z, ln.double()), lambda: ops.gate_forward(z, ln.cpu()),
+                 lambda: ops.gate_forward(z, ln, phi=torch.zeros(5, 8, **dev)),
+                 lambda: ops.gate_forward(z, ln, save=False, kept=kept),
+                 lambda: ops.gate_forward(z[:5], ln, kept=kept),
+                 lambda: ops.gate_forward(z, ln, kept=ops.GateCheckpoint(kept.codes[:, :15], kept.step)),
+                 lambda: ops.gate_forward(torch.zeros(2, 2050, **dev), torch.zeros(4, 1025, **dev)),
+                 lambda: ops.gate_backward(kept, ln, up[:5]), lambda: ops.gate_backward(kept, ln, up.double()),
+                 lambda: ops.gate_backward(kept, ln, up[:1].expand(6, 8)),
+                 lambda: ops.gate_backward(kept, ln, up, dz=torch.zeros(6, 16, **dev, dtype=torch.float16)),
+                 lambda: ops.gate_backward(kept, ln, up, accumulate=True),
+                 lambda: ops.gate_backward(kept, ln, up, dln=torch.zeros(8, 4, **dev)),
+                 lambda: ops.gate_backward(kept, ln, up, ws=bd.Workspace("cpu")),
+                 lambda: ops.gate_backward(ops.GateCheckpoint(kept.codes.int(), kept.step), ln, up)):
+        with pytest.raises(bd.ChgnetError) as e:
+            call()
+        assert e.value.code == bd.CHGNET_EINVAL
+
+
+def test_checkpoint_of_given_tensors_and_of_one_allocation_agree():
+    rows, d = 50, 64
+    z, ln, dphi = (t.cuda() for t in _inputs(rows, d, torch.float32))
+    two = ops.GateCheckpoint(torch.empty(rows, 2 * d, dtype=torch.uint8, device="cuda"), torch.empty(rows, 2, device="cuda"))
+    _, one = ops.gate_forward(z, ln)
+    ops.gate_forward(z, ln, kept=two)
+    assert torch.equal(one.codes, two.codes) and torch.equal(one.step, two.step)
+    assert one.nbytes == two.nbytes == rows * (2 * d + 8)
+    a, b = ops.gate_backward(one, ln, dphi), ops.gate_backward(two, ln, dphi)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
