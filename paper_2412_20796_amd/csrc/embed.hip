@@ -579,16 +579,6 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int voc
   }
 }
 
-// Whether a call whose blocks take `cols` columns each is the one launch: what
-// its blocks look at must stay small, and so must the rows of a frequent token,
-// which one block adds up alone. Of 94 table rows, with tokens evenly spread and
-// with a third of them on one row, against the ordering's four launches, us a
-// call: 16,384 of 64 fp32 11 and 19 (20 and 22), 12,000 of 128 7 and 18 (18 and
-// 19), 16,384 of 128 11 and 29, 8,192 of 512 9 and 26 (17 and 18).
-bool few_tokens(int64_t n, int cols, int64_t vocab) {
-  return n <= kFewTokens && std::min(n, vocab) * n <= (1 << 21) && n * cols <= 3 << 19;
-}
-
 // Values a lane: 16 bytes of the type, 4 values of 16 bits where 8 do not fit
 // the alignment, else 1. Lanes a row: the fewest of 16, 32 and 64 that hold d
 // values (64 lanes take further columns in turn).
@@ -619,6 +609,18 @@ int with_lanes(int d, int vec, F&& f) {
   return f(integral_constant<int, 4>{}, integral_constant<int, 64>{});
 }
 
+// Whether a call of this layout takes the one launch: what its blocks look at
+// must stay small, and so must the rows of a frequent token, which the groups of
+// lanes of one block add up alone. Of 94 table rows, with tokens evenly spread
+// and with a third of them on one row, against the ordering's four launches, us
+// a call: 16,384 of 64 fp32 11 and 19 (20 and 22), 12,000 of 128 7 and 18 (18
+// and 19), 16,384 of 128 11 and 29, 8,192 of 512 9 and 26 (17 and 18); 5,389 of
+// 627 fp16, one value a lane and ten blocks a row, 40 on one row (20).
+bool few_tokens(int64_t n, int64_t vocab, int64_t tiles, int lanes, int vec) {
+  return n <= kFewTokens && std::min(n, vocab) * n * tiles <= (1 << 21) && n * lanes * std::max(vec, 4) <= 3 << 19;
+}
+int64_t tiles_of(int32_t d, int vec) { return cdiv(d, (int64_t)lanes_of(d, vec) * vec); }
+
 int check_embed(const char* who, int64_t n, int32_t d, int64_t vocab, int32_t dtype, int32_t first) {
   const std::string w(who);
   if (n < 0) return fail(CHGNET_EINVAL, w + ": n is negative");
@@ -643,7 +645,10 @@ struct EmbedWs {
   float* part;
 };
 void carve_embed(Arena& ar, int64_t n, int32_t d, int64_t vocab, EmbedWs& w) {
-  if (few_tokens(n, std::min(d, 512), vocab)) return;  // whichever columns the call's blocks take
+  // (none for the one launch, if it is taken whichever layout the alignment allows)
+  bool few = true;
+  for (int vec : {1, 4, 8}) few = few && few_tokens(n, vocab, tiles_of(d, vec), lanes_of(d, vec), vec);
+  if (few) return;
   for (int k = 0; k < 2; ++k) {
     w.row[k] = ar.take<int>(n);
     w.pos[k] = ar.take<int>(n);
@@ -705,7 +710,7 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
   const int n = (int)n64, vocab = (int)vocab64;
   const int add = accumulate != 0;
   const int vec = vec_of(dtype, d, ldo, ldw, dout, dtable, 4);
-  if (few_tokens(n, std::min(d, lanes_of(d, vec) * vec), vocab)) {
+  if (few_tokens(n, vocab, tiles_of(d, vec), lanes_of(d, vec), vec)) {
     if (n == 0 && add) return CHGNET_OK;
     const bool by_row = vocab <= n;
     const unsigned blocks = (unsigned)(by_row ? vocab : n + (add ? 0 : std::min<int64_t>(4096, cdiv(vocab, kFewZeroRows))));
