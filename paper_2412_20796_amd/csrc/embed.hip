@@ -609,15 +609,20 @@ int with_lanes(int d, int vec, F&& f) {
   return f(integral_constant<int, 4>{}, integral_constant<int, 64>{});
 }
 
-// Whether a call of this layout takes the one launch: what its blocks look at
-// must stay small, and so must the rows of a frequent token, which the groups of
-// lanes of one block add up alone. Of 94 table rows, with tokens evenly spread
-// and with a third of them on one row, against the ordering's four launches, us
-// a call: 16,384 of 64 fp32 11 and 19 (20 and 22), 12,000 of 128 7 and 18 (18
-// and 19), 16,384 of 128 11 and 29, 8,192 of 512 9 and 26 (17 and 18); 5,389 of
-// 627 fp16, one value a lane and ten blocks a row, 40 on one row (20).
+// Whether a call of this layout takes the one launch: the tokens that its blocks
+// look at must stay few (fewer where blocks by token do it, most of which find
+// that they are not the first of their kind), and so must the rows of a frequent
+// token, which the groups of lanes of one block add up alone. With tokens evenly
+// spread and with a third of them on one row, against the ordering's four or six
+// launches, us a call: of 94 rows 16,384 of 64 fp32 11 and 19 (20 and 22), 12,000
+// of 128 7 and 18 (18 and 19), 16,384 of 128 11 and 29 (18 and 20), 8,192 of 512
+// 9 and 26 (18 and 19); 8,000 of 1,000 rows of 64 20 and 21 (31 and 30); by token
+// 2,000 of 5,000 rows of 64 16 and 15 (27 and 29), of 50,000 rows of 512 in bf16
+// 44 and 41 (37 and 38).
 bool few_tokens(int64_t n, int64_t vocab, int64_t tiles, int lanes, int vec) {
-  return n <= kFewTokens && std::min(n, vocab) * n * tiles <= (1 << 21) && n * lanes * std::max(vec, 4) <= 3 << 19;
+  if (n > kFewTokens) return false;
+  const int64_t looks = (vocab <= n ? vocab : n + cdiv(vocab, kFewZeroRows)) * n * tiles;
+  return looks <= (vocab <= n ? 1 << 23 : 1 << 22) && n * lanes * std::max(vec, 4) <= 3 << 19;
 }
 int64_t tiles_of(int32_t d, int vec) { return cdiv(d, (int64_t)lanes_of(d, vec) * vec); }
 

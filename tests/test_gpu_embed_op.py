@@ -76,13 +76,14 @@ def test_lookup_strides():
             assert bool((out[37:] == 7).all()) and bool((out[:, d:] == 7).all())
 
 
-# sizes below and above the switch to the ordering (16,384 tokens, 2^21 tokens looked at), around its stretches of 1,024
-# tokens a block, its chunks of 16 and more, digits of one to three passes, widths of one and several column blocks
+# sizes below and above the switches to the ordering (16,384 tokens; 2^23 tokens looked at by row: 8,388 of 1,000 rows, and
+# 2^22 by token: 2,023 of 3,000 rows; lanes: 12,288 of 128), around its stretches of 1,024 tokens a block, its chunks of 16 and more, digits of one to three passes, widths of one and several column blocks
 @pytest.mark.parametrize("how", ["random", "one", "two ends", "in order", "outside", "none", "skewed"])
 @pytest.mark.parametrize("n,vocab,d", [(1, 1, 1), (1, 94, 64), (63, 94, 64), (513, 94, 128), (1023, 3000, 20),
                                        (1024, 94, 128), (1025, 94, 128), (1040, 1, 64), (2047, 2, 64), (2048, 255, 130),
                                        (2049, 256, 65), (5844, 94, 128), (16384, 128, 64), (16384, 129, 64),
-                                       (16385, 94, 64), (16383, 94, 130), (9999, 70000, 33), (16400, 300, 512),
+                                       (16385, 94, 64), (16383, 94, 130), (8388, 1000, 64), (8389, 1000, 64),
+                                       (2023, 3000, 64), (2060, 3000, 64), (12288, 94, 128), (12289, 94, 128), (9999, 70000, 33), (16400, 300, 512),
                                        (40000, 1000, 9), (300007, 94, 64)])
 def test_gradient(n, vocab, d, how):
     first = n % 2
