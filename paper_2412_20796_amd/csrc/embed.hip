@@ -86,10 +86,11 @@ __global__ void __launch_bounds__(256) k_embed_fwd(int64_t n, int d, int vocab, 
 // ---------------------------------------------------------------------------
 // Ordering of the positions by table row: passes over digits of at most 8 bits,
 // least significant first, each stable. A pass is two launches over at most
-// kSortBlocks blocks, each with a contiguous stretch of the tokens: the counts of every digit in every stretch, then the places. A
-// block of the second launch adds up the counts of the stretches before its own
-// and of the lower digits itself (at most 256 x 256 numbers, in L2), so that no
-// scan stands between the two.
+// kSortBlocks blocks, each with a contiguous stretch of the tokens: the counts of
+// every digit in every stretch, then the places. A block of the second launch
+// adds up the counts of the stretches before its own and of the lower digits
+// itself (at most 256 x 256 numbers, in L2), so that no scan stands between the
+// two.
 // ---------------------------------------------------------------------------
 constexpr int kSortBlocks = 256, kSortThreads = 1024, kDigits = 256;
 
@@ -243,8 +244,9 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_place(SortPass s) {
 // goes on. The block then joins its chunks' partial sums in order, and what
 // crosses the block's stretch is one partial row of slot 0 and one of slot 1 in
 // the workspace. FAR: the rows, each read once, are loaded past the caches
-// (1,000,003 rows of 128 in fp32: 126 -> 114 us the whole gradient). The launch's first `nzero` blocks look up 512 table rows each
-// among the ordered ones and write the zeros of those that no token has.
+// (1,000,003 rows of 128 in fp32: 126 -> 114 us the whole gradient). The launch's
+// first `nzero` blocks look up 512 table rows each among the ordered ones and
+// write the zeros of those that no token has.
 // ---------------------------------------------------------------------------
 struct RunSums {
   int n, vocab, chunk, stretch, nstretch, d;  // stretch: positions of a block
@@ -575,7 +577,7 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int d, int voc
     float sum = red[0][t];
     for (int k = 1; k < groups; ++k) sum += red[k][t];
     float* w = dw + v * ldw + c0 + t;
-    *w = add ? *w + scale * sum : scale * sum;
+    *w = add ? *w + scale * sum : m ? scale * sum : 0.f;
   }
 }
 

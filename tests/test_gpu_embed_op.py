@@ -250,3 +250,13 @@ def test_what_the_binding_refuses():
         with pytest.raises(bd.ChgnetError) as e:
             call()
         assert e.value.code == bd.CHGNET_EINVAL
+
+
+@pytest.mark.parametrize("n,vocab", [(300, 94), (300, 5000), (20000, 94), (20000, 70000)])
+def test_rows_without_a_token_are_zero_at_any_scale(n, vocab):
+    tok = _tokens(n, vocab, 0, "one").cuda()
+    for scale in (-1.0, float("inf")):
+        dw = ops.embed_backward(tok, torch.ones(n, 64, device="cuda"), vocab, scale=scale)
+        assert bool((dw[vocab // 2] == scale * n).all())
+        dw[vocab // 2] = 0
+        assert torch.equal(dw.view(torch.int32), torch.zeros_like(dw).view(torch.int32))  # and no negative zeros
