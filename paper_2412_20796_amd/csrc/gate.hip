@@ -17,10 +17,10 @@
 // Measured (kernel time, bytes that the pass cannot do without over it): 397,934
 // rows of 128 in fp32 forward 102 to 116 us (6.2 to 7.0 TB/s), without the
 // checkpoint 104 (5.9), backward 120 to 137 (5.2 to 5.9), where a copy of as much
-// reaches 4.7 TB/s; 85,274 rows of 64 14.6 and 17.7 us (5.3 and 4.4). Both are
+// reaches 4.7 TB/s; 85,274 rows of 64 14.6 and 17.8 us (5.3 and 4.3). Both are
 // bound by memory there, with the vector units busy 56 to 66 % of the time. Rows
-// that allow no vector loads are bound by the instructions of their single-value
-// accesses: 20,011 rows of 333 in bf16 20 and 26 us (2.6 and 2.0 TB/s).
+// of 16-bit values that allow no vector loads are as busy on half the bytes, and
+// bound by that: 20,011 rows of 333 in bf16 20 and 26 us (2.7 and 2.1 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
