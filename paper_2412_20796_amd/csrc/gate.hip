@@ -198,8 +198,7 @@ __global__ void __launch_bounds__(kBwdThreads) k_gate_act_bwd(int64_t rows, int 
   d = cols.d;
   const float inv_d = cols.inv_d;
   // LayerNorm parameters in registers; at 16 columns a lane with an end to look
-  // for, where there is no
-  // room for them (70 registers spilled), in LDS
+  // for, where there is no room for them (70 registers spilled), in LDS
   constexpr bool kLnInLds = CPL == 16 && !FULL;
   __shared__ float lnS[kLnInLds ? 4 * VEC * LPR * NQ : 1];
   float gc[CPL], bc[CPL], gg[CPL], bg[CPL];

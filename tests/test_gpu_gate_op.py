@@ -172,6 +172,27 @@ def test_large_and_small_values():
         ref.assert_within(dz, rz, bz, what="scale %g" % scale)
 
 
+@pytest.mark.parametrize("d", [64, 70, 600])
+@pytest.mark.parametrize("size", [1e21, 1e30])
+def test_variance_past_the_range(size, d):
+    """A core whose variance is infinite in fp32 counts as all at its mean, and no gradient passes it."""
+    rows = 37
+    z, ln, dphi = _inputs(rows, d, torch.float32)
+    z[:, :d] *= size
+    mid = z.clone()
+    mid[:, :d] = 0
+    phi, kept, dz, dln = _run(z, ln, dphi)
+    q, step, _ = ref.checkpoint(z)
+    assert torch.equal(kept.codes.cpu().double(), q) and torch.equal(kept.step.cpu().double(), step)
+    r, b = ref.gate(mid, ln)
+    ref.assert_within(phi, r, b)
+    q[:, :d] = 0
+    rz, rl, bz, bl = ref.gate_grad(q, step, ln, dphi)
+    assert (dz[:, :d] == 0).all() and (dln[0] == 0).all()
+    ref.assert_within(dz[:, d:], rz[:, d:], bz[:, d:])
+    ref.assert_within(dln, rl, bl)
+
+
 @pytest.mark.parametrize("d", [64, 128, 70])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 def test_values_that_are_not_finite(value, d):
