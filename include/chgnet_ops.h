@@ -43,9 +43,10 @@ extern "C" {
  * they follow each other in the flat parameter vector:
  *   phi = SiLU(LN(core) g_c + b_c) * sigmoid(LN(gate) g_g + b_g)   [rows, d]
  * with LN(x) = (x - mean) / sqrt(var + 1e-5) over the row's d values, mean and
- * variance in fp32: where the variance passes fp32's range (values some 1e19
- * apart) LN(x) is 0 and no gradient passes it, where the sum of the values does
- * (about 1e35) phi is NaN. 1 <= d <= 1024.
+ * variance in fp32. Where the variance passes fp32's range (a deviation of 1.8e19)
+ * LN(x) is 0 and no gradient passes it, in both passes. The mean is off by its
+ * rounding: values far from zero for their deviation (or that of 1e-5) have an
+ * LN(x) that is off by some 1e-7 of their ratio. 1 <= d <= 1024.
  *
  * With codes != NULL also the checkpoint for chgnet_gate_backward: codes
  * [rows, 2d] bytes and step [rows, 2] fp32 (8-byte aligned). For each half x of

@@ -33,6 +33,26 @@
 namespace chg {
 namespace {
 
+// Powers of two that keep the sums over a row of d values in fp32's range wherever
+// its mean and variance are: values are summed as x 2^-l and squares as ((x - mean)
+// 2^-h)^2, with the least l and h of 2^l >= d and 4^h >= d. (Without them the sum of
+// squares passes the range at a variance d times smaller, where the backward pass,
+// which sums squares of codes, does not. They take 0.5 of 16 us in bf16 rows of
+// 64, whose vector units are the busiest, and 0.2 at most elsewhere. A path of its
+// own for such rows took up to 5 of 22 us of all, for its registers.)
+struct Scale {
+  float sum, mean, dev, var, up;  // 2^-l, 2^(l - h) / d, 2^-h, 4^h / d, 2^h
+  __device__ __forceinline__ Scale(int d, float inv_d) {
+    const int l = 31 - __builtin_clz(2 * d - 1), h = (l + 1) / 2;
+    auto pow2 = [](int e) { return __int_as_float((127 + e) << 23); };
+    sum = pow2(-l);
+    mean = inv_d * pow2(l - h);
+    dev = pow2(-h);
+    var = inv_d * pow2(2 * h);
+    up = pow2(h);
+  }
+};
+
 // Row of d values in LPR lanes: lane j holds the NQ groups of VEC values at
 // columns (q LPR + j) VEC. MIN: d is greater, so that only the groups past it
 // are looked at for their end; FULL: d is exactly the LPR VEC NQ columns.
@@ -79,8 +99,27 @@ struct Cols {
 #pragma unroll
       for (int k = 0; k < VEC; ++k) v[q * VEC + k] = has(q) ? p[col(q) + k] : 0.f;
   }
-  // x - mean in place (0 in columns past d), and 1 / deviation of x * unit
-  __device__ __forceinline__ float center(float (&x)[CPL], float unit) const {
+  // (x - mean) 2^-h in place (0 in columns past d), and 1 / deviation of x
+  __device__ __forceinline__ float center(float (&x)[CPL], const Scale& sc) const {
+    float s = x[0] * sc.sum;
+#pragma unroll
+    for (int k = 1; k < CPL; ++k) s = fmaf(x[k], sc.sum, s);
+    const float m = rowsum<LPR>(s) * sc.mean;
+    float v = 0.f;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        float& y = x[q * VEC + k];
+        y = has(q) ? fmaf(y, sc.dev, -m) : 0.f;
+        v += y * y;
+      }
+    // at least the LayerNorm epsilon: no denormal argument
+    return __builtin_amdgcn_rsqf(rowsum<LPR>(v) * sc.var + kLnEps);
+  }
+  // x - mean in place (0 in columns past d), and 1 / deviation of x * unit, for
+  // codes x: what passes fp32's range is the variance alone, in unit^2
+  __device__ __forceinline__ float center_codes(float (&x)[CPL], float unit) const {
     float s = 0.f;
 #pragma unroll
     for (int k = 0; k < CPL; ++k) s += x[k];
@@ -94,7 +133,6 @@ struct Cols {
         y = has(q) ? y - m : 0.f;
         v += y * y;
       }
-    // at least the LayerNorm epsilon: no denormal argument
     return __builtin_amdgcn_rsqf(rowsum<LPR>(v) * inv_d * (unit * unit) + kLnEps);
   }
 };
@@ -114,6 +152,12 @@ __global__ void __launch_bounds__(256) k_gate_act_fwd(int64_t rows, int d, const
   cols.load_any(ln + d, bc);
   cols.load_any(ln + 2 * d, gg);
   cols.load_any(ln + 3 * d, bg);
+  const Scale sc(d, cols.inv_d);
+#pragma unroll
+  for (int k = 0; k < CPL; ++k) {  // (of rows in 2^-h)
+    gc[k] *= sc.up;
+    gg[k] *= sc.up;
+  }
   const int64_t stride = (int64_t)gridDim.x * 4 * C::RPW;
   int64_t row = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * C::RPW + lane / LPR;
   float nc[CPL], ng[CPL];
@@ -162,7 +206,7 @@ __global__ void __launch_bounds__(256) k_gate_act_fwd(int64_t rows, int d, const
       }
       if (cols.j == 0) step[row] = st;
     }
-    const float rc = cols.center(xc, 1.f), rg = cols.center(xg, 1.f);
+    const float rc = cols.center(xc, sc), rg = cols.center(xg, sc);
     float o[CPL];
 #pragma unroll
     for (int k = 0; k < CPL; ++k) {
@@ -280,7 +324,7 @@ __global__ void __launch_bounds__(kBwdThreads) k_gate_act_bwd(int64_t rows, int 
           bg[q * VEC + k] = p[3 * VEC * LPR * NQ];
         }
     }
-    const float rc = cols.center(xc, uc), rg = cols.center(xg, ug);
+    const float rc = cols.center_codes(xc, uc), rg = cols.center_codes(xg, ug);
     const float fc = uc * rc, fg = ug * rg;
     float s1c = 0.f, s2c = 0.f, s1g = 0.f, s2g = 0.f;
     float dyc[CPL], dyg[CPL];
