@@ -372,7 +372,9 @@ __device__ __forceinline__ void ln_stats(float (&zc)[CPL], float (&zg)[CPL], flo
 
 // The same from the codes of a row's 8-bit checkpoint (rowops.hpp), in zc and zg:
 // the least value that they count from drops out with the mean, and their sums
-// are exact.
+// are exact. The sum of squares is scaled before it is divided by D, so that it
+// passes fp32's range where the forward pass's (ln_stats) did and the row counts
+// as all at its mean in both.
 template <int D, int CPL>
 __device__ __forceinline__ void ln_stats_codes(float (&zc)[CPL], float (&zg)[CPL], float2 step, float& rc, float& rg) {
   constexpr int LPR = Lanes<D, CPL>::LPR;
@@ -391,8 +393,8 @@ __device__ __forceinline__ void ln_stats_codes(float (&zc)[CPL], float (&zg)[CPL
     vc += zc[k] * zc[k];
     vg += zg[k] * zg[k];
   }
-  rc = __builtin_amdgcn_rsqf(rowsum<LPR>(vc) * (1.0f / D) * (step.x * step.x) + kLnEps);
-  rg = __builtin_amdgcn_rsqf(rowsum<LPR>(vg) * (1.0f / D) * (step.y * step.y) + kLnEps);
+  rc = __builtin_amdgcn_rsqf(rowsum<LPR>(vc) * (step.x * step.x) * (1.0f / D) + kLnEps);
+  rg = __builtin_amdgcn_rsqf(rowsum<LPR>(vg) * (step.y * step.y) * (1.0f / D) + kLnEps);
   const float fc = rc * step.x, fg = rg * step.y;
 #pragma unroll
   for (int k = 0; k < CPL; ++k) {
