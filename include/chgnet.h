@@ -68,7 +68,7 @@ typedef struct {
                          update read layer-t features); 1: the reference
                          block of Eq. 10 (bond conv reads v^{t+1}, angle
                          update reads v^{t+1} and e^{t+1})                  */
-  int32_t conservative; /* 1: forces and stress as derivatives of the energy,
+  int16_t conservative; /* 1: forces and stress as derivatives of the energy,
                          F_i = -dE/dr_i, sigma = (1/V) dE/d(eps) for the
                          strain r -> (I + eps) r of positions and lattice
                          (the reference output layer, Sec. II-B (4)); the
@@ -81,7 +81,7 @@ typedef struct {
                          numbers), with either block. The workspace then
                          holds the dual-number buffers
                          as well (chgnet_workspace_size includes them).     */
-  int32_t act_bits;   /* 0: the gates' pre-activations, most of what a
+  int16_t act_bits;   /* 0: the gates' pre-activations, most of what a
                          forward pass keeps for the backward pass, are kept
                          in fp32; 8: in 8 bits, each half row in steps of
                          (max - min) / 255 (the checkpoint of chgnet_ops.h),
@@ -89,7 +89,10 @@ typedef struct {
                          forces, stresses and the loss are the same bits; the
                          gates' derivatives are those at the kept values.
                          The same value for every call on a workspace. Not
-                         with the conservative readout.                      */
+                         with the conservative readout. (It and the field
+                         before it share 32 bits that held `conservative`
+                         alone: what was built before act_bits passes 0
+                         there.)                                             */
 } chgnet_hparams;
 
 /* Loss of chgnet_step (Sec. IV, "Parameters Setting"), host memory. Each term

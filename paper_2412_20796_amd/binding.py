@@ -33,7 +33,7 @@ class HParams(ctypes.Structure):
     _fields_ = [("d", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("n_rbf", ctypes.c_int32),
                 ("n_fourier", ctypes.c_int32), ("envelope_p", ctypes.c_int32), ("r_atom", ctypes.c_float),
                 ("r_bond", ctypes.c_float), ("magmom", ctypes.c_int32), ("sequential", ctypes.c_int32),
-                ("conservative", ctypes.c_int32), ("act_bits", ctypes.c_int32)]
+                ("conservative", ctypes.c_int16), ("act_bits", ctypes.c_int16)]
 
 
 class LossCfg(ctypes.Structure):
@@ -103,6 +103,8 @@ def _check(code):
 
 def hparams(d=64, n_layers=4, n_rbf=31, n_fourier=31, envelope_p=8, r_atom=6.0, r_bond=3.0, magmom=False,
             sequential=False, conservative=False, act_bits=0) -> HParams:
+    if not all(-(1 << 15) <= x < 1 << 15 for x in (conservative, act_bits)):  # (ctypes would keep the low bits)
+        raise ChgnetError(CHGNET_EINVAL, "conservative must be 0 or 1 and act_bits 0 or 8")
     return HParams(d, n_layers, n_rbf, n_fourier, envelope_p, r_atom, r_bond, int(magmom), int(sequential),
                    int(conservative), act_bits)
 

@@ -79,6 +79,9 @@ int fail(int code, const std::string& msg) {
   return code;
 }
 
+// (a longer struct would be read past the end of an older caller's)
+static_assert(sizeof(chgnet_hparams) == 40, "chgnet_hparams keeps its size");
+
 int validate_hparams(const chgnet_hparams* hp) {
   if (!hp) return fail(CHGNET_EINVAL, "hparams is NULL");
   if (hp->d != 64 && hp->d != 128) return fail(CHGNET_EINVAL, "d must be 64 or 128");
