@@ -222,20 +222,42 @@ class DeviceGraph:
         return dg
 
 
+def _capturing(buf):
+    """Whether a call on buf's GPU is being captured into a graph."""
+    if not buf.is_cuda:
+        return False
+    if torch._C._cuda_getDevice() == buf.get_device():
+        return torch._C._cuda_isCurrentStreamCapturing()
+    with torch.cuda.device(buf.device):
+        return torch._C._cuda_isCurrentStreamCapturing()
+
+
 class Workspace:
-    """Caller-owned scratch buffer, grown on demand."""
+    """Caller-owned scratch buffer, grown on demand. A buffer that a captured call was given is kept as long as the
+    Workspace: each replay writes to it, and its memory must not go to other tensors once the buffer is outgrown."""
 
     def __init__(self, device="cuda"):
         self.device = device
         self.buf = None
+        self._in_graph = False
+        self._graph_bufs = []
 
     def ensure(self, nbytes):
         if self.buf is None or self.buf.numel() < nbytes:
+            if self._in_graph:
+                self._graph_bufs.append(self.buf)
+                self._in_graph = False
             self.buf = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device)
+        self._mark()
         return self.buf
+
+    def _mark(self):
+        if not self._in_graph:
+            self._in_graph = _capturing(self.buf)
 
     @property
     def ptr(self):
+        self._mark()
         return ctypes.c_void_p(self.buf.data_ptr())
 
     @property
