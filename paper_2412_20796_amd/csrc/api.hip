@@ -41,7 +41,7 @@ int embed_forward_entry(int64_t n, int32_t d, int64_t vocab, int32_t dtype, cons
 int embed_backward_workspace_entry(int64_t n, int32_t d, int64_t vocab, size_t* bytes);
 int embed_backward_entry(int64_t n, int32_t d, int64_t vocab, int32_t dtype, const int32_t* tok, int32_t first,
                          const void* dout, int64_t lddout, float scale, float* dtable, int64_t lddtable,
-                         int accumulate, void* ws, size_t ws_bytes, hipStream_t st);
+                         int accumulate, void* ws, size_t ws_bytes, hipStream_t st, const char* tag = nullptr);
 
 namespace {
 thread_local std::string g_last_error;

@@ -704,9 +704,10 @@ int embed_backward_workspace_entry(int64_t n, int32_t d, int64_t vocab, size_t* 
   return CHGNET_OK;
 }
 
+// tag: the launches' name in a profile, in place of their own
 int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype, const int32_t* tok, int32_t first,
                          const void* dout, int64_t ldo, float scale, float* dtable, int64_t ldw, int accumulate,
-                         void* ws, size_t ws_bytes, hipStream_t st) {
+                         void* ws, size_t ws_bytes, hipStream_t st, const char* tag) {
   CHG_TRY(check_embed("embed_backward", n64, d, vocab64, dtype, first));
   if (n64 > kMaxTokens) return fail(CHGNET_EINVAL, "embed_backward: n must be at most 2^30");
   if (ldo < d || ldw < d) return fail(CHGNET_EINVAL, "embed_backward: a row stride is below the row's width");
@@ -724,7 +725,7 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
     return with_type(dtype, [&](auto t) {
       using T = decltype(t);
       return with_lanes<T>(d, vec, [&](auto V, auto L) -> int {
-        KLAUNCH(st, "k_embed_few",
+        KLAUNCH(st, tag ? tag : "k_embed_few",
                 k_embed_few<T, V.value, L.value><<<dim3(blocks, (unsigned)cdiv(d, L.value * V.value)), kFewThreads, 0, st>>>(
                     n, d, vocab, tok, first, static_cast<const T*>(dout), ldo, scale, dtable, ldw, add, by_row));
         return CHGNET_OK;
@@ -760,9 +761,9 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
     s.pos = w.pos[(p + 1) & 1];
     s.row_out = w.row[p & 1];
     s.pos_out = w.pos[p & 1];
-    KLAUNCH(st, "k_embed_count", k_embed_count<<<nb, kSortThreads, 0, st>>>(s));
-    if (rounds == 1) KLAUNCH(st, "k_embed_place", k_embed_place<1><<<nb, kSortThreads, 0, st>>>(s));
-    else KLAUNCH(st, "k_embed_place", k_embed_place<4><<<nb, kSortThreads, 0, st>>>(s));
+    KLAUNCH(st, tag ? tag : "k_embed_count", k_embed_count<<<nb, kSortThreads, 0, st>>>(s));
+    if (rounds == 1) KLAUNCH(st, tag ? tag : "k_embed_place", k_embed_place<1><<<nb, kSortThreads, 0, st>>>(s));
+    else KLAUNCH(st, tag ? tag : "k_embed_place", k_embed_place<4><<<nb, kSortThreads, 0, st>>>(s));
   }
   RunSums r{};
   r.n = n;
@@ -788,12 +789,12 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
       const T* x = static_cast<const T*>(dout);
       if constexpr (V.value > 1) {
         if ((int64_t)n * d * (int64_t)sizeof(T) >= kFarBytes) {
-          KLAUNCH(st, "k_embed_runs",
+          KLAUNCH(st, tag ? tag : "k_embed_runs",
                   k_embed_runs<T, V.value, L.value, NQ, true><<<grid, kRunThreads, 0, st>>>(r, r.row, r.pos, x));
           return CHGNET_OK;
         }
       }
-      KLAUNCH(st, "k_embed_runs",
+      KLAUNCH(st, tag ? tag : "k_embed_runs",
               k_embed_runs<T, V.value, L.value, NQ, false><<<grid, kRunThreads, 0, st>>>(r, r.row, r.pos, x));
       return CHGNET_OK;
     });
@@ -803,8 +804,8 @@ int embed_backward_entry(int64_t n64, int32_t d, int64_t vocab64, int32_t dtype,
     const int v = d % 4 == 0 ? 4 : 1;
     int lanes = 16;
     while (lanes < kJoinThreads && lanes * v < d) lanes *= 2;
-    if (v == 4) KLAUNCH(st, "k_embed_join", k_embed_join<4><<<r.nstretch - 1, kJoinThreads, 0, st>>>(r, lanes));
-    else KLAUNCH(st, "k_embed_join", k_embed_join<1><<<r.nstretch - 1, kJoinThreads, 0, st>>>(r, lanes));
+    if (v == 4) KLAUNCH(st, tag ? tag : "k_embed_join", k_embed_join<4><<<r.nstretch - 1, kJoinThreads, 0, st>>>(r, lanes));
+    else KLAUNCH(st, tag ? tag : "k_embed_join", k_embed_join<1><<<r.nstretch - 1, kJoinThreads, 0, st>>>(r, lanes));
   }
   return CHGNET_OK;
 }

@@ -33,7 +33,7 @@ int validate_batch(const chgnet_batch* b);
 size_t embed_backward_bytes(int64_t n, int32_t d, int64_t vocab);
 int embed_backward_entry(int64_t n, int32_t d, int64_t vocab, int32_t dtype, const int32_t* tok, int32_t first,
                          const void* dout, int64_t lddout, float scale, float* dtable, int64_t lddtable,
-                         int accumulate, void* ws, size_t ws_bytes, hipStream_t st);
+                         int accumulate, void* ws, size_t ws_bytes, hipStream_t st, const char* tag);
 
 namespace {
 
@@ -3514,7 +3514,7 @@ int element_table_grad(const Ctx& c, const float* dv0, float* gWZ, const char* t
   const int64_t N = c.dm.N;
   const int D = c.dm.D;
   if (N > kEmbZAtoms)
-    return embed_backward_entry(N, D, 94, CHGNET_F32, c.batch->Z, 1, dv0, D, 1.0f, gWZ, D, 1, c.a.embz, c.a.embz_bytes, st);
+    return embed_backward_entry(N, D, 94, CHGNET_F32, c.batch->Z, 1, dv0, D, 1.0f, gWZ, D, 1, c.a.embz, c.a.embz_bytes, st, tag);
   KLAUNCH(st, tag, k_embed_bwd_Z<<<94, 64 * kEmbZWaves, 0, st>>>((int)N, D, c.batch->Z, dv0, gWZ));
   return CHGNET_OK;
 }
