@@ -6,7 +6,9 @@ Argument marshalling and checks only, as in ``binding``: torch tensors supply
 device memory and the stream (the current one of the tensors' device), and a
 missing library raises. Every tensor of a call is on one GPU; rows may have a
 stride, columns are contiguous. Inputs are not differentiated by autograd: a
-``torch.autograd.Function`` of the caller's calls the two passes.
+``torch.autograd.Function`` of the caller's calls the two passes. An input that
+autograd follows (it requires a gradient, outside ``torch.no_grad()`` and such a
+Function) is refused, since its gradient would be lost.
 
 The calls on few rows take as long as their launches, about 4 us each; the checks
 are written so that they add little to that (a dozen attribute reads).
@@ -88,6 +90,11 @@ def _start(name, t):
         _bad("%s must be on a GPU" % name)
     rows, cols = shape
     return rows, cols, dtype, code, _stride(name, t, rows, cols), gpu
+
+
+def _followed(name):
+    _bad("%s requires a gradient, which this call does not pass on: call it from a torch.autograd.Function or under "
+         "torch.no_grad()" % name)
 
 
 def _first(first):
@@ -180,6 +187,8 @@ class GateCheckpoint:
 def gate_forward(z, ln, save=True, phi=None, kept=None):
     """phi [rows, d] of z [rows, 2d] (core | gate) and ln [4, d] fp32 (g_c, b_c, g_g, b_g); z in fp32, bf16 or fp16.
     With `save` returns (phi, GateCheckpoint) for gate_backward, else phi. phi and kept: tensors to write into."""
+    if (z.requires_grad or ln.requires_grad) and torch.is_grad_enabled():
+        _followed("z or ln")
     rows, cols, dtype, code, ldz, gpu = _start("z", z)
     d = cols // 2
     if cols != 2 * d:
@@ -205,6 +214,8 @@ def gate_forward(z, ln, save=True, phi=None, kept=None):
 def gate_backward(kept, ln, dphi, dz=None, dln=None, accumulate=False, ws=None):
     """(dz [rows, 2d], dln [4, d]) from the checkpoint of gate_forward and dphi [rows, d]; dln is fp32 and added to what
     it holds with `accumulate`. ws: a Workspace of the caller's (one for each call that may run at the same time)."""
+    if (dphi.requires_grad or ln.requires_grad) and torch.is_grad_enabled():
+        _followed("dphi or ln")
     rows, d, dtype, code, ldp, gpu = _start("dphi", dphi)
     codes, step = kept._pointers(rows, d, gpu)
     _packed("ln", ln, (4, d), torch.float32, gpu)
@@ -226,6 +237,8 @@ def gate_backward(kept, ln, dphi, dz=None, dln=None, accumulate=False, ws=None):
 
 def embed_forward(table, tok, scale=1.0, first=0, out=None):
     """out [n, d] = scale * table[tok - first] for int32 tokens [n]; zeros for tokens outside the table [vocab, d]."""
+    if table.requires_grad and torch.is_grad_enabled():
+        _followed("table")
     vocab, d, dtype, code, ldt, gpu = _start("table", table)
     n = tok.numel()
     _packed("tok", tok, (n,), torch.int32, gpu)
@@ -242,6 +255,8 @@ def embed_forward(table, tok, scale=1.0, first=0, out=None):
 def embed_backward(tok, dout, vocab, scale=1.0, first=0, dtable=None, accumulate=False, ws=None):
     """dtable [vocab, d] fp32: row v = scale * the sum of dout [n, d] over the tokens with tok - first = v, added to what
     it holds with `accumulate`. ws: a Workspace of the caller's (one for each call that may run at the same time)."""
+    if dout.requires_grad and torch.is_grad_enabled():
+        _followed("dout")
     n, d, _, code, ldo, gpu = _start("dout", dout)
     if vocab < 1:
         _bad("vocab must be at least 1")
