@@ -233,14 +233,17 @@ def _capturing(buf):
 
 
 class Workspace:
-    """Caller-owned scratch buffer, grown on demand. A buffer that a captured call was given is kept as long as the
-    Workspace: each replay writes to it, and its memory must not go to other tensors once the buffer is outgrown."""
+    """Caller-owned scratch buffer, grown on demand. Once outgrown, a buffer that a captured call was given is kept as long
+    as the Workspace, since each replay writes to it; the memory of another goes to other tensors when the work of the
+    streams whose calls had it has ended."""
 
     def __init__(self, device="cuda"):
         self.device = device
         self.buf = None
+        self._gpu = None
         self._in_graph = False
         self._graph_bufs = []
+        self._streams = ()
 
     def ensure(self, nbytes):
         if self.buf is None or self.buf.numel() < nbytes:
@@ -248,12 +251,25 @@ class Workspace:
                 self._graph_bufs.append(self.buf)
                 self._in_graph = False
             self.buf = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device)
+            self._gpu = self.buf.get_device() if self.buf.is_cuda else None
+            self._streams = (self._stream(),)  # (the allocator knows of this one)
         self._mark()
         return self.buf
 
+    def _stream(self):
+        """The current stream of the buffer's GPU, as a number."""
+        return None if self._gpu is None else torch._C._cuda_getCurrentRawStream(self._gpu)
+
     def _mark(self):
-        if not self._in_graph:
-            self._in_graph = _capturing(self.buf)
+        """The buffer is about to be given to a call on the current stream."""
+        stream = self._stream()
+        # (nothing is captured on the default stream: the usual call ends here)
+        if self._in_graph or (stream == 0 and stream in self._streams):
+            return
+        self._in_graph = _capturing(self.buf)
+        if stream not in self._streams and not self._in_graph:
+            self.buf.record_stream(torch.cuda.current_stream(self.buf.device))
+            self._streams += (stream,)
 
     @property
     def ptr(self):

@@ -68,3 +68,23 @@ def test_replay_after_the_workspace_has_grown():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and all(bool((t == 7).all()) for t in others)
+
+
+@gpu
+def test_an_outgrown_buffer_waits_for_the_streams_that_had_it():
+    """A buffer made on one stream and given to a call on another: once outgrown, its memory goes to no tensor of the first
+    stream before the second one's work has ended."""
+    n = 32 << 20
+    ws, s = bd.Workspace(), torch.cuda.Stream()
+    at = ws.ensure(n).data_ptr()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(int(2e8))  # some 0.1 s, in place of a long call
+        ws.ensure(n)
+        done = torch.cuda.Event()
+        done.record()
+        ws.ensure(2 * n)
+    other = torch.empty(n, dtype=torch.uint8, device="cuda")
+    assert not done.query(), "the stream was through before the tensor was made"
+    assert other.data_ptr() != at
+    torch.cuda.synchronize()
