@@ -59,7 +59,7 @@ extern "C" {
  * half with a value that is not finite, or whose max - min is above fp32's
  * range, has a step that is not finite, and dz of its row and the LayerNorm
  * gradients are then NaN. codes == NULL (then step too): inference, nothing is
- * kept and phi has the same bits. */
+ * kept and phi has the same bits as with codes on a 4-byte boundary. */
 int chgnet_gate_forward(int64_t rows, int32_t d, int32_t dtype, const void* z, int64_t ldz, const float* ln,
                         void* phi, int64_t ldphi, uint8_t* codes, float* step, void* stream);
 

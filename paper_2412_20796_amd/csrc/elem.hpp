@@ -69,7 +69,7 @@ __device__ __forceinline__ void store_nt(T* p, const float (&v)[V]) {
 }
 
 // Input bytes of a call from which it loads them past the caches: half of the
-// last cache's 256 MB. (The gate: 154 MB of z after the product that wrote it: 121 -> 115
+// last cache's 256 MB (by layouts that have such loads: see there). (The gate: 154 MB of z after the product that wrote it: 121 -> 115
 // us with what comes before and after; 87 MB: the same; 44 MB that no kernel
 // has touched lately: 33 -> 40.)
 constexpr int64_t kFarBytes = 128 << 20;

@@ -15,12 +15,15 @@
 // the next rows are loaded before the present ones are worked on.
 //
 // Measured (kernel time, bytes that the pass cannot do without over it): 397,934
-// rows of 128 in fp32 forward 102 to 116 us (6.2 to 7.0 TB/s), without the
-// checkpoint 104 (5.9), backward 120 to 137 (5.2 to 5.9), where a copy of as much
-// reaches 4.7 TB/s; 85,274 rows of 64 14.6 and 17.8 us (5.3 and 4.3). Both are
-// bound by memory there, with the vector units busy 56 to 66 % of the time. Rows
-// of 16-bit values that allow no vector loads are as busy on half the bytes, and
-// bound by that: 20,011 rows of 333 in bf16 20 and 26 us (2.7 and 2.1 TB/s).
+// rows of 128 in fp32 forward 103 to 116 us (6.2 to 7.0 TB/s), without the
+// checkpoint 104 (5.9), backward 117 to 142 (5.0 to 6.1), where a copy of as much
+// reaches 4.7 TB/s; 85,274 rows of 64 14.4 and 17.7 us (5.3 and 4.3). Both are
+// bound by memory there, with the vector units busy 56 to 68 % of the time. Rows
+// of 16-bit values are as busy on half the bytes, and bound by that, the more so
+// without vector loads (20,011 rows of 333 in bf16 20 and 25 us, 2.7 and 2.1 TB/s)
+// and where columns of the layout are empty: 8e6 values in bf16 take, forward and
+// backward in us a call, 15 and 23 as rows of 256, 20 and 29 of 333, 24 and 44 of
+// 130, 31 and 44 of 34, 49 and 63 of 20.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -61,7 +64,10 @@ struct Scale {
 // on both passes of 85,274 rows of 64 and of 397,934 rows of 128: 38.7 and 287 us
 // with plain accesses, 32.7 and 274 with such stores, 40.2 and 240 with such
 // loads too, which pay where the inputs do not fit the last cache (kFarBytes);
-// a kernel that reads the results next takes no longer at any size.
+// a kernel that reads the results next takes no longer at any size. FAR is for
+// FULL rows: others gain by it only far past that size (forward and backward of
+// 320 columns in us, without and with: 55 and 66, 59 and 73 for 25e6 values in
+// fp32, 131 and 136, 113 and 136 for 50e6, 97 and 120, 96 and 136 for 50e6 in bf16).
 template <int VEC, int LPR, int NQ, int MIN, bool FULL, bool FAR>
 struct Cols {
   static constexpr int CPL = VEC * NQ, RPW = 64 / LPR;
@@ -242,7 +248,8 @@ __global__ void __launch_bounds__(kBwdThreads) k_gate_act_bwd(int64_t rows, int 
   d = cols.d;
   const float inv_d = cols.inv_d;
   // LayerNorm parameters in registers; at 16 columns a lane with an end to look
-  // for, where there is no room for them (70 registers spilled), in LDS
+  // for, where there is no room for them, in LDS (else 70 registers spill; single
+  // values a lane still spill 6 of them)
   constexpr bool kLnInLds = CPL == 16 && !FULL;
   __shared__ float lnS[kLnInLds ? 4 * VEC * LPR * NQ : 1];
   float gc[CPL], bc[CPL], gg[CPL], bg[CPL];
@@ -407,8 +414,10 @@ __global__ void __launch_bounds__(256) k_gate_ln_zero(int n, float* __restrict__
 
 // Calls f with the narrowest layout that holds rows of width d: four values a lane
 // where alignment allows 16-byte (8-byte) accesses, else one. (Groups of four at
-// any address, with the row's last one short, took as long as single values: 8e6
-// values of width 333 in bf16, forward 23 and 21 us, backward 31 and 31.)
+// any address, with the row's last one short, took as long as these single values
+// or longer: 8e6 values in bf16 forward and backward, groups against singles in us,
+// of width 34 36 and 46, 31 and 44; 45 26 and 36, 26 and 36; 130 24 and 44, 24 and
+// 44; 333 20 and 29, 20 and 29; 601 20 and 33, 20 and 33; 1,001 22 and 31, 22 and 31.)
 template <class F>
 int with_layout(int d, bool vec, bool far, F&& f) {
   using std::integral_constant;

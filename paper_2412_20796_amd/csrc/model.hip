@@ -2297,10 +2297,12 @@ __global__ void k_seed_edges2(int E, const int* __restrict__ edge_rev, const flo
 // partial sums are added in wavefront order.
 constexpr int kEmbZWaves = 8;
 // Batches of more atoms take the embedding operator's gradient (embed.hip),
-// whose time does not go with the most frequent element: of 8,632 atoms of
-// uniform elements 15 us here and 8 there, of 34,528 atoms 45 and 25, and where
-// every third atom is oxygen 40 and 14, and 157 and 25 (d = 64). Smaller batches
-// keep this kernel's order of the sum, at 7 to 14 us against 7 to 11.
+// whose time does not go with the most frequent element. Launches of a profiled
+// step, d = 64, here and there in us: 8,632 atoms of uniform elements 16 and 11,
+// 17,264 23 and 34, 34,528 39 and 35; where every third atom is oxygen 54 and 24,
+// 110 and 36, 212 and 36. The step takes as long either way (12.66 ms for 34,528
+// atoms and one layer), since weight gradients run beside it. Smaller batches
+// keep this kernel's order of the sum.
 constexpr int64_t kEmbZAtoms = 8192;
 __global__ void __launch_bounds__(64 * kEmbZWaves) k_embed_bwd_Z(int N, int D, const int* __restrict__ Z,
                                                                  const float* __restrict__ dv0, float* __restrict__ gWZ) {
