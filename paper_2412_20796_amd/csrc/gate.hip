@@ -28,6 +28,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "common.hpp"
 #include "elem.hpp"
@@ -42,11 +43,12 @@ namespace {
 // squares passes the range at a variance d times smaller, where the backward pass,
 // which sums squares of codes, does not. They take 0.5 of 16 us in bf16 rows of
 // 64, whose vector units are the busiest, and 0.2 at most elsewhere. A path of its
-// own for such rows took up to 5 of 22 us of all, for its registers.)
+// own for such rows took up to 5 of 22 us of all, for its registers.) The squares
+// of fp16 values, 65,504 at most, need none.
 struct Scale {
   float sum, mean, dev, var, up;  // 2^-l, 2^(l - h) / d, 2^-h, 4^h / d, 2^h
-  __device__ __forceinline__ Scale(int d, float inv_d) {
-    const int l = 31 - __builtin_clz(2 * d - 1), h = (l + 1) / 2;
+  __device__ __forceinline__ Scale(int d, float inv_d, bool any) {
+    const int l = any ? 31 - __builtin_clz(2 * d - 1) : 0, h = (l + 1) / 2;
     auto pow2 = [](int e) { return __int_as_float((127 + e) << 23); };
     sum = pow2(-l);
     mean = inv_d * pow2(l - h);
@@ -105,7 +107,7 @@ struct Cols {
 #pragma unroll
       for (int k = 0; k < VEC; ++k) v[q * VEC + k] = has(q) ? p[col(q) + k] : 0.f;
   }
-  // (x - mean) 2^-h in place (0 in columns past d), and 1 / deviation of x
+  // (x - mean) 2^-h in place (0 in columns past d), and 2^h / deviation of x
   __device__ __forceinline__ float center(float (&x)[CPL], const Scale& sc) const {
     float s = x[0] * sc.sum;
 #pragma unroll
@@ -121,7 +123,7 @@ struct Cols {
         v += y * y;
       }
     // at least the LayerNorm epsilon: no denormal argument
-    return __builtin_amdgcn_rsqf(rowsum<LPR>(v) * sc.var + kLnEps);
+    return __builtin_amdgcn_rsqf(rowsum<LPR>(v) * sc.var + kLnEps) * sc.up;
   }
   // x - mean in place (0 in columns past d), and 1 / deviation of x * unit, for
   // codes x: what passes fp32's range is the variance alone, in unit^2
@@ -158,12 +160,7 @@ __global__ void __launch_bounds__(256) k_gate_act_fwd(int64_t rows, int d, const
   cols.load_any(ln + d, bc);
   cols.load_any(ln + 2 * d, gg);
   cols.load_any(ln + 3 * d, bg);
-  const Scale sc(d, cols.inv_d);
-#pragma unroll
-  for (int k = 0; k < CPL; ++k) {  // (of rows in 2^-h)
-    gc[k] *= sc.up;
-    gg[k] *= sc.up;
-  }
+  const Scale sc(d, cols.inv_d, !std::is_same<T, f16_t>::value);
   const int64_t stride = (int64_t)gridDim.x * 4 * C::RPW;
   int64_t row = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * C::RPW + lane / LPR;
   float nc[CPL], ng[CPL];

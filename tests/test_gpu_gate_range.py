@@ -72,3 +72,12 @@ def test_sum_past_the_range(value, d):
         ref.assert_within(phi, r, b)
     else:
         assert bool(torch.isfinite(phi).all())
+
+
+def test_scales_up_to_the_range():
+    """A LayerNorm scale next to fp32's largest number, at a value next to its row's mean: their product is in range, and
+    phi a number."""
+    z, ln, _ = _rows(37, 64, 1.0, 0)
+    ln[0, 5] = 3e38
+    z[:, 5] = z[:, [k for k in range(64) if k != 5]].mean(1)
+    assert bool(torch.isfinite(ops.gate_forward(z.cuda(), ln.cuda(), save=False)).all())
