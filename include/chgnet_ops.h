@@ -89,6 +89,75 @@ int chgnet_embed_backward(int64_t n, int32_t d, int64_t vocab, int32_t dtype, co
                           const void* dout, int64_t lddout, float scale, float* dtable, int64_t lddtable,
                           int accumulate, void* ws, size_t ws_bytes, void* stream);
 
+/* Norms of rows x [rows, d], n(x):
+ *   CHGNET_NORM_RMS    x r,           r = 1 / sqrt(mean(x^2) + eps)
+ *   CHGNET_NORM_LAYER  (x - mean) r,  r = 1 / sqrt(var + eps)
+ *   CHGNET_NORM_NONE   x (where a call says so)
+ * with sums in fp32. Where the mean square (the variance) passes fp32's range
+ * n(x) is 0 and no gradient passes it. 1 <= d <= 16384, 1e-20 <= eps <= 1,
+ * rows < 2^32. Parameters are fp32, one row [d] (scale) or two [2, d] (scale,
+ * shift), at any float. */
+#define CHGNET_NORM_NONE 0
+#define CHGNET_NORM_RMS 1
+#define CHGNET_NORM_LAYER 2
+
+/* h = w[0] n(x) + w[1], and its gradients: dx from dh, dw [w_rows, d] fp32, added
+ * to what it holds with accumulate != 0. ws: at least
+ * chgnet_residual_backward_workspace(rows, d, w_rows) bytes, 16-byte aligned. */
+int chgnet_norm_forward(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, int32_t kind, const float* w,
+                        int32_t w_rows, float eps, void* h, int64_t ldh, void* stream);
+int chgnet_residual_backward_workspace(int64_t rows, int32_t d, int32_t param_rows, size_t* bytes);
+int chgnet_norm_backward(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, int32_t kind, const float* w,
+                         int32_t w_rows, float eps, const void* dh, int64_t lddh, void* dx, int64_t lddx, float* dw,
+                         int accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* Residual connection around a block: its stream x [rows, d], its output f, and
+ * the norms after it and before the next block:
+ *   t = post[0] n_post(f) + post[1]
+ *   y = alpha x + beta Drop(sigmoid(gate) t)
+ *   h = pre[0] n_pre(y) + pre[1]        (y as it is stored)
+ * post NULL (post_kind then CHGNET_NORM_NONE): t = f; with post and
+ * CHGNET_NORM_NONE a learned scale. gate: pre-activations, [rows, gate_cols] with
+ * gate_cols = d or 1 (one for the row), or NULL: no gate. pre NULL: no h. Drop is
+ * chgnet_dropout's with p, seed, call and step (p = 0: none); what it drops of f and
+ * gate has no part in y or in any gradient but through the norm's statistics. */
+typedef struct chgnet_residual {
+  int32_t post_kind, post_rows; /* CHGNET_NORM_*, rows of post */
+  int32_t pre_kind, pre_rows;
+  int32_t gate_cols;
+  float alpha, beta, eps, p;
+  uint64_t seed, call;
+  const int64_t* step; /* on the GPU, 8-byte aligned, or NULL */
+} chgnet_residual;
+
+int chgnet_residual_forward(int64_t rows, int32_t d, int32_t dtype, const chgnet_residual* cfg, const void* x, int64_t ldx,
+                            const void* f, int64_t ldf, const void* gate, int64_t ldgate, const float* post,
+                            const float* pre, void* y, int64_t ldy, void* h, int64_t ldh, void* stream);
+
+/* Its gradients from those of y (dy; NULL: zero) and of h (dh, with pre): dx, df,
+ * dgate (with gate), and in fp32 dpost and dpre (with post and pre), added to what
+ * they hold with accumulate != 0. Nothing of the forward pass is kept but y, which
+ * is read with pre; f is read with post or gate. ws: at least
+ * chgnet_residual_backward_workspace(rows, d, rows of post + rows of pre) bytes,
+ * 16-byte aligned. */
+int chgnet_residual_backward(int64_t rows, int32_t d, int32_t dtype, const chgnet_residual* cfg, const void* y, int64_t ldy,
+                             const void* f, int64_t ldf, const void* gate, int64_t ldgate, const float* post,
+                             const float* pre, const void* dy, int64_t lddy, const void* dh, int64_t lddh, void* dx,
+                             int64_t lddx, void* df, int64_t lddf, void* dgate, int64_t lddgate, float* dpost, float* dpre,
+                             int accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* Dropout of x [rows, d]: out = x / (1 - q) where a value is kept, else 0, with q
+ * = p rounded to a multiple of 2^-16; q = 1 keeps none. Value (i, j) is kept if
+ * its 16 bits are at least 2^16 q: half j % 2 (low first) of word (j % 8) / 2 of
+ * Philox4x32-10 (Salmon et al., SC 2011) with the counter (j / 8, i, low and high
+ * word of n) and the key (low and high word of seed), n = call + *step (mod 2^64;
+ * step on the GPU, or NULL: 0). The same seed and n give the same mask, whatever
+ * the type, width, strides and launch: the call on the upstream gradient is the
+ * backward pass, and a graph that adds to *step draws anew at each replay. rows <
+ * 2^32, 1 <= d <= 2^30, 0 <= p <= 1. */
+int chgnet_dropout(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, float p, uint64_t seed,
+                   uint64_t call, const int64_t* step, void* out, int64_t ldout, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

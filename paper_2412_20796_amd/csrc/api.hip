@@ -42,6 +42,22 @@ int embed_backward_workspace_entry(int64_t n, int32_t d, int64_t vocab, size_t* 
 int embed_backward_entry(int64_t n, int32_t d, int64_t vocab, int32_t dtype, const int32_t* tok, int32_t first,
                          const void* dout, int64_t lddout, float scale, float* dtable, int64_t lddtable,
                          int accumulate, void* ws, size_t ws_bytes, hipStream_t st, const char* tag = nullptr);
+int norm_forward_entry(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, int32_t kind, const float* w,
+                       int32_t w_rows, float eps, void* h, int64_t ldh, hipStream_t st);
+int norm_backward_entry(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, int32_t kind, const float* w,
+                        int32_t w_rows, float eps, const void* dh, int64_t lddh, void* dx, int64_t lddx, float* dw,
+                        int accumulate, void* ws, size_t ws_bytes, hipStream_t st);
+int residual_forward_entry(int64_t rows, int32_t d, int32_t dtype, const chgnet_residual* cfg, const void* x, int64_t ldx,
+                           const void* f, int64_t ldf, const void* gate, int64_t ldgate, const float* post,
+                           const float* pre, void* y, int64_t ldy, void* h, int64_t ldh, hipStream_t st);
+int residual_backward_workspace_entry(int64_t rows, int32_t d, int32_t param_rows, size_t* bytes);
+int residual_backward_entry(int64_t rows, int32_t d, int32_t dtype, const chgnet_residual* cfg, const void* y, int64_t ldy,
+                            const void* f, int64_t ldf, const void* gate, int64_t ldgate, const float* post,
+                            const float* pre, const void* dy, int64_t lddy, const void* dh, int64_t lddh, void* dx,
+                            int64_t lddx, void* df, int64_t lddf, void* dgate, int64_t lddgate, float* dpost, float* dpre,
+                            int accumulate, void* ws, size_t ws_bytes, hipStream_t st);
+int dropout_entry(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, float p, uint64_t seed, uint64_t call,
+                  const int64_t* step, void* out, int64_t ldout, hipStream_t st);
 
 namespace {
 thread_local std::string g_last_error;
@@ -296,6 +312,44 @@ int chgnet_profile_stop(char* buf, size_t buflen) {
   if (!buf || buflen <= out.size()) return chg::fail(CHGNET_EINVAL, "profile buffer too small");
   std::snprintf(buf, buflen, "%s", out.c_str());
   return truncated ? chg::fail(CHGNET_EWORKSPACE, "more launches than max_launches; later ones not timed") : CHGNET_OK;
+}
+
+int chgnet_norm_forward(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, int32_t kind, const float* w,
+                        int32_t w_rows, float eps, void* h, int64_t ldh, void* stream) {
+  return chg::norm_forward_entry(rows, d, dtype, x, ldx, kind, w, w_rows, eps, h, ldh, static_cast<hipStream_t>(stream));
+}
+
+int chgnet_residual_backward_workspace(int64_t rows, int32_t d, int32_t param_rows, size_t* bytes) {
+  return chg::residual_backward_workspace_entry(rows, d, param_rows, bytes);
+}
+
+int chgnet_norm_backward(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, int32_t kind, const float* w,
+                         int32_t w_rows, float eps, const void* dh, int64_t lddh, void* dx, int64_t lddx, float* dw,
+                         int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  return chg::norm_backward_entry(rows, d, dtype, x, ldx, kind, w, w_rows, eps, dh, lddh, dx, lddx, dw, accumulate, ws,
+                                  ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+int chgnet_residual_forward(int64_t rows, int32_t d, int32_t dtype, const chgnet_residual* cfg, const void* x, int64_t ldx,
+                            const void* f, int64_t ldf, const void* gate, int64_t ldgate, const float* post,
+                            const float* pre, void* y, int64_t ldy, void* h, int64_t ldh, void* stream) {
+  return chg::residual_forward_entry(rows, d, dtype, cfg, x, ldx, f, ldf, gate, ldgate, post, pre, y, ldy, h, ldh,
+                                     static_cast<hipStream_t>(stream));
+}
+
+int chgnet_residual_backward(int64_t rows, int32_t d, int32_t dtype, const chgnet_residual* cfg, const void* y, int64_t ldy,
+                             const void* f, int64_t ldf, const void* gate, int64_t ldgate, const float* post,
+                             const float* pre, const void* dy, int64_t lddy, const void* dh, int64_t lddh, void* dx,
+                             int64_t lddx, void* df, int64_t lddf, void* dgate, int64_t lddgate, float* dpost, float* dpre,
+                             int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  return chg::residual_backward_entry(rows, d, dtype, cfg, y, ldy, f, ldf, gate, ldgate, post, pre, dy, lddy, dh, lddh, dx,
+                                      lddx, df, lddf, dgate, lddgate, dpost, dpre, accumulate, ws, ws_bytes,
+                                      static_cast<hipStream_t>(stream));
+}
+
+int chgnet_dropout(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, float p, uint64_t seed,
+                   uint64_t call, const int64_t* step, void* out, int64_t ldout, void* stream) {
+  return chg::dropout_entry(rows, d, dtype, x, ldx, p, seed, call, step, out, ldout, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

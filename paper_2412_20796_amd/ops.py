@@ -1,6 +1,7 @@
 """Thin ctypes binding of the operators in include/chgnet_ops.h: the gate of the
-gated MLP with an 8-bit checkpoint of its input, and the scaled embedding lookup
-with its gradient.
+gated MLP with an 8-bit checkpoint of its input, the scaled embedding lookup with
+its gradient, norms and the residual connection around a block with its gate and
+dropout.
 
 Argument marshalling and checks only, as in ``binding``: torch tensors supply
 device memory and the stream (the current one of the tensors' device), and a
@@ -16,6 +17,7 @@ are written so that they add little to that (a dozen attribute reads).
 from __future__ import annotations
 
 import ctypes
+from collections import namedtuple
 from functools import lru_cache
 
 import torch
@@ -23,11 +25,21 @@ import torch
 from . import binding as bd
 
 EXPORTED = ("chgnet_gate_forward", "chgnet_gate_backward_workspace", "chgnet_gate_backward", "chgnet_embed_forward",
-            "chgnet_embed_backward_workspace", "chgnet_embed_backward")
+            "chgnet_embed_backward_workspace", "chgnet_embed_backward", "chgnet_norm_forward", "chgnet_norm_backward",
+            "chgnet_residual_forward", "chgnet_residual_backward_workspace", "chgnet_residual_backward", "chgnet_dropout")
 # (torch.cuda.current_stream and current_device, without the objects and checks around them: 1.3 us a call)
 _raw_stream, _current_gpu = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+NORMS = {"none": 0, "rms": 1, "layer": 2}
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _lib = None
+
+
+class _Residual(ctypes.Structure):
+    """chgnet_residual"""
+
+    _fields_ = ([(n, ctypes.c_int32) for n in ("post_kind", "post_rows", "pre_kind", "pre_rows", "gate_cols")]
+                + [(n, ctypes.c_float) for n in ("alpha", "beta", "eps", "p")]
+                + [("seed", ctypes.c_uint64), ("call", ctypes.c_uint64), ("step", ctypes.c_void_p)])
 
 
 def lib():
@@ -42,6 +54,14 @@ def lib():
         L.chgnet_embed_backward_workspace.argtypes = [i64, i32, i64, ctypes.POINTER(sz)]
         L.chgnet_embed_backward.argtypes = [i64, i32, i64, i32, vp, i32, vp, i64, ctypes.c_float, vp, i64,
                                             ctypes.c_int, vp, sz, vp]
+        f32, u64, cint = ctypes.c_float, ctypes.c_uint64, ctypes.c_int
+        L.chgnet_norm_forward.argtypes = [i64, i32, i32, vp, i64, i32, vp, i32, f32, vp, i64, vp]
+        L.chgnet_norm_backward.argtypes = [i64, i32, i32, vp, i64, i32, vp, i32, f32, vp, i64, vp, i64, vp, cint, vp, sz, vp]
+        L.chgnet_residual_forward.argtypes = [i64, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp]
+        L.chgnet_residual_backward_workspace.argtypes = [i64, i32, i32, ctypes.POINTER(sz)]
+        L.chgnet_residual_backward.argtypes = [i64, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64,
+                                               vp, i64, vp, i64, vp, vp, cint, vp, sz, vp]
+        L.chgnet_dropout.argtypes = [i64, i32, i32, vp, i64, f32, u64, u64, vp, vp, i64, vp]
         for name in EXPORTED:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -273,3 +293,190 @@ def embed_backward(tok, dout, vocab, scale=1.0, first=0, dtable=None, accumulate
     _call(lib().chgnet_embed_backward, gpu, (n, d, vocab, code, tok.data_ptr(), first, dout.data_ptr(), ldo, scale,
                                              dtable.data_ptr(), ldw, bool(accumulate), p, nbytes))
     return dtable
+
+
+@lru_cache(maxsize=4096)
+def _residual_bytes(rows, d, param_rows):
+    need = ctypes.c_size_t()
+    bd._check(lib().chgnet_residual_backward_workspace(rows, d, param_rows, ctypes.byref(need)))
+    return need.value
+
+
+def _params(name, w, d, gpu):
+    """Rows of a norm's fp32 parameters [1, d] (scale) or [2, d] (scale, shift)."""
+    if w.dim() != 2 or w.shape[0] not in (1, 2):
+        _bad("%s must be [1, %d] (scale) or [2, %d] (scale, shift), not %s" % (name, d, d, list(w.shape)))
+    _packed(name, w, (w.shape[0], d), torch.float32, gpu)
+    return w.shape[0]
+
+
+def _norm_kind(kind):
+    if kind not in NORMS:
+        _bad("unknown norm %r: one of %s" % (kind, ", ".join(NORMS)))
+    return NORMS[kind]
+
+
+def _like(name, out, rows, cols, dtype, gpu, like):
+    """(tensor, row stride) of a call's output: the caller's or a new one."""
+    if out is None:
+        return torch.empty((rows, cols), dtype=dtype, device=like.device), cols
+    return out, _rows(name, out, rows, cols, dtype, gpu)
+
+
+def _param_grad(name, out, w, accumulate, gpu):
+    if out is None:
+        if accumulate:
+            _bad("accumulate needs a %s to add to" % name)
+        return torch.empty_like(w)
+    _packed(name, out, w.shape, torch.float32, gpu)
+    return out
+
+
+def _draw(seed, call, step, gpu):
+    """Address of `step`; seed and call are checked (ctypes would keep the low bits)."""
+    if not (0 <= seed < 1 << 64 and 0 <= call < 1 << 64):
+        _bad("seed and call must be in 0 .. 2^64 - 1")
+    if step is None:
+        return None
+    _packed("step", step, (1,), torch.int64, gpu)
+    return step.data_ptr()
+
+
+def dropout(x, p, seed, call=0, step=None, out=None):
+    """x [rows, d] / (1 - p) where the counter-based generator keeps a value, else 0 (p counts in steps of 2^-16). The mask
+    is that of (seed, call + step) whatever the type and strides, and is not stored: the same call on the upstream gradient is
+    the backward pass. step: int64 [1] on the GPU, for graphs whose replays draw anew."""
+    if x.requires_grad and torch.is_grad_enabled():
+        _followed("x")
+    rows, d, dtype, code, ldx, gpu = _start("x", x)
+    at = _draw(seed, call, step, gpu)
+    out, ldo = _like("out", out, rows, d, dtype, gpu, x)
+    _call(lib().chgnet_dropout, gpu, (rows, d, code, x.data_ptr(), ldx, p, seed, call, at, out.data_ptr(), ldo))
+    return out
+
+
+def norm_forward(x, w, kind="rms", eps=1e-5, h=None):
+    """h [rows, d] = w[0] n(x) + w[1] with n the RMS norm ("rms") or the LayerNorm ("layer") of each row; w fp32 [1, d] (no
+    shift) or [2, d]; x in fp32, bf16 or fp16."""
+    if (x.requires_grad or w.requires_grad) and torch.is_grad_enabled():
+        _followed("x or w")
+    rows, d, dtype, code, ldx, gpu = _start("x", x)
+    n = _params("w", w, d, gpu)
+    h, ldh = _like("h", h, rows, d, dtype, gpu, x)
+    _call(lib().chgnet_norm_forward, gpu, (rows, d, code, x.data_ptr(), ldx, _norm_kind(kind), w.data_ptr(), n, eps,
+                                           h.data_ptr(), ldh))
+    return h
+
+
+def norm_backward(x, w, dh, kind="rms", eps=1e-5, dx=None, dw=None, accumulate=False, ws=None):
+    """(dx [rows, d], dw like w) of norm_forward from dh [rows, d]; dw is fp32 and added to what it holds with `accumulate`.
+    ws: a Workspace of the caller's (one for each call that may run at the same time)."""
+    if (x.requires_grad or w.requires_grad or dh.requires_grad) and torch.is_grad_enabled():
+        _followed("x, w or dh")
+    rows, d, dtype, code, ldx, gpu = _start("x", x)
+    n = _params("w", w, d, gpu)
+    ldu = _rows("dh", dh, rows, d, dtype, gpu)
+    dx, ldd = _like("dx", dx, rows, d, dtype, gpu, x)
+    dw = _param_grad("dw", dw, w, accumulate, gpu)
+    p, nbytes, _keep = _workspace(ws, _residual_bytes(rows, d, n), gpu, x)
+    _call(lib().chgnet_norm_backward, gpu, (rows, d, code, x.data_ptr(), ldx, _norm_kind(kind), w.data_ptr(), n, eps,
+                                            dh.data_ptr(), ldu, dx.data_ptr(), ldd, dw.data_ptr(), bool(accumulate), p, nbytes))
+    return dx, dw
+
+
+@lru_cache(maxsize=64)
+def _residual_cfg(*fields):
+    return _Residual(*fields)
+
+
+def _residual(f, post, post_kind, gate, pre, pre_kind, alpha, beta, p, seed, call, step, eps, rows, d, dtype, gpu):
+    """(chgnet_residual, its pointer arguments from f to pre, rows of parameters, the gate's columns)."""
+    ldf = _rows("f", f, rows, d, dtype, gpu)
+    if post_kind is None:
+        post_kind = "none" if post is None else "rms"
+    post_n = post_rows = pre_rows = cols = ldg = 0
+    post_n, pre_n = _norm_kind(post_kind), _norm_kind(pre_kind)
+    if post is not None:
+        post_rows = _params("post", post, d, gpu)
+    elif post_n:
+        _bad("the norm after the block needs its parameters, post")
+    if pre is not None:
+        pre_rows = _params("pre", pre, d, gpu)
+        if not pre_n:
+            _bad("pre_kind must be rms or layer")
+    if gate is not None:
+        cols = d if gate.shape == (rows, d) else 1
+        ldg = _rows("gate", gate, rows, cols, dtype, gpu)
+    at = _draw(seed, call, step, gpu)
+    # (by values, never for a step: a cached struct holds no address)
+    make = _residual_cfg if at is None else _Residual
+    cfg = make(post_n, post_rows, pre_n, pre_rows, cols, alpha, beta, eps, p, seed, call, at)
+    return cfg, (f.data_ptr(), ldf, gate.data_ptr() if cols else None, ldg, post.data_ptr() if post_rows else None,
+                 pre.data_ptr() if pre_rows else None), post_rows + pre_rows, cols
+
+
+def _any_followed(*tensors):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def residual_forward(x, f, post=None, post_kind=None, gate=None, pre=None, pre_kind="rms", alpha=1.0, beta=1.0, p=0.0, seed=0,
+                     call=0, step=None, eps=1e-5, y=None, h=None):
+    """The residual connection around a block: its stream x and its output f [rows, d], the norm after it, its gate, dropout
+    and residual scale, and the norm before the next block. Returns (y, h):
+        y = alpha x + beta Drop(sigmoid(gate) (post[0] n(f) + post[1])),  h = pre[0] n(y) + pre[1]  (None without pre)
+    post, pre: fp32 [1, d] (scale) or [2, d] (scale, shift); kinds "rms", "layer", and after the block also "none" (a learned
+    scale). gate: pre-activations [rows, d] or [rows, 1]. p, seed, call, step: as in `dropout`."""
+    if _any_followed(x, f, post, gate, pre):
+        _followed("x, f, post, gate or pre")
+    rows, d, dtype, code, ldx, gpu = _start("x", x)
+    cfg, args, _, _ = _residual(f, post, post_kind, gate, pre, pre_kind, alpha, beta, p, seed, call, step, eps, rows, d,
+                                dtype, gpu)
+    y, ldy = _like("y", y, rows, d, dtype, gpu, x)
+    ldh = d
+    if pre is not None:
+        h, ldh = _like("h", h, rows, d, dtype, gpu, x)
+    elif h is not None:
+        _bad("h needs the parameters pre of its norm")
+    _call(lib().chgnet_residual_forward, gpu, (rows, d, code, ctypes.byref(cfg), x.data_ptr(), ldx, *args, y.data_ptr(), ldy,
+                                               None if h is None else h.data_ptr(), ldh))
+    return y, h
+
+
+ResidualGradients = namedtuple("ResidualGradients", "dx df dgate dpost dpre")
+
+
+def residual_backward(y, f, dy, dh=None, post=None, post_kind=None, gate=None, pre=None, pre_kind="rms", alpha=1.0, beta=1.0,
+                      p=0.0, seed=0, call=0, step=None, eps=1e-5, dx=None, df=None, dgate=None, dpost=None, dpre=None,
+                      accumulate=False, ws=None):
+    """ResidualGradients of residual_forward from the gradients dy of its y (None: zero) and dh of its h; y is what it returned,
+    the other arguments are as they were. dpost and dpre are fp32 and added to what they hold with `accumulate`; the gradients
+    of what is not there are None. ws: a Workspace of the caller's (one for each call that may run at the same time)."""
+    if _any_followed(y, f, dy, dh, post, gate, pre):
+        _followed("y, f, dy, dh, post, gate or pre")
+    rows, d, dtype, code, ldy, gpu = _start("y", y)
+    cfg, args, n, cols = _residual(f, post, post_kind, gate, pre, pre_kind, alpha, beta, p, seed, call, step, eps, rows, d,
+                                   dtype, gpu)
+    if (dh is None) != (pre is None):
+        _bad("dh goes with pre")
+    if dy is None and dh is None:
+        _bad("neither dy nor dh is given")
+    ldu = 0 if dy is None else _rows("dy", dy, rows, d, dtype, gpu)
+    ldh = 0 if dh is None else _rows("dh", dh, rows, d, dtype, gpu)
+    dx, ldx = _like("dx", dx, rows, d, dtype, gpu, y)
+    df, ldf = _like("df", df, rows, d, dtype, gpu, y)
+    ldg = 0
+    if cols:
+        dgate, ldg = _like("dgate", dgate, rows, cols, dtype, gpu, y)
+    for name, out, of in (("dgate", dgate, gate), ("dpost", dpost, post), ("dpre", dpre, pre)):
+        if of is None and out is not None:
+            _bad("%s is given but not %s" % (name, name[1:]))
+    if post is not None:
+        dpost = _param_grad("dpost", dpost, post, accumulate, gpu)
+    if pre is not None:
+        dpre = _param_grad("dpre", dpre, pre, accumulate, gpu)
+    w, nbytes, _keep = _workspace(ws, _residual_bytes(rows, d, n), gpu, y) if n else (None, 0, None)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    _call(lib().chgnet_residual_backward, gpu, (
+        rows, d, code, ctypes.byref(cfg), y.data_ptr(), ldy, *args, ptr(dy), ldu, ptr(dh), ldh, dx.data_ptr(), ldx,
+        df.data_ptr(), ldf, ptr(dgate), ldg, ptr(dpost), ptr(dpre), bool(accumulate), w, nbytes))
+    return ResidualGradients(dx, df, dgate, dpost, dpre)
