@@ -158,6 +158,51 @@ int chgnet_residual_backward(int64_t rows, int32_t d, int32_t dtype, const chgne
 int chgnet_dropout(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, float p, uint64_t seed,
                    uint64_t call, const int64_t* step, void* out, int64_t ldout, void* stream);
 
+/* A matrix [rows, cols] in 8-bit floating point: codes (e4m3: 4 bits of
+ * exponent, 3 of mantissa, largest 448) and for each block of block_rows (1 or
+ * 128) x 128 of them an exponent byte, 2^(byte - 127), 255 for NaN:
+ *   value[i][j] = code[i][j] 2^(scale[i / block_rows][j / 128] - 127)
+ * Codes of a row follow each other, rows are ld bytes apart (a multiple of 16, on
+ * 16-byte boundaries); where cols is no multiple of 16 the bytes up to the next one
+ * are 0 (chgnet_fp8_quantize writes them). Scale rows are ld_scale bytes apart (a
+ * multiple of 4, on 4-byte boundaries). rows < 2^31, 0 <= cols <= 2^23. */
+typedef struct chgnet_fp8 {
+  int64_t rows, cols;
+  uint8_t* codes;
+  int64_t ld;
+  uint8_t* scale;
+  int64_t ld_scale;
+  int32_t block_rows;
+} chgnet_fp8;
+
+/* Quantises x [rows, cols] into q, and its transpose [cols, rows] into t, whose
+ * blocks of 128 run along the rows of x; either may be NULL. A block's scale is
+ * the least power of two by which its largest magnitude is at most 448, but at
+ * least 2^-126; codes are rounded to nearest, ties to even. A block with a value that
+ * is not finite has the scale NaN. With block_rows = 128 both forms hold the same
+ * values. rows <= 2^23. */
+int chgnet_fp8_quantize(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* q,
+                        const chgnet_fp8* t, void* stream);
+
+/* out [M, N] of `dtype` = a b^T for a [M, K] and b [N, K], summed in fp32, added to
+ * what it holds with accumulate != 0. A linear layer's y = x w^T, dx = dy w and dw =
+ * dy^T x are this with the forms of chgnet_fp8_quantize: (x, w), (dy, w^T), (dy^T,
+ * x^T). For 16-bit results the products of a block are added eight at a time, cut
+ * off at 2^-13 of the largest one's power of two (of normal values some 1e-4 of a
+ * result); for fp32 results they are exact, for values that are fp32 numbers (past
+ * its largest they count as infinite, below 2^-126 they may count as 0). ws: at least
+ * chgnet_fp8_matmul_workspace(M, N, K) bytes, 16-byte aligned (none where that is 0). */
+int chgnet_fp8_matmul_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);
+int chgnet_fp8_matmul(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, void* out, int64_t ldout, int accumulate,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/* Linear layer: out [rows, N] = q(x) w^T for x [rows, K] and w [N, K], where q(x) is
+ * x as chgnet_fp8_quantize has it with block_rows = 1; out has x's dtype. rows <=
+ * 2^23. ws: at least chgnet_fp8_linear_workspace(rows, N, K) bytes, 16-byte aligned. */
+int chgnet_fp8_linear_workspace(int64_t rows, int64_t n, int64_t k, size_t* bytes);
+int chgnet_fp8_linear(int64_t rows, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* w, void* out,
+                      int64_t ldout, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

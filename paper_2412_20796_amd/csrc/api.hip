@@ -58,6 +58,14 @@ int residual_backward_entry(int64_t rows, int32_t d, int32_t dtype, const chgnet
                             int accumulate, void* ws, size_t ws_bytes, hipStream_t st);
 int dropout_entry(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, float p, uint64_t seed, uint64_t call,
                   const int64_t* step, void* out, int64_t ldout, hipStream_t st);
+int fp8_quantize_entry(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* q,
+                       const chgnet_fp8* t, hipStream_t st);
+int fp8_matmul_workspace_entry(int64_t m, int64_t n, int64_t k, size_t* bytes);
+int fp8_matmul_entry(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, void* out, int64_t ldout, int accumulate,
+                     void* ws, size_t ws_bytes, hipStream_t st);
+int fp8_linear_workspace_entry(int64_t rows, int64_t n, int64_t k, size_t* bytes);
+int fp8_linear_entry(int64_t rows, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* w, void* out, int64_t ldout,
+                     void* ws, size_t ws_bytes, hipStream_t st);
 
 namespace {
 thread_local std::string g_last_error;
@@ -350,6 +358,29 @@ int chgnet_residual_backward(int64_t rows, int32_t d, int32_t dtype, const chgne
 int chgnet_dropout(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, float p, uint64_t seed,
                    uint64_t call, const int64_t* step, void* out, int64_t ldout, void* stream) {
   return chg::dropout_entry(rows, d, dtype, x, ldx, p, seed, call, step, out, ldout, static_cast<hipStream_t>(stream));
+}
+
+int chgnet_fp8_quantize(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* q,
+                        const chgnet_fp8* t, void* stream) {
+  return chg::fp8_quantize_entry(rows, cols, dtype, x, ldx, q, t, static_cast<hipStream_t>(stream));
+}
+
+int chgnet_fp8_matmul_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes) {
+  return chg::fp8_matmul_workspace_entry(m, n, k, bytes);
+}
+
+int chgnet_fp8_matmul(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, void* out, int64_t ldout, int accumulate,
+                      void* ws, size_t ws_bytes, void* stream) {
+  return chg::fp8_matmul_entry(a, b, dtype, out, ldout, accumulate, ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+int chgnet_fp8_linear_workspace(int64_t rows, int64_t n, int64_t k, size_t* bytes) {
+  return chg::fp8_linear_workspace_entry(rows, n, k, bytes);
+}
+
+int chgnet_fp8_linear(int64_t rows, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* w, void* out,
+                      int64_t ldout, void* ws, size_t ws_bytes, void* stream) {
+  return chg::fp8_linear_entry(rows, dtype, x, ldx, w, out, ldout, ws, ws_bytes, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

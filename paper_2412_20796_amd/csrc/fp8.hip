@@ -1,0 +1,605 @@
+// Matrix products of 8-bit floating point with a power of two for each block of
+// 128 values (chgnet_ops.h), and the quantiser that makes their factors.
+//
+//   code = e4m3(x 2^-e),  2^e the least power of two with max |x| <= 448 2^e in
+//   the block, at least 2^-126;  out[m][n] = sum over k of a[m][k] b[n][k]
+//
+// Powers of two because the matrix instruction multiplies by them: its operands
+// carry 8-bit exponents beside the codes, so a block's scale costs no vector
+// work and no rounding. In floating-point codes they cost no precision either,
+// but for values some 2^-16 of their block's largest.
+//
+// The instruction adds eight products at a time in steps of 2^-13 of the largest
+// one's power of two and cuts off what is below (measured; sums of such eights are
+// fp32's). For normal values a result is off by about 1e-4 of its size, far
+// inside the half step of a 16-bit result. Results in fp32 take the codes as bf16
+// values, which hold them and their scales exactly, and its products, which are
+// added to fp32's last place, at half of the rate.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "common.hpp"
+#include "elem.hpp"
+#include "rowops.hpp"
+
+namespace chg {
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef bf16_t v2b __attribute__((ext_vector_type(2)));
+typedef bf16_t v8b __attribute__((ext_vector_type(8)));
+
+constexpr int kBlock = 128;   // values under one scale
+constexpr int64_t kMostK = 1 << 23, kMostRows = int64_t(1) << 31;
+
+// ---------------------------------------------------------------------------
+// Scales and codes
+// ---------------------------------------------------------------------------
+
+// Exponent byte (2^(e - 127)) for a block's largest magnitude, as fp32 bits: at
+// most 1.75 2^8 in codes. 255, which stands for NaN, where a value is not finite.
+__device__ __forceinline__ unsigned scale_byte(unsigned big) {
+  const int e = (int)((big + 0x1fffffu) >> 23) - 8;  // one more above a mantissa of 1.75
+  return big >= 0x7f800000u ? 255u : (unsigned)(e < 1 ? 1 : e);
+}
+// 2^-e of such a byte; 0 for NaN, so that the block's codes are 0 (or NaN, which
+// the products have anyway)
+__device__ __forceinline__ float scale_inverse(unsigned byte) {
+  return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);
+}
+__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// four codes, the first in the low byte
+__device__ __forceinline__ unsigned codes4(float a, float b, float c, float d) {
+  unsigned r = 0;
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, r, false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+}
+template <int LPR>
+__device__ __forceinline__ unsigned rowmax_bits(unsigned v) {
+  auto step = [&](unsigned o) { v = o > v ? o : v; };
+  step(__float_as_uint(dpp<0xB1>(__uint_as_float(v))));
+  step(__float_as_uint(dpp<0x4E>(__uint_as_float(v))));
+  if (LPR >= 8) step(__float_as_uint(dpp<0x141>(__uint_as_float(v))));
+  if (LPR >= 16) step(__float_as_uint(dpp<0x140>(__uint_as_float(v))));
+  return v;
+}
+// largest over the four groups of 16 lanes
+__device__ __forceinline__ unsigned groupmax_bits(unsigned v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = a[0] > a[1] ? a[0] : a[1];
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return b[0] > b[1] ? b[0] : b[1];
+}
+
+// Values x[0 .. 7] at column c of a row of n columns; 0 past its end
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, int64_t c, int64_t n, float (&v)[8]) {
+  if (VEC && c + 8 <= n) {
+    load_v<8>(p + c, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = c + k < n ? (float)p[c + k] : 0.f;
+  }
+}
+
+// Rows under 1 x 128 scales: 16 lanes have a block, 8 values each.
+template <class T, bool VEC>
+__global__ void __launch_bounds__(256) k_fp8_rows(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
+                                                  uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scale,
+                                                  int64_t lds) {
+  const int64_t nb = (cols + kBlock - 1) / kBlock, end = (cols + 15) / 16 * 16;
+  const int j = threadIdx.x & 15;
+  const int64_t stride = (int64_t)gridDim.x * 16;
+  for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < rows * nb; i += stride) {
+    const int64_t row = i / nb, b = i - row * nb, c = b * kBlock + 8 * j;
+    float v[8];
+    load8<T, VEC>(x + row * ldx, c, cols, v);
+    unsigned big = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) big = max(big, magnitude(v[k]));
+    const unsigned byte = scale_byte(rowmax_bits<16>(big));
+    const float inv = scale_inverse(byte);
+    if (c < end) {
+      uint2 q;
+      q.x = codes4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+      q.y = codes4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+      *reinterpret_cast<uint2*>(codes + row * ldc + c) = q;
+    }
+    if (j == 0) scale[row * lds + b] = (uint8_t)byte;
+  }
+}
+
+// A tile of 128 x 128 a block, codes of it and of its transpose (either may be
+// left out). SQUARE: one scale for the tile, which both share; else 1 x 128 of
+// the rows of each. A thread has 8 x 8 values; the transposed codes go through
+// LDS, in units of the 8 bytes that a thread has of a column, unit u of column c
+// at u ^ (c / 8 % 16), so that 16 lanes write to 16 banks' pairs.
+template <class T, bool VEC, bool SQUARE>
+__global__ void __launch_bounds__(256) k_fp8_tile(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
+                                                  uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scale,
+                                                  int64_t lds, uint8_t* __restrict__ codes_t, int64_t ldct,
+                                                  uint8_t* __restrict__ scale_t, int64_t ldst) {
+  __shared__ uint2 tile[128][16];
+  __shared__ unsigned colmax[4][128];
+  const int64_t tiles_c = (cols + 127) / 128;
+  const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
+  const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t r0 = tr * 128 + rg * 8, c0 = tc * 128 + cg * 8;
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (r0 + i < rows) {
+      load8<T, VEC>(x + (r0 + i) * ldx, c0, cols, v[i]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+    }
+  }
+  unsigned whole = 0;
+  unsigned col[8] = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) col[k] = max(col[k], magnitude(v[i][k]));
+  if constexpr (SQUARE) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) whole = max(whole, col[k]);
+    whole = groupmax_bits(rowmax_bits<16>(whole));
+    if (lane == 0) colmax[wave][0] = whole;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      col[k] = groupmax_bits(col[k]);
+      if (lane < 16) colmax[wave][cg * 8 + k] = col[k];
+    }
+  }
+  __syncthreads();
+  if constexpr (SQUARE) {
+    whole = max(max(colmax[0][0], colmax[1][0]), max(colmax[2][0], colmax[3][0]));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int c = cg * 8 + k;
+      col[k] = max(max(colmax[0][c], colmax[1][c]), max(colmax[2][c], colmax[3][c]));
+    }
+  }
+  const unsigned all = scale_byte(whole);
+  if (codes) {
+    const int64_t end = (cols + 15) / 16 * 16;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      unsigned byte = all;
+      if constexpr (!SQUARE) {
+        unsigned big = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) big = max(big, magnitude(v[i][k]));
+        byte = scale_byte(rowmax_bits<16>(big));
+      }
+      const float inv = scale_inverse(byte);
+      if (r0 + i < rows) {
+        if (c0 < end) {
+          uint2 q;
+          q.x = codes4(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
+          q.y = codes4(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
+          *reinterpret_cast<uint2*>(codes + (r0 + i) * ldc + c0) = q;
+        }
+        if (!SQUARE && cg == 0) scale[(r0 + i) * lds + tc] = (uint8_t)byte;
+      }
+    }
+    if (SQUARE && threadIdx.x == 0) scale[tr * lds + tc] = (uint8_t)all;
+  }
+  if (!codes_t) return;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const unsigned byte = SQUARE ? all : scale_byte(col[k]);
+    const float inv = scale_inverse(byte);
+    uint2 q;
+    q.x = codes4(v[0][k] * inv, v[1][k] * inv, v[2][k] * inv, v[3][k] * inv);
+    q.y = codes4(v[4][k] * inv, v[5][k] * inv, v[6][k] * inv, v[7][k] * inv);
+    tile[cg * 8 + k][rg ^ cg] = q;
+    if (!SQUARE && rg == 0 && c0 + k < cols) scale_t[(c0 + k) * ldst + tr] = (uint8_t)byte;
+  }
+  if (SQUARE && threadIdx.x == 0) scale_t[tc * ldst + tr] = (uint8_t)all;
+  __syncthreads();
+  const int64_t end = (rows + 15) / 16 * 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = i * 256 + threadIdx.x, c = t >> 3, u = t & 7, g = c >> 3;
+    const int64_t cc = tc * 128 + c, rr = tr * 128 + u * 16;
+    const uint2 a = tile[c][(2 * u) ^ g], b = tile[c][(2 * u + 1) ^ g];
+    if (cc < cols && rr < end) *reinterpret_cast<uint4*>(codes_t + cc * ldct + rr) = make_uint4(a.x, a.y, b.x, b.y);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Products
+// ---------------------------------------------------------------------------
+
+// One factor: codes [rows, K] and scale bytes [rows / 128 or rows, K / 128]
+struct Factor {
+  const uint8_t *codes, *scale;
+  int64_t ldc, lds;
+  int64_t rows;
+  int shift;  // row >> shift has the scales: 7 (a block of 128 rows) or 0
+};
+struct ProductArgs {
+  Factor a, b;
+  int64_t K;
+  void* out;
+  int64_t ldo;
+  float* part;  // [split][M][N] partial sums, or NULL: `out` is written
+  int kb_split;  // blocks of 128 along K that one split has
+  int add;
+};
+
+__device__ __align__(16) const uint8_t kZeros[16] = {};
+
+// a lane's 32 codes as bf16 values, times their scale
+__device__ __forceinline__ void wide(const v8i& q, int byte, v8b (&v)[4]) {
+  const float s = byte == 255 ? __builtin_nanf("") : __uint_as_float(byte ? (unsigned)byte << 23 : 0x400000u);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i], s, false);
+    const v2b b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i], s, true);
+    const v2b c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + 1], s, false);
+    const v2b d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + 1], s, true);
+    v[i] = v8b{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void put4(T* p, const v4f& v, int64_t n, int64_t N, bool vec, bool add) {
+  float t[4] = {v[0], v[1], v[2], v[3]};
+  if (vec && n + 4 <= N) {
+    if (add) {
+      float o[4];
+      load_v<4>(p, o);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) t[k] += o[k];
+    }
+    store_v<4>(p, t);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (n + k < N) p[k] = (T)(add ? (float)p[k] + t[k] : t[k]);
+  }
+}
+
+// A block has BM x BN results, its WM x WN wavefronts equal parts of them. Both
+// factors' codes of 128 values of K go to LDS past the registers, the next ones
+// while the present are multiplied; a row's 8 pieces of 16 bytes sit at piece ^
+// (row % 8), so that the lanes of a load meet in no bank. The factors change
+// places in the instruction, so that a lane has four results of a row.
+// EXACT: products of bf16 values. Which of a block's 128 values an instruction
+// multiplies is any order that both factors share: a lane's bytes 8 s .. 8 s + 7.
+template <class T, bool EXACT, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(ProductArgs p) {
+  constexpr int THREADS = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+  constexpr int PIECES = (BM + BN) * 8 / THREADS;  // of 16 bytes, a thread
+  __shared__ __align__(1024) uint8_t lds[2][(BM + BN) * kBlock];
+  const int64_t M = p.a.rows, N = p.b.rows;
+  const int64_t tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
+  // tiles: each of the 8 chiplets has a run of them, in groups of 8 rows of tiles
+  int64_t tile = blockIdx.x;
+  {
+    const int64_t n = tiles_m * tiles_n, q = n / 8, r = n % 8, x = tile % 8;
+    tile = x * q + (x < r ? x : r) + tile / 8;
+  }
+  int64_t tm, tn;
+  {
+    const int64_t group = 8 * tiles_n, g = tile / group, first = g * 8, size = tiles_m - first < 8 ? tiles_m - first : 8;
+    const int64_t in = tile - g * group;
+    tm = first + in % size;
+    tn = in / size;
+  }
+  const int64_t m0 = tm * BM, n0 = tn * BN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  const int64_t nkb = (p.K + kBlock - 1) / kBlock;
+  const int64_t kb0 = (int64_t)blockIdx.y * p.kb_split;
+  const int64_t kb1 = kb0 + p.kb_split < nkb ? kb0 + p.kb_split : nkb;
+
+  // addresses of this thread's pieces: rows past the end are the last one again
+  const uint8_t* src[PIECES];
+  int piece[PIECES];
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    const int t = i * THREADS + threadIdx.x, row = t >> 3;
+    piece[i] = (t & 7) ^ (row & 7);
+    const bool is_a = row < BM;
+    const int64_t r = is_a ? m0 + row : n0 + row - BM, last = is_a ? M - 1 : N - 1;
+    const Factor& f = is_a ? p.a : p.b;
+    src[i] = f.codes + (r < last ? r : last) * f.ldc + 16 * piece[i];
+  }
+  auto fetch = [&](int64_t kb, int buf) {
+    const int64_t at = kb * kBlock;
+    const int64_t left = p.K - at;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const uint8_t* s = src[i] + at;
+      if (left < kBlock && 16 * piece[i] >= left) s = kZeros;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)s,
+                                       (__attribute__((address_space(3))) void*)(lds[buf] + (i * THREADS + wave * 64) * 16), 16,
+                                       0, 0);
+    }
+  };
+  const int r16 = lane & 15, g = lane >> 4;
+  // scale words: row's bytes of four blocks of K
+  const uint8_t* sa[TM];
+  const uint8_t* sb[TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t r = m0 + wm + 16 * i + r16;
+    sa[i] = p.a.scale + ((r < M ? r : M - 1) >> p.a.shift) * p.a.lds;
+  }
+#pragma unroll
+  for (int i = 0; i < TN; ++i) {
+    const int64_t r = n0 + wn + 16 * i + r16;
+    sb[i] = p.b.scale + ((r < N ? r : N - 1) >> p.b.shift) * p.b.lds;
+  }
+  v4f acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+  auto fragment = [&](const uint8_t* base, int row) {
+    const uint8_t* q = base + (row + r16) * kBlock;
+    const v4i a = *reinterpret_cast<const v4i*>(q + (((2 * g) ^ (r16 & 7)) * 16));
+    const v4i b = *reinterpret_cast<const v4i*>(q + (((2 * g + 1) ^ (r16 & 7)) * 16));
+    return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  };
+  if (kb0 < kb1) fetch(kb0, 0);
+  for (int64_t kb = kb0; kb < kb1; ++kb) {
+    const int buf = (int)(kb - kb0) & 1;
+    int ea[TM], eb[TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) ea[i] = sa[i][kb];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) eb[j] = sb[j][kb];
+    __syncthreads();  // the codes are there, and the other buffer is read
+    if (kb + 1 < kb1) fetch(kb + 1, buf ^ 1);
+    if constexpr (EXACT) {
+      v8b bf[TN][4];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) wide(fragment(lds[buf] + BM * kBlock, wn + 16 * j), eb[j], bf[j]);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        v8b af[4];
+        wide(fragment(lds[buf], wm + 16 * i), ea[i], af);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[j][s], af[s], acc[i][j], 0, 0, 0);
+      }
+    } else {
+      v8i bf[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) bf[j] = fragment(lds[buf] + BM * kBlock, wn + 16 * j);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const v8i af = fragment(lds[buf], wm + 16 * i);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bf[j], af, acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t m = m0 + wm + 16 * i + r16;
+    if (m >= M) continue;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int64_t n = n0 + wn + 16 * j + 4 * g;
+      if (p.part) {
+        put4(p.part + ((int64_t)blockIdx.y * M + m) * N + n, acc[i][j], n, N, (N & 3) == 0, false);
+      } else {
+        T* o = static_cast<T*>(p.out) + m * p.ldo + n;
+        put4(o, acc[i][j], n, N, (p.ldo & 3) == 0 && ((uintptr_t)p.out & (4 * sizeof(T) - 1)) == 0, p.add);
+      }
+    }
+  }
+}
+
+// out (+)= the sum of the splits' parts, in order
+template <class T>
+__global__ void __launch_bounds__(256) k_fp8_join(int64_t M, int64_t N, int splits, const float* __restrict__ part,
+                                                  T* __restrict__ out, int64_t ldo, int add) {
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * N; i += stride) {
+    const int64_t m = i / N, n = i - m * N;
+    float s = part[i];
+    for (int k = 1; k < splits; ++k) s += part[(int64_t)k * M * N + i];
+    T* o = out + m * ldo + n;
+    *o = (T)(add ? (float)*o + s : s);
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) k_fp8_zero(int64_t M, int64_t N, T* __restrict__ out, int64_t ldo) {
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * N; i += stride) out[i / N * ldo + i % N] = (T)0.f;
+}
+
+int bad(const char* who, const char* what) { return fail(CHGNET_EINVAL, std::string(who) + ": " + what); }
+
+// Shape of one quantised matrix; pointers only where `there`
+int check_factor(const char* who, const chgnet_fp8* f, bool there) {
+  if (!f) return bad(who, "a matrix is NULL");
+  if (f->rows < 0 || f->rows >= kMostRows) return bad(who, "rows must be in 0 .. 2^31 - 1");
+  if (f->cols < 0 || f->cols > kMostK) return bad(who, "columns must be in 0 .. 2^23");
+  if (f->block_rows != 1 && f->block_rows != kBlock) return bad(who, "block_rows must be 1 or 128");
+  if (f->ld < cdiv(f->cols, 16) * 16 || f->ld % 16) return bad(who, "ld must be a multiple of 16 that holds the columns");
+  if (f->ld_scale < cdiv(f->cols, kBlock) || f->ld_scale % 4)
+    return bad(who, "ld_scale must be a multiple of 4 that holds a byte for each 128 columns");
+  if (there && f->cols > 0 && (!f->codes || !f->scale)) return bad(who, "null argument");
+  if (!aligned_to(f->codes, 16) || !aligned_to(f->scale, 4)) return bad(who, "codes must be 16-byte, scale 4-byte aligned");
+  return CHGNET_OK;
+}
+Factor factor(const chgnet_fp8* f) {
+  return {f->codes, f->scale, f->ld, f->ld_scale, f->rows, f->block_rows == kBlock ? 7 : 0};
+}
+
+struct Plan {
+  int splits, kb_split;
+};
+// Splits of K: where the tiles are fewer than the compute units
+Plan plan(int64_t M, int64_t N, int64_t K) {
+  const int64_t tiles = cdiv(M, 128) * cdiv(N, 128), nkb = std::max<int64_t>(1, cdiv(K, kBlock));
+  int64_t s = tiles >= 256 ? 1 : std::min<int64_t>(cdiv(512, tiles), std::max<int64_t>(1, nkb / 4));
+  const int64_t per = cdiv(nkb, s);
+  return {(int)cdiv(nkb, per), (int)per};
+}
+
+}  // namespace
+
+int fp8_quantize_entry(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* q,
+                       const chgnet_fp8* t, hipStream_t st) {
+  const char* who = "fp8_quantize";
+  if (rows < 0 || rows > kMostK || cols < 0 || cols > kMostK) return bad(who, "rows and columns must be in 0 .. 2^23");
+  if (!elem_size(dtype)) return bad(who, "unknown dtype");
+  if (ldx < cols) return bad(who, "a row stride is below the row's width");
+  if (!q && !t) return bad(who, "neither codes nor those of the transpose are asked for");
+  if (q) {
+    CHG_TRY(check_factor(who, q, rows > 0));
+    if (q->rows != rows || q->cols != cols) return bad(who, "the codes are of another shape");
+  }
+  if (t) {
+    CHG_TRY(check_factor(who, t, cols > 0));
+    if (t->rows != cols || t->cols != rows) return bad(who, "the transposed codes are of another shape");
+  }
+  if (q && t && q->block_rows != t->block_rows) return bad(who, "both forms have the same block_rows");
+  if (rows == 0 || cols == 0) return CHGNET_OK;
+  const size_t es = elem_size(dtype);
+  if (!x) return bad(who, "null argument");
+  if (!aligned_to(x, es)) return bad(who, "x is not aligned to its values");
+  const bool vec = ldx * es % 16 == 0 && aligned_to(x, 16);
+  const bool square = (q ? q : t)->block_rows == kBlock;
+  return with_type(dtype, [&](auto v) -> int {
+    using T = decltype(v);
+    const T* p = static_cast<const T*>(x);
+    if (!square && !t) {
+      const unsigned blocks = (unsigned)std::min<int64_t>(4096, cdiv(rows * cdiv(cols, kBlock), 16));
+#define CHG_ROWS(V) \
+  KLAUNCH(st, "k_fp8_rows", k_fp8_rows<T, V><<<blocks, 256, 0, st>>>(rows, cols, p, ldx, q->codes, q->ld, q->scale, q->ld_scale))
+      if (vec) CHG_ROWS(true);
+      else CHG_ROWS(false);
+#undef CHG_ROWS
+      return CHGNET_OK;
+    }
+    const int64_t tiles = cdiv(rows, 128) * cdiv(cols, 128);
+    if (tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles of 128 x 128");
+    const chgnet_fp8 none{}, &a = q ? *q : none, &b = t ? *t : none;
+#define CHG_TILE(V, S)                                                                                                     \
+  KLAUNCH(st, "k_fp8_tile", k_fp8_tile<T, V, S><<<(unsigned)tiles, 256, 0, st>>>(                                          \
+                                rows, cols, p, ldx, a.codes, a.ld, a.scale, a.ld_scale, b.codes, b.ld, b.scale, b.ld_scale))
+    if (vec && square) CHG_TILE(true, true);
+    else if (vec) CHG_TILE(true, false);
+    else if (square) CHG_TILE(false, true);
+    else CHG_TILE(false, false);
+#undef CHG_TILE
+    return CHGNET_OK;
+  });
+}
+
+int fp8_matmul_workspace_entry(int64_t M, int64_t N, int64_t K, size_t* bytes) {
+  const char* who = "fp8_matmul_workspace";
+  if (M < 0 || N < 0 || M >= kMostRows || N >= kMostRows || K < 0 || K > kMostK) return bad(who, "sizes out of range");
+  if (!bytes) return bad(who, "bytes is NULL");
+  *bytes = 0;
+  if (M == 0 || N == 0) return CHGNET_OK;
+  const Plan pl = plan(M, N, K);
+  if (pl.splits > 1) *bytes = sizeof(float) * (size_t)pl.splits * (size_t)M * (size_t)N;
+  return CHGNET_OK;
+}
+
+int fp8_matmul_entry(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, void* out, int64_t ldout, int accumulate,
+                     void* ws, size_t ws_bytes, hipStream_t st) {
+  const char* who = "fp8_matmul";
+  CHG_TRY(check_factor(who, a, a && a->rows > 0));
+  CHG_TRY(check_factor(who, b, b && b->rows > 0));
+  if (a->cols != b->cols) return bad(who, "the factors have different numbers of columns");
+  if (!elem_size(dtype)) return bad(who, "unknown dtype");
+  const int64_t M = a->rows, N = b->rows, K = a->cols;
+  if (ldout < N) return bad(who, "a row stride is below the row's width");
+  if (M == 0 || N == 0) return CHGNET_OK;
+  if (!out) return bad(who, "null argument");
+  if (!aligned_to(out, elem_size(dtype))) return bad(who, "out is not aligned to its values");
+  size_t need = 0;
+  CHG_TRY(fp8_matmul_workspace_entry(M, N, K, &need));
+  if (need && (!ws || ws_bytes < need))
+    return fail(CHGNET_EWORKSPACE, std::string(who) + ": workspace too small (query chgnet_fp8_matmul_workspace)");
+  if (!aligned_to(ws, 16)) return bad(who, "ws is not 16-byte aligned");
+  const Plan pl = plan(M, N, K);
+  ProductArgs p{factor(a), factor(b), K, out, ldout, pl.splits > 1 ? static_cast<float*>(ws) : nullptr, pl.kb_split,
+                accumulate != 0};
+  const int64_t tiles = cdiv(M, 128) * cdiv(N, 128);
+  if (tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles of 128 x 128");
+  return with_type(dtype, [&](auto v) -> int {
+    using T = decltype(v);
+    constexpr bool exact = std::is_same<T, float>::value;
+    if (pl.splits > 1) {
+      KLAUNCH(st, "k_fp8_product",
+              k_fp8_product<float, exact, 128, 128, 2, 2><<<dim3((unsigned)tiles, pl.splits), 256, 0, st>>>(p));
+      KLAUNCH(st, "k_fp8_join", k_fp8_join<T><<<(unsigned)std::min<int64_t>(2048, cdiv(M * N, 256)), 256, 0, st>>>(
+                                    M, N, pl.splits, p.part, static_cast<T*>(out), ldout, p.add));
+    } else {
+      KLAUNCH(st, "k_fp8_product", k_fp8_product<T, exact, 128, 128, 2, 2><<<dim3((unsigned)tiles, 1), 256, 0, st>>>(p));
+    }
+    return CHGNET_OK;
+  });
+}
+
+// Layout of a linear layer's workspace: codes and scales of x, the product's own
+struct LinearWs {
+  chgnet_fp8 q;
+  size_t product, total;
+};
+static LinearWs linear_ws(int64_t M, int64_t K, size_t product, void* ws) {
+  LinearWs w{};
+  w.q.rows = M, w.q.cols = K, w.q.block_rows = 1;
+  w.q.ld = cdiv(K, 16) * 16, w.q.ld_scale = cdiv(cdiv(K, kBlock), 4) * 4;
+  const size_t codes = align_up((size_t)M * w.q.ld, 256), scale = align_up((size_t)M * w.q.ld_scale, 256);
+  w.q.codes = static_cast<uint8_t*>(ws);
+  w.q.scale = static_cast<uint8_t*>(ws) + codes;
+  w.product = codes + scale;
+  w.total = w.product + product;
+  return w;
+}
+
+int fp8_linear_workspace_entry(int64_t M, int64_t N, int64_t K, size_t* bytes) {
+  size_t product = 0;
+  CHG_TRY(fp8_matmul_workspace_entry(M, N, K, &product));
+  if (!bytes) return bad("fp8_linear_workspace", "bytes is NULL");
+  *bytes = M && N && K ? linear_ws(M, K, product, nullptr).total : 0;
+  return CHGNET_OK;
+}
+
+int fp8_linear_entry(int64_t rows, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* w, void* out, int64_t ldout,
+                     void* ws, size_t ws_bytes, hipStream_t st) {
+  const char* who = "fp8_linear";
+  if (rows < 0 || rows > kMostK) return bad(who, "rows must be in 0 .. 2^23");
+  if (!elem_size(dtype)) return bad(who, "unknown dtype");
+  CHG_TRY(check_factor(who, w, w && w->rows > 0));
+  if (ldx < w->cols || ldout < w->rows) return bad(who, "a row stride is below the row's width");
+  if (rows == 0 || w->rows == 0) return CHGNET_OK;
+  const size_t es = elem_size(dtype);
+  if (!out || (!x && w->cols)) return bad(who, "null argument");
+  if (!aligned_to(x, es) || !aligned_to(out, es)) return bad(who, "an array is not aligned to its values");
+  size_t product = 0;
+  CHG_TRY(fp8_matmul_workspace_entry(rows, w->rows, w->cols, &product));
+  const LinearWs l = linear_ws(rows, w->cols, product, ws);
+  if (w->cols && (!ws || ws_bytes < l.total))
+    return fail(CHGNET_EWORKSPACE, "fp8_linear: workspace too small (query chgnet_fp8_linear_workspace)");
+  if (!aligned_to(ws, 16)) return bad(who, "ws is not 16-byte aligned");
+  CHG_TRY(fp8_quantize_entry(rows, w->cols, dtype, x, ldx, &l.q, nullptr, st));
+  return fp8_matmul_entry(&l.q, w, dtype, out, ldout, 0, static_cast<uint8_t*>(ws) + l.product, product, st);
+}
+
+}  // namespace chg

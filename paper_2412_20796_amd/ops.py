@@ -1,7 +1,7 @@
 """Thin ctypes binding of the operators in include/chgnet_ops.h: the gate of the
 gated MLP with an 8-bit checkpoint of its input, the scaled embedding lookup with
 its gradient, norms and the residual connection around a block with its gate and
-dropout.
+dropout, linear layers in 8-bit floating point.
 
 Argument marshalling and checks only, as in ``binding``: torch tensors supply
 device memory and the stream (the current one of the tensors' device), and a
@@ -26,7 +26,9 @@ from . import binding as bd
 
 EXPORTED = ("chgnet_gate_forward", "chgnet_gate_backward_workspace", "chgnet_gate_backward", "chgnet_embed_forward",
             "chgnet_embed_backward_workspace", "chgnet_embed_backward", "chgnet_norm_forward", "chgnet_norm_backward",
-            "chgnet_residual_forward", "chgnet_residual_backward_workspace", "chgnet_residual_backward", "chgnet_dropout")
+            "chgnet_residual_forward", "chgnet_residual_backward_workspace", "chgnet_residual_backward", "chgnet_dropout",
+            "chgnet_fp8_quantize", "chgnet_fp8_matmul_workspace", "chgnet_fp8_matmul", "chgnet_fp8_linear_workspace",
+            "chgnet_fp8_linear")
 # (torch.cuda.current_stream and current_device, without the objects and checks around them: 1.3 us a call)
 _raw_stream, _current_gpu = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 NORMS = {"none": 0, "rms": 1, "layer": 2}
@@ -40,6 +42,13 @@ class _Residual(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("post_kind", "post_rows", "pre_kind", "pre_rows", "gate_cols")]
                 + [(n, ctypes.c_float) for n in ("alpha", "beta", "eps", "p")]
                 + [("seed", ctypes.c_uint64), ("call", ctypes.c_uint64), ("step", ctypes.c_void_p)])
+
+
+class _Fp8(ctypes.Structure):
+    """chgnet_fp8"""
+
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("codes", ctypes.c_void_p), ("ld", ctypes.c_int64),
+                ("scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64), ("block_rows", ctypes.c_int32)]
 
 
 def lib():
@@ -62,6 +71,11 @@ def lib():
         L.chgnet_residual_backward.argtypes = [i64, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64,
                                                vp, i64, vp, i64, vp, vp, cint, vp, sz, vp]
         L.chgnet_dropout.argtypes = [i64, i32, i32, vp, i64, f32, u64, u64, vp, vp, i64, vp]
+        psz = ctypes.POINTER(sz)
+        L.chgnet_fp8_quantize.argtypes = [i64, i64, i32, vp, i64, vp, vp, vp]
+        L.chgnet_fp8_matmul_workspace.argtypes = L.chgnet_fp8_linear_workspace.argtypes = [i64, i64, i64, psz]
+        L.chgnet_fp8_matmul.argtypes = [vp, vp, i32, vp, i64, cint, vp, sz, vp]
+        L.chgnet_fp8_linear.argtypes = [i64, i32, vp, i64, vp, vp, i64, vp, sz, vp]
         for name in EXPORTED:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -480,3 +494,153 @@ def residual_backward(y, f, dy, dh=None, post=None, post_kind=None, gate=None, p
         rows, d, code, ctypes.byref(cfg), y.data_ptr(), ldy, *args, ptr(dy), ldu, ptr(dh), ldh, dx.data_ptr(), ldx,
         df.data_ptr(), ldf, ptr(dgate), ldg, ptr(dpost), ptr(dpre), bool(accumulate), w, nbytes))
     return ResidualGradients(dx, df, dgate, dpost, dpre)
+
+
+class Fp8Matrix:
+    """A matrix [rows, cols] in 8-bit floating point: codes (torch.float8_e4m3fn) and a power of two (torch.float8_e8m0fnu) for
+    each block of block_rows (1 or 128) x 128 of them; its values are codes.float() times their block's scale.float(). From
+    tensors of the caller's, codes [rows, cols] in rows that start on 16 bytes and, up to the next multiple of 16 columns, end
+    in zeros; scale [rows / block_rows, cols / 128], rounded up, in rows that start on 4 bytes. Or made by fp8_quantize."""
+
+    __slots__ = ("rows", "cols", "block_rows", "_codes", "_scale", "_data", "_c", "_gpu")
+
+    def __init__(self, codes, scale, block_rows=1):
+        if codes.dim() != 2 or codes.dtype is not torch.float8_e4m3fn:
+            _bad("codes must be a matrix of torch.float8_e4m3fn, not %s %s" % (list(codes.shape), codes.dtype))
+        if block_rows not in (1, 128):
+            _bad("block_rows must be 1 or 128")
+        rows, cols = codes.shape
+        shape = (-(-rows // block_rows), -(-cols // 128))
+        gpu = codes.get_device()
+        if scale.dtype is not torch.float8_e8m0fnu or scale.shape != shape or scale.get_device() != gpu:
+            _bad("scale must be %s of torch.float8_e8m0fnu on %s, not %s %s on %s"
+                 % (list(shape), codes.device, list(scale.shape), scale.dtype, scale.device))
+        self._codes, self._scale, self._data, self._gpu = codes, scale, None, gpu
+        self._make(rows, cols, block_rows, codes.data_ptr(), self._row("codes", codes, 16), scale.data_ptr(),
+                   self._row("scale", scale, 4))
+
+    @staticmethod
+    def _row(name, t, unit):
+        """Row stride of bytes whose rows start on `unit` bytes and can be read up to the next multiple of it."""
+        rows, cols = t.shape
+        whole = -(-cols // unit) * unit
+        ld = t.stride(0) if rows > 1 else whole
+        if (cols > 1 and t.stride(1) != 1) or ld % unit or ld < whole or t.data_ptr() % unit:
+            _bad("%s must have contiguous columns, and rows that start on %d bytes and do not overlap" % (name, unit))
+        if rows and t.storage_offset() + (rows - 1) * ld + whole > t.untyped_storage().nbytes():
+            _bad("%s must have %d bytes in its last row too" % (name, whole))
+        return ld
+
+    def _make(self, rows, cols, block_rows, codes, ld, scale, ld_scale):
+        self.rows, self.cols, self.block_rows = rows, cols, block_rows
+        self._c = _Fp8(rows, cols, codes, ld, scale, ld_scale, block_rows)
+
+    @classmethod
+    def empty(cls, rows, cols, block_rows=1, device="cuda"):
+        """One allocation for fp8_quantize to write to."""
+        self = cls.__new__(cls)
+        ld, lds = -(-cols // 16) * 16, -(-cols // 512) * 4
+        self._data = torch.empty(rows * ld + -(-rows // block_rows) * lds, dtype=torch.uint8, device=device)
+        self._gpu = self._data.get_device()
+        p = self._data.data_ptr()
+        self._make(rows, cols, block_rows, p, ld, p + rows * ld, lds)
+        self._codes = self._scale = None
+        return self
+
+    @property
+    def shape(self):
+        return (self.rows, self.cols)
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            n = self.rows * self._c.ld
+            self._codes = self._data[:n].view(torch.float8_e4m3fn).view(self.rows, self._c.ld)[:, :self.cols]
+        return self._codes
+
+    @property
+    def scale(self):
+        if self._scale is None:
+            n, rows = self.rows * self._c.ld, -(-self.rows // self.block_rows)
+            self._scale = self._data[n:].view(torch.float8_e8m0fnu).view(rows, self._c.ld_scale)[:, :-(-self.cols // 128)]
+        return self._scale
+
+
+def _fp8_out(name, m, rows, cols, block_rows, gpu, like):
+    if m is None:
+        return Fp8Matrix.empty(rows, cols, block_rows, like.device)
+    if m.rows != rows or m.cols != cols or m.block_rows != block_rows or m._gpu != gpu:
+        _bad("%s must be of [%d, %d] with block_rows %d on GPU %d" % (name, rows, cols, block_rows, gpu))
+    return m
+
+
+def _fp8_quantize(x, block_rows, want, want_t, out, out_t):
+    if x.requires_grad and torch.is_grad_enabled():
+        _followed("x")
+    rows, cols, _, code, ldx, gpu = _start("x", x)
+    if block_rows not in (1, 128):
+        _bad("block_rows must be 1 or 128")
+    q = _fp8_out("out", out, rows, cols, block_rows, gpu, x) if want else None
+    t = _fp8_out("out_t", out_t, cols, rows, block_rows, gpu, x) if want_t else None
+    _call(lib().chgnet_fp8_quantize, gpu, (rows, cols, code, x.data_ptr(), ldx, ctypes.byref(q._c) if want else None,
+                                           ctypes.byref(t._c) if want_t else None))
+    return q, t
+
+
+def fp8_quantize(x, block_rows=1, transposed=False, out=None):
+    """x [rows, cols] in fp32, bf16 or fp16 as an Fp8Matrix, with a power of two for each block of block_rows (1, or 128 for
+    weights) x 128; with `transposed` its transpose [cols, rows], whose blocks run along the rows of x."""
+    q, t = _fp8_quantize(x, block_rows, not transposed, transposed, out, out)
+    return t if transposed else q
+
+
+def fp8_quantize_both(x, block_rows=1, out=None, out_t=None):
+    """Both forms in one pass over x: what a training step needs of a linear layer's input, weight and upstream gradient."""
+    return _fp8_quantize(x, block_rows, True, True, out, out_t)
+
+
+@lru_cache(maxsize=4096)
+def _fp8_bytes(fn, m, n, k):
+    need = ctypes.c_size_t()
+    bd._check(getattr(lib(), fn)(m, n, k, ctypes.byref(need)))
+    return need.value
+
+
+def fp8_matmul(a, b, dtype=torch.bfloat16, out=None, accumulate=False, ws=None):
+    """out [M, N] = a b^T of Fp8Matrix a [M, K] and b [N, K], summed in fp32, in `dtype` (or out's); added to what it holds with
+    `accumulate`. With (q, t) of fp8_quantize_both a linear layer's output is (x.q, w.q), its input's gradient (dy.q, w.t) and
+    its weight's (dy.t, x.t). ws: a Workspace of the caller's (one for each call that may run at the same time)."""
+    gpu, m, n, k = a._gpu, a.rows, b.rows, a.cols
+    if gpu < 0 or b._gpu != gpu:
+        _bad("both matrices must be on one GPU")
+    if out is None:
+        if accumulate:
+            _bad("accumulate needs an out to add to")
+        if dtype not in DTYPES:
+            _bad("dtype must be fp32, bf16 or fp16, not %s" % dtype)
+        out, ldo = torch.empty((m, n), dtype=dtype, device=torch.device("cuda", gpu)), n
+    else:
+        dtype = out.dtype
+        if dtype not in DTYPES:
+            _bad("out must be fp32, bf16 or fp16, not %s" % dtype)
+        ldo = _rows("out", out, m, n, dtype, gpu)
+    need = _fp8_bytes("chgnet_fp8_matmul_workspace", m, n, k)
+    p, nbytes, _keep = _workspace(ws, need, gpu, out) if need else (None, 0, None)
+    _call(lib().chgnet_fp8_matmul, gpu, (ctypes.byref(a._c), ctypes.byref(b._c), DTYPES[dtype], out.data_ptr(), ldo,
+                                         bool(accumulate), p, nbytes))
+    return out
+
+
+def fp8_linear(x, w, out=None, ws=None):
+    """out [rows, N] = q(x) w^T of x [rows, K] in fp32, bf16 or fp16 and an Fp8Matrix w [N, K], where q(x) is fp8_quantize's
+    x; out is of x's type. ws: a Workspace of the caller's (one for each call that may run at the same time)."""
+    if x.requires_grad and torch.is_grad_enabled():
+        _followed("x")
+    rows, k, dtype, code, ldx, gpu = _start("x", x)
+    if k != w.cols or w._gpu != gpu:
+        _bad("w must be of [N, %d] on GPU %d, not of [%d, %d]" % (k, gpu, w.rows, w.cols))
+    out, ldo = _like("out", out, rows, w.rows, dtype, gpu, x)
+    need = _fp8_bytes("chgnet_fp8_linear_workspace", rows, w.rows, k)
+    p, nbytes, _keep = _workspace(ws, need, gpu, x) if need else (None, 0, None)
+    _call(lib().chgnet_fp8_linear, gpu, (rows, code, x.data_ptr(), ldx, ctypes.byref(w._c), out.data_ptr(), ldo, p, nbytes))
+    return out
