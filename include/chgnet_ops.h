@@ -165,7 +165,8 @@ int chgnet_dropout(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_
  * Codes of a row follow each other, rows are ld bytes apart (a multiple of 16, on
  * 16-byte boundaries); where cols is no multiple of 16 the bytes up to the next one
  * are 0 (chgnet_fp8_quantize writes them). Scale rows are ld_scale bytes apart (a
- * multiple of 4, on 4-byte boundaries). rows < 2^31, 0 <= cols <= 2^23. */
+ * multiple of 4, on 4-byte boundaries). Strides are at most 2^23, rows < 2^31, 0 <=
+ * cols <= 2^23. */
 typedef struct chgnet_fp8 {
   int64_t rows, cols;
   uint8_t* codes;

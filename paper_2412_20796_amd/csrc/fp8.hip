@@ -239,9 +239,20 @@ struct ProductArgs {
 
 __device__ __align__(16) const uint8_t kZeros[16] = {};
 
+// 16 or 4 bytes a lane past the registers: to `l` and the lanes' places behind it
+__device__ __forceinline__ void to_lds16(const void* g, void* l) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g,
+                                   (__attribute__((address_space(3))) void*)l, 16, 0, 0);
+}
+__device__ __forceinline__ void to_lds4(const void* g, void* l) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g,
+                                   (__attribute__((address_space(3))) void*)l, 4, 0, 0);
+}
+
 // a lane's 32 codes as bf16 values, times their scale
-__device__ __forceinline__ void wide(const v8i& q, int byte, v8b (&v)[4]) {
-  const float s = byte == 255 ? __builtin_nanf("") : __uint_as_float(byte ? (unsigned)byte << 23 : 0x400000u);
+__device__ __forceinline__ void wide(const v8i& q, unsigned word, v8b (&v)[4]) {
+  const unsigned byte = word & 255;
+  const float s = byte == 255 ? __builtin_nanf("") : __uint_as_float(byte ? byte << 23 : 0x400000u);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i], s, false);
@@ -282,6 +293,7 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
   constexpr int THREADS = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   constexpr int PIECES = (BM + BN) * 8 / THREADS;  // of 16 bytes, a thread
   __shared__ __align__(1024) uint8_t lds[2][(BM + BN) * kBlock];
+  __shared__ unsigned words[2][BM + BN];
   const int64_t M = p.a.rows, N = p.b.rows;
   const int64_t tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
   // tiles: each of the 8 chiplets has a run of them, in groups of 8 rows of tiles
@@ -304,44 +316,54 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
   const int64_t kb0 = (int64_t)blockIdx.y * p.kb_split;
   const int64_t kb1 = kb0 + p.kb_split < nkb ? kb0 + p.kb_split : nkb;
 
-  // addresses of this thread's pieces: rows past the end are the last one again
-  const uint8_t* src[PIECES];
-  int piece[PIECES];
+  // this thread's pieces, as offsets from the tile's first rows: rows past the
+  // end are the last one again
+  constexpr int A_PIECES = BM * 8 / THREADS;
+  static_assert(BM * 8 % THREADS == 0 && BN * 8 % THREADS == 0, "a step's pieces are of one factor");
+  static_assert(BM + BN <= 2 * THREADS, "a word of scales a thread and step");
+  const int last_a = (int)(M - m0 < BM ? M - m0 : BM) - 1, last_b = (int)(N - n0 < BN ? N - n0 : BN) - 1;
+  const uint8_t *const codes_a = p.a.codes + m0 * p.a.ldc, *const codes_b = p.b.codes + n0 * p.b.ldc;
+  unsigned src[PIECES];
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
-    const int t = i * THREADS + threadIdx.x, row = t >> 3;
-    piece[i] = (t & 7) ^ (row & 7);
-    const bool is_a = row < BM;
-    const int64_t r = is_a ? m0 + row : n0 + row - BM, last = is_a ? M - 1 : N - 1;
-    const Factor& f = is_a ? p.a : p.b;
-    src[i] = f.codes + (r < last ? r : last) * f.ldc + 16 * piece[i];
+    const int row = (i * THREADS + threadIdx.x) / 8 - (i < A_PIECES ? 0 : BM), last = i < A_PIECES ? last_a : last_b;
+    src[i] = (unsigned)(row < last ? row : last) * (unsigned)(i < A_PIECES ? p.a.ldc : p.b.ldc);
   }
+  const unsigned piece = 16 * ((threadIdx.x & 7) ^ (threadIdx.x >> 3 & 7));
   auto fetch = [&](int64_t kb, int buf) {
     const int64_t at = kb * kBlock;
-    const int64_t left = p.K - at;
+    uint8_t* to = lds[buf] + wave * 1024;
+    if (at + piece < p.K) {  // (pieces past the end of K are zeros)
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const uint8_t* s = src[i] + at;
-      if (left < kBlock && 16 * piece[i] >= left) s = kZeros;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)s,
-                                       (__attribute__((address_space(3))) void*)(lds[buf] + (i * THREADS + wave * 64) * 16), 16,
-                                       0, 0);
+      for (int i = 0; i < PIECES; ++i)
+        to_lds16((i < A_PIECES ? codes_a : codes_b) + at + (src[i] + piece), to + i * THREADS * 16);
+    }
+    if (at + kBlock > p.K && at + piece >= p.K) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i)
+        *reinterpret_cast<uint4*>(to + i * THREADS * 16 + (threadIdx.x & 63) * 16) = make_uint4(0, 0, 0, 0);
+    }
+  };
+  // scales: a word has a row's bytes of four blocks of K
+  const int64_t sm0 = m0 >> p.a.shift, sn0 = n0 >> p.b.shift;
+  unsigned word_src[(BM + BN) / THREADS];
+#pragma unroll
+  for (int i = 0; i < (BM + BN) / THREADS; ++i) {
+    const int row = i * THREADS + threadIdx.x;
+    const bool is_a = row < BM;
+    const Factor& f = is_a ? p.a : p.b;
+    const int r = is_a ? row : row - BM, last = is_a ? last_a : last_b;
+    word_src[i] = (unsigned)((((is_a ? m0 : n0) + (r < last ? r : last)) >> f.shift) - (is_a ? sm0 : sn0)) * (unsigned)f.lds;
+  }
+  auto fetch_scales = [&](int64_t kb, int buf) {
+#pragma unroll
+    for (int i = 0; i < (BM + BN) / THREADS; ++i) {
+      const uint8_t* base = (i * THREADS + wave * 64 < BM ? p.a.scale + sm0 * p.a.lds : p.b.scale + sn0 * p.b.lds) + kb;
+      to_lds4(base + word_src[i], words[buf] + i * THREADS + wave * 64);
     }
   };
   const int r16 = lane & 15, g = lane >> 4;
-  // scale words: row's bytes of four blocks of K
-  const uint8_t* sa[TM];
-  const uint8_t* sb[TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int64_t r = m0 + wm + 16 * i + r16;
-    sa[i] = p.a.scale + ((r < M ? r : M - 1) >> p.a.shift) * p.a.lds;
-  }
-#pragma unroll
-  for (int i = 0; i < TN; ++i) {
-    const int64_t r = n0 + wn + 16 * i + r16;
-    sb[i] = p.b.scale + ((r < N ? r : N - 1) >> p.b.shift) * p.b.lds;
-  }
+  unsigned ea[TM], eb[TN];
   v4f acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -353,15 +375,26 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
     const v4i b = *reinterpret_cast<const v4i*>(q + (((2 * g + 1) ^ (r16 & 7)) * 16));
     return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   };
-  if (kb0 < kb1) fetch(kb0, 0);
+  if (kb0 < kb1) {
+    fetch_scales(kb0, 0);
+    fetch(kb0, 0);
+  }
   for (int64_t kb = kb0; kb < kb1; ++kb) {
-    const int buf = (int)(kb - kb0) & 1;
-    int ea[TM], eb[TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) ea[i] = sa[i][kb];
-#pragma unroll
-    for (int j = 0; j < TN; ++j) eb[j] = sb[j][kb];
+    const int i = (int)(kb - kb0), buf = i & 1;
     __syncthreads();  // the codes are there, and the other buffer is read
+    if ((i & 3) == 0) {
+      const unsigned* w = words[i >> 2 & 1];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) ea[i] = w[wm + 16 * i + r16];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) eb[j] = w[BM + wn + 16 * j + r16];
+      if (kb + 4 < kb1) fetch_scales(kb + 4, (i >> 2 & 1) ^ 1);
+    } else {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) ea[i] >>= 8;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) eb[j] >>= 8;
+    }
     if (kb + 1 < kb1) fetch(kb + 1, buf ^ 1);
     if constexpr (EXACT) {
       v8b bf[TN][4];
@@ -435,9 +468,10 @@ int check_factor(const char* who, const chgnet_fp8* f, bool there) {
   if (f->rows < 0 || f->rows >= kMostRows) return bad(who, "rows must be in 0 .. 2^31 - 1");
   if (f->cols < 0 || f->cols > kMostK) return bad(who, "columns must be in 0 .. 2^23");
   if (f->block_rows != 1 && f->block_rows != kBlock) return bad(who, "block_rows must be 1 or 128");
-  if (f->ld < cdiv(f->cols, 16) * 16 || f->ld % 16) return bad(who, "ld must be a multiple of 16 that holds the columns");
-  if (f->ld_scale < cdiv(f->cols, kBlock) || f->ld_scale % 4)
-    return bad(who, "ld_scale must be a multiple of 4 that holds a byte for each 128 columns");
+  if (f->ld < cdiv(f->cols, 16) * 16 || f->ld % 16 || f->ld > kMostK)
+    return bad(who, "ld must be a multiple of 16 that holds the columns, at most 2^23");
+  if (f->ld_scale < cdiv(f->cols, kBlock) || f->ld_scale % 4 || f->ld_scale > kMostK)
+    return bad(who, "ld_scale must be a multiple of 4 that holds a byte for each 128 columns, at most 2^23");
   if (there && f->cols > 0 && (!f->codes || !f->scale)) return bad(who, "null argument");
   if (!aligned_to(f->codes, 16) || !aligned_to(f->scale, 4)) return bad(who, "codes must be 16-byte, scale 4-byte aligned");
   return CHGNET_OK;
@@ -447,14 +481,17 @@ Factor factor(const chgnet_fp8* f) {
 }
 
 struct Plan {
+  bool large;  // tiles of 256 x 256 and not of 128 x 128
+  int64_t tiles;
   int splits, kb_split;
 };
 // Splits of K: where the tiles are fewer than the compute units
 Plan plan(int64_t M, int64_t N, int64_t K) {
-  const int64_t tiles = cdiv(M, 128) * cdiv(N, 128), nkb = std::max<int64_t>(1, cdiv(K, kBlock));
+  const bool large = cdiv(M, 256) * cdiv(N, 256) >= 256;
+  const int64_t t = large ? 256 : 128, tiles = cdiv(M, t) * cdiv(N, t), nkb = std::max<int64_t>(1, cdiv(K, kBlock));
   int64_t s = tiles >= 256 ? 1 : std::min<int64_t>(cdiv(512, tiles), std::max<int64_t>(1, nkb / 4));
-  const int64_t per = cdiv(nkb, s);
-  return {(int)cdiv(nkb, per), (int)per};
+  const int64_t per = cdiv(cdiv(nkb, s), 4) * 4;  // (of whole words of scales)
+  return {large, tiles, (int)cdiv(nkb, per), (int)per};
 }
 
 }  // namespace
@@ -539,18 +576,19 @@ int fp8_matmul_entry(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, vo
   const Plan pl = plan(M, N, K);
   ProductArgs p{factor(a), factor(b), K, out, ldout, pl.splits > 1 ? static_cast<float*>(ws) : nullptr, pl.kb_split,
                 accumulate != 0};
-  const int64_t tiles = cdiv(M, 128) * cdiv(N, 128);
-  if (tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles of 128 x 128");
+  if (pl.tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles of 256 x 256");
   return with_type(dtype, [&](auto v) -> int {
     using T = decltype(v);
     constexpr bool exact = std::is_same<T, float>::value;
+    const dim3 grid((unsigned)pl.tiles, pl.splits);
     if (pl.splits > 1) {
-      KLAUNCH(st, "k_fp8_product",
-              k_fp8_product<float, exact, 128, 128, 2, 2><<<dim3((unsigned)tiles, pl.splits), 256, 0, st>>>(p));
+      KLAUNCH(st, "k_fp8_product", k_fp8_product<float, exact, 128, 128, 2, 2><<<grid, 256, 0, st>>>(p));
       KLAUNCH(st, "k_fp8_join", k_fp8_join<T><<<(unsigned)std::min<int64_t>(2048, cdiv(M * N, 256)), 256, 0, st>>>(
                                     M, N, pl.splits, p.part, static_cast<T*>(out), ldout, p.add));
+    } else if (pl.large) {
+      KLAUNCH(st, "k_fp8_product", k_fp8_product<T, exact, 256, 256, 2, 4><<<grid, 512, 0, st>>>(p));
     } else {
-      KLAUNCH(st, "k_fp8_product", k_fp8_product<T, exact, 128, 128, 2, 2><<<dim3((unsigned)tiles, 1), 256, 0, st>>>(p));
+      KLAUNCH(st, "k_fp8_product", k_fp8_product<T, exact, 128, 128, 2, 2><<<grid, 256, 0, st>>>(p));
     }
     return CHGNET_OK;
   });
