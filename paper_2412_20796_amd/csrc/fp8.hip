@@ -237,8 +237,6 @@ struct ProductArgs {
   int add;
 };
 
-__device__ __align__(16) const uint8_t kZeros[16] = {};
-
 // 16 or 4 bytes a lane past the registers: to `l` and the lanes' places behind it
 __device__ __forceinline__ void to_lds16(const void* g, void* l) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g,
@@ -249,45 +247,54 @@ __device__ __forceinline__ void to_lds4(const void* g, void* l) {
                                    (__attribute__((address_space(3))) void*)l, 4, 0, 0);
 }
 
-// a lane's 32 codes as bf16 values, times their scale
-__device__ __forceinline__ void wide(const v8i& q, unsigned word, v8b (&v)[4]) {
+// 8 codes as bf16 values, times their scale
+__device__ __forceinline__ v8b wide(const uint2& q, float s) {
+  const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.x, s, false);
+  const v2b b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.x, s, true);
+  const v2b c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.y, s, false);
+  const v2b d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.y, s, true);
+  return v8b{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// 2^(byte - 127) for the low byte of a word
+__device__ __forceinline__ float scale_value(unsigned word) {
   const unsigned byte = word & 255;
-  const float s = byte == 255 ? __builtin_nanf("") : __uint_as_float(byte ? byte << 23 : 0x400000u);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i], s, false);
-    const v2b b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i], s, true);
-    const v2b c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + 1], s, false);
-    const v2b d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + 1], s, true);
-    v[i] = v8b{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-  }
+  return byte == 255 ? __builtin_nanf("") : __uint_as_float(byte ? byte << 23 : 0x400000u);
 }
 
+// 16 results of a row, of which the first `left` are the matrix's
 template <class T>
-__device__ __forceinline__ void put4(T* p, const v4f& v, int64_t n, int64_t N, bool vec, bool add) {
-  float t[4] = {v[0], v[1], v[2], v[3]};
-  if (vec && n + 4 <= N) {
-    if (add) {
-      float o[4];
-      load_v<4>(p, o);
+__device__ __forceinline__ void put16(T* p, const v4f (&v)[4], int64_t left, bool vec, bool add) {
+  constexpr int W = 16 / sizeof(T);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) t[k] += o[k];
+  for (int q = 0; q < 16 / W; ++q) {
+    float t[W];
+#pragma unroll
+    for (int k = 0; k < W; ++k) t[k] = v[(q * W + k) / 4][k % 4];
+    if (vec) {
+      if (add) {
+        float o[W];
+        load_v<W>(p + q * W, o);
+#pragma unroll
+        for (int k = 0; k < W; ++k) t[k] += o[k];
+      }
+      store_v<W>(p + q * W, t);
+    } else {
+#pragma unroll
+      for (int k = 0; k < W; ++k)
+        if (q * W + k < left) p[q * W + k] = (T)(add ? (float)p[q * W + k] + t[k] : t[k]);
     }
-    store_v<4>(p, t);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (n + k < N) p[k] = (T)(add ? (float)p[k] + t[k] : t[k]);
   }
 }
 
 // A block has BM x BN results, its WM x WN wavefronts equal parts of them. Both
 // factors' codes of 128 values of K go to LDS past the registers, the next ones
-// while the present are multiplied; a row's 8 pieces of 16 bytes sit at piece ^
-// (row % 8), so that the lanes of a load meet in no bank. The factors change
-// places in the instruction, so that a lane has four results of a row.
-// EXACT: products of bf16 values. Which of a block's 128 values an instruction
-// multiplies is any order that both factors share: a lane's bytes 8 s .. 8 s + 7.
+// while the present are multiplied. The factors change places in the instruction,
+// and column 16 g + 4 j + i of a wavefront's 64 is row 4 g + i of its j-th
+// operand, so that lane group g ends with 16 results of a row, one after another.
+// A row's 8 pieces of 16 bytes sit at piece ^ key(row), the keys such that the 16
+// rows of an operand meet in no bank: 16 lanes read 256 bytes, two rows, at a
+// time (with keys of row % 8 a load took twice as long: 8192^3 463 us).
+// EXACT: products of bf16 values, 32 of a block's 128 at a time.
 template <class T, bool EXACT, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(ProductArgs p) {
   constexpr int THREADS = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
@@ -329,19 +336,25 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
     const int row = (i * THREADS + threadIdx.x) / 8 - (i < A_PIECES ? 0 : BM), last = i < A_PIECES ? last_a : last_b;
     src[i] = (unsigned)(row < last ? row : last) * (unsigned)(i < A_PIECES ? p.a.ldc : p.b.ldc);
   }
-  const unsigned piece = 16 * ((threadIdx.x & 7) ^ (threadIdx.x >> 3 & 7));
+  auto piece = [&](int i) -> unsigned {
+    const unsigned key = i < A_PIECES ? threadIdx.x >> 4 & 7 : (threadIdx.x >> 4 & 1) | (i * (THREADS / 128) + (threadIdx.x >> 7) & 3) << 1;
+    return 16 * ((threadIdx.x & 7) ^ key);
+  };
   auto fetch = [&](int64_t kb, int buf) {
     const int64_t at = kb * kBlock;
     uint8_t* to = lds[buf] + wave * 1024;
-    if (at + piece < p.K) {  // (pieces past the end of K are zeros)
+    if (at + kBlock <= p.K) {
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
-        to_lds16((i < A_PIECES ? codes_a : codes_b) + at + (src[i] + piece), to + i * THREADS * 16);
-    }
-    if (at + kBlock > p.K && at + piece >= p.K) {
+        to_lds16((i < A_PIECES ? codes_a : codes_b) + at + (src[i] + piece(i)), to + i * THREADS * 16);
+    } else {  // pieces past the end of K are zeros
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i)
-        *reinterpret_cast<uint4*>(to + i * THREADS * 16 + (threadIdx.x & 63) * 16) = make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < PIECES; ++i) {
+        if (at + piece(i) < p.K)
+          to_lds16((i < A_PIECES ? codes_a : codes_b) + at + (src[i] + piece(i)), to + i * THREADS * 16);
+        else
+          *reinterpret_cast<uint4*>(to + i * THREADS * 16 + (threadIdx.x & 63) * 16) = make_uint4(0, 0, 0, 0);
+      }
     }
   };
   // scales: a word has a row's bytes of four blocks of K
@@ -369,12 +382,17 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-  auto fragment = [&](const uint8_t* base, int row) {
-    const uint8_t* q = base + (row + r16) * kBlock;
-    const v4i a = *reinterpret_cast<const v4i*>(q + (((2 * g) ^ (r16 & 7)) * 16));
-    const v4i b = *reinterpret_cast<const v4i*>(q + (((2 * g + 1) ^ (r16 & 7)) * 16));
-    return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  // half h of a lane's 32 codes of an operand: piece g + 4 h of its row
+  static_assert(TN == 4, "64 columns a wavefront");
+  const int col16 = (r16 >> 2) * 16 + (r16 & 3);  // + 4 j
+  const int key_a = r16 >> 1, key_b = (r16 >> 1 & 1) | (r16 >> 2) << 1;
+  auto half_a = [&](int buf, int i, int h) {
+    return *reinterpret_cast<const v4i*>(lds[buf] + (wm + 16 * i + r16) * kBlock + ((g + 4 * h) ^ key_a) * 16);
   };
+  auto half_b = [&](int buf, int j, int h) {
+    return *reinterpret_cast<const v4i*>(lds[buf] + (BM + wn + col16 + 4 * j) * kBlock + ((g + 4 * h) ^ key_b) * 16);
+  };
+  auto whole = [](const v4i& a, const v4i& b) { return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; };
   if (kb0 < kb1) {
     fetch_scales(kb0, 0);
     fetch(kb0, 0);
@@ -387,7 +405,7 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
 #pragma unroll
       for (int i = 0; i < TM; ++i) ea[i] = w[wm + 16 * i + r16];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) eb[j] = w[BM + wn + 16 * j + r16];
+      for (int j = 0; j < TN; ++j) eb[j] = w[BM + wn + col16 + 4 * j];
       if (kb + 4 < kb1) fetch_scales(kb + 4, (i >> 2 & 1) ^ 1);
     } else {
 #pragma unroll
@@ -396,48 +414,68 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
       for (int j = 0; j < TN; ++j) eb[j] >>= 8;
     }
     if (kb + 1 < kb1) fetch(kb + 1, buf ^ 1);
+    // operands of a are loaded AHEAD of their products
     if constexpr (EXACT) {
-      v8b bf[TN][4];
+      constexpr int AHEAD = 2;
 #pragma unroll
-      for (int j = 0; j < TN; ++j) wide(fragment(lds[buf] + BM * kBlock, wn + 16 * j), eb[j], bf[j]);
+      for (int h = 0; h < 2; ++h) {
+        v4i a[AHEAD + 1], b[TN];
+        v8b bw[TN][2];
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        v8b af[4];
-        wide(fragment(lds[buf], wm + 16 * i), ea[i], af);
+        for (int j = 0; j < TN; ++j) b[j] = half_b(buf, j, h);
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+        for (int i = 0; i < AHEAD; ++i) a[i] = half_a(buf, i, h);
 #pragma unroll
-          for (int s = 0; s < 4; ++s)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[j][s], af[s], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < TN; ++j) {
+          bw[j][0] = wide(make_uint2(b[j][0], b[j][1]), scale_value(eb[j]));
+          bw[j][1] = wide(make_uint2(b[j][2], b[j][3]), scale_value(eb[j]));
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          if (i + AHEAD < TM) a[(i + AHEAD) % (AHEAD + 1)] = half_a(buf, i + AHEAD, h);
+          const v4i q = a[i % (AHEAD + 1)];
+          const v8b w0 = wide(make_uint2(q[0], q[1]), scale_value(ea[i]));
+          const v8b w1 = wide(make_uint2(q[2], q[3]), scale_value(ea[i]));
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][0], w0, acc[i][j], 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][1], w1, acc[i][j], 0, 0, 0);
+        }
       }
     } else {
-      v8i bf[TN];
+      constexpr int AHEAD = 2;
+      v8i a[AHEAD + 1], b[TN];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) bf[j] = fragment(lds[buf] + BM * kBlock, wn + 16 * j);
+      for (int j = 0; j < TN; ++j) b[j] = whole(half_b(buf, j, 0), half_b(buf, j, 1));
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) a[i] = whole(half_a(buf, i, 0), half_a(buf, i, 1));
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 * (TN + AHEAD), 0);
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        const v8i af = fragment(lds[buf], wm + 16 * i);
+        if (i + AHEAD < TM) {
+          a[(i + AHEAD) % (AHEAD + 1)] = whole(half_a(buf, i + AHEAD, 0), half_a(buf, i + AHEAD, 1));
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bf[j], af, acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i % (AHEAD + 1)], acc[i][j], 0, 0, 0, eb[j], 0,
+                                                                       ea[i]);
+        __builtin_amdgcn_sched_group_barrier(0x8, TN, 0);
       }
     }
   }
+  const int64_t n = n0 + wn + 16 * g;
+  auto results = [&](auto* out, int64_t ld, bool add) {
+    using O = std::remove_pointer_t<decltype(out)>;
+    const bool vec = n + 16 <= N && (ld * sizeof(O) & 15) == 0 && ((uintptr_t)out & 15) == 0;
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int64_t m = m0 + wm + 16 * i + r16;
-    if (m >= M) continue;
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int64_t n = n0 + wn + 16 * j + 4 * g;
-      if (p.part) {
-        put4(p.part + ((int64_t)blockIdx.y * M + m) * N + n, acc[i][j], n, N, (N & 3) == 0, false);
-      } else {
-        T* o = static_cast<T*>(p.out) + m * p.ldo + n;
-        put4(o, acc[i][j], n, N, (p.ldo & 3) == 0 && ((uintptr_t)p.out & (4 * sizeof(T) - 1)) == 0, p.add);
-      }
+    for (int i = 0; i < TM; ++i) {
+      const int64_t m = m0 + wm + 16 * i + r16;
+      if (m < M) put16(out + m * ld + n, acc[i], N - n, vec, add);
     }
-  }
+  };
+  if (p.part) results(p.part + (int64_t)blockIdx.y * M * N, N, false);
+  else results(static_cast<T*>(p.out), p.ldo, p.add != 0);
 }
 
 // out (+)= the sum of the splits' parts, in order
