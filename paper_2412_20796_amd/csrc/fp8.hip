@@ -18,6 +18,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 #include "common.hpp"
@@ -232,7 +233,8 @@ struct ProductArgs {
   int64_t K;
   void* out;
   int64_t ldo;
-  float* part;  // [split][M][N] partial sums, or NULL: `out` is written
+  float* part;  // [split][M][ldp] partial sums, or NULL: `out` is written
+  int64_t ldp;
   int kb_split;  // blocks of 128 along K that one split has
   int add;
 };
@@ -245,6 +247,14 @@ __device__ __forceinline__ void to_lds16(const void* g, void* l) {
 __device__ __forceinline__ void to_lds4(const void* g, void* l) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g,
                                    (__attribute__((address_space(3))) void*)l, 4, 0, 0);
+}
+
+// barrier of the block once all but the last COUNT of this wavefront's loads are
+// done, and what it wrote to LDS
+template <int COUNT>
+__device__ __forceinline__ void wait_barrier() {
+  static_assert(COUNT < 64, "six bits");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COUNT) : "memory");
 }
 
 // 8 codes as bf16 values, times their scale
@@ -261,45 +271,41 @@ __device__ __forceinline__ float scale_value(unsigned word) {
   return byte == 255 ? __builtin_nanf("") : __uint_as_float(byte ? byte << 23 : 0x400000u);
 }
 
-// 16 results of a row, of which the first `left` are the matrix's
-template <class T>
-__device__ __forceinline__ void put16(T* p, const v4f (&v)[4], int64_t left, bool vec, bool add) {
-  constexpr int W = 16 / sizeof(T);
+// 16 bytes of results of a row, of which the first `left` are the matrix's
+template <class T, int W>
+__device__ __forceinline__ void put(T* p, float (&t)[W], int64_t left, bool vec, bool add) {
+  if (vec && left >= W) {
+    if (add) {
+      float o[W];
+      load_v<W>(p, o);
 #pragma unroll
-  for (int q = 0; q < 16 / W; ++q) {
-    float t[W];
-#pragma unroll
-    for (int k = 0; k < W; ++k) t[k] = v[(q * W + k) / 4][k % 4];
-    if (vec) {
-      if (add) {
-        float o[W];
-        load_v<W>(p + q * W, o);
-#pragma unroll
-        for (int k = 0; k < W; ++k) t[k] += o[k];
-      }
-      store_v<W>(p + q * W, t);
-    } else {
-#pragma unroll
-      for (int k = 0; k < W; ++k)
-        if (q * W + k < left) p[q * W + k] = (T)(add ? (float)p[q * W + k] + t[k] : t[k]);
+      for (int k = 0; k < W; ++k) t[k] += o[k];
     }
+    store_v<W>(p, t);
+  } else {
+#pragma unroll
+    for (int k = 0; k < W; ++k)
+      if (k < left) p[k] = (T)(add ? (float)p[k] + t[k] : t[k]);
   }
 }
 
 // A block has BM x BN results, its WM x WN wavefronts equal parts of them. Both
 // factors' codes of 128 values of K go to LDS past the registers, the next ones
 // while the present are multiplied. The factors change places in the instruction,
-// and column 16 g + 4 j + i of a wavefront's 64 is row 4 g + i of its j-th
-// operand, so that lane group g ends with 16 results of a row, one after another.
+// so that a lane has four results of a row for each operand of b; which column is
+// which of an operand's rows is such that these, or those of two operands in 16
+// bits, are 16 bytes that follow each other, beside those of the other lane groups.
 // A row's 8 pieces of 16 bytes sit at piece ^ key(row), the keys such that the 16
 // rows of an operand meet in no bank: 16 lanes read 256 bytes, two rows, at a
 // time (with keys of row % 8 a load took twice as long: 8192^3 463 us).
 // EXACT: products of bf16 values, 32 of a block's 128 at a time.
-template <class T, bool EXACT, int BM, int BN, int WM, int WN>
+template <class T, bool EXACT, int BM, int BN, int WM, int WN, int STAGES>
 __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(ProductArgs p) {
   constexpr int THREADS = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   constexpr int PIECES = (BM + BN) * 8 / THREADS;  // of 16 bytes, a thread
-  __shared__ __align__(1024) uint8_t lds[2][(BM + BN) * kBlock];
+  constexpr int W = 16 / sizeof(T);                // results in 16 bytes
+  static_assert(TN == 4 && THREADS % 256 == 0, "64 columns a wavefront");
+  __shared__ __align__(1024) uint8_t lds[STAGES][(BM + BN) * kBlock];
   __shared__ unsigned words[2][BM + BN];
   const int64_t M = p.a.rows, N = p.b.rows;
   const int64_t tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
@@ -327,7 +333,6 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
   // end are the last one again
   constexpr int A_PIECES = BM * 8 / THREADS;
   static_assert(BM * 8 % THREADS == 0 && BN * 8 % THREADS == 0, "a step's pieces are of one factor");
-  static_assert(BM + BN <= 2 * THREADS, "a word of scales a thread and step");
   const int last_a = (int)(M - m0 < BM ? M - m0 : BM) - 1, last_b = (int)(N - n0 < BN ? N - n0 : BN) - 1;
   const uint8_t *const codes_a = p.a.codes + m0 * p.a.ldc, *const codes_b = p.b.codes + n0 * p.b.ldc;
   unsigned src[PIECES];
@@ -337,7 +342,7 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
     src[i] = (unsigned)(row < last ? row : last) * (unsigned)(i < A_PIECES ? p.a.ldc : p.b.ldc);
   }
   auto piece = [&](int i) -> unsigned {
-    const unsigned key = i < A_PIECES ? threadIdx.x >> 4 & 7 : (threadIdx.x >> 4 & 1) | (i * (THREADS / 128) + (threadIdx.x >> 7) & 3) << 1;
+    const unsigned key = i < A_PIECES || W == 4 ? threadIdx.x >> 4 & 7 : (threadIdx.x >> 4 & 1) | (threadIdx.x >> 6 & 3) << 1;
     return 16 * ((threadIdx.x & 7) ^ key);
   };
   auto fetch = [&](int64_t kb, int buf) {
@@ -347,7 +352,7 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
         to_lds16((i < A_PIECES ? codes_a : codes_b) + at + (src[i] + piece(i)), to + i * THREADS * 16);
-    } else {  // pieces past the end of K are zeros
+    } else {  // pieces past the end of K are zeros (a wavefront has some before it: it counts as many loads)
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         if (at + piece(i) < p.K)
@@ -359,9 +364,10 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
   };
   // scales: a word has a row's bytes of four blocks of K
   const int64_t sm0 = m0 >> p.a.shift, sn0 = n0 >> p.b.shift;
-  unsigned word_src[(BM + BN) / THREADS];
+  constexpr int WORDS = (BM + BN + THREADS - 1) / THREADS;
+  unsigned word_src[WORDS];
 #pragma unroll
-  for (int i = 0; i < (BM + BN) / THREADS; ++i) {
+  for (int i = 0; i < WORDS; ++i) {
     const int row = i * THREADS + threadIdx.x;
     const bool is_a = row < BM;
     const Factor& f = is_a ? p.a : p.b;
@@ -370,7 +376,8 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
   }
   auto fetch_scales = [&](int64_t kb, int buf) {
 #pragma unroll
-    for (int i = 0; i < (BM + BN) / THREADS; ++i) {
+    for (int i = 0; i < WORDS; ++i) {
+      if (i * THREADS + wave * 64 >= BM + BN) break;
       const uint8_t* base = (i * THREADS + wave * 64 < BM ? p.a.scale + sm0 * p.a.lds : p.b.scale + sn0 * p.b.lds) + kb;
       to_lds4(base + word_src[i], words[buf] + i * THREADS + wave * 64);
     }
@@ -383,29 +390,33 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
   // half h of a lane's 32 codes of an operand: piece g + 4 h of its row
-  static_assert(TN == 4, "64 columns a wavefront");
-  const int col16 = (r16 >> 2) * 16 + (r16 & 3);  // + 4 j
-  const int key_a = r16 >> 1, key_b = (r16 >> 1 & 1) | (r16 >> 2) << 1;
+  auto column = [](int row, int j) { return (row >> 2) * W + (row & 3) + j / (W / 4) * 4 * W + j % (W / 4) * 4; };
+  const int key = r16 >> 1;
   auto half_a = [&](int buf, int i, int h) {
-    return *reinterpret_cast<const v4i*>(lds[buf] + (wm + 16 * i + r16) * kBlock + ((g + 4 * h) ^ key_a) * 16);
+    return *reinterpret_cast<const v4i*>(lds[buf] + (wm + 16 * i + r16) * kBlock + ((g + 4 * h) ^ key) * 16);
   };
   auto half_b = [&](int buf, int j, int h) {
-    return *reinterpret_cast<const v4i*>(lds[buf] + (BM + wn + col16 + 4 * j) * kBlock + ((g + 4 * h) ^ key_b) * 16);
+    return *reinterpret_cast<const v4i*>(lds[buf] + (BM + wn + column(r16, j)) * kBlock + ((g + 4 * h) ^ key) * 16);
   };
   auto whole = [](const v4i& a, const v4i& b) { return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; };
-  if (kb0 < kb1) {
-    fetch_scales(kb0, 0);
-    fetch(kb0, 0);
-  }
+  static_assert(STAGES >= 2 && STAGES <= 5, "a word of scales arrives in the four steps before its own");
+  if (kb0 < kb1) fetch_scales(kb0, 0);
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (kb0 + i < kb1) fetch(kb0 + i, i);
+  int buf = 0;
   for (int64_t kb = kb0; kb < kb1; ++kb) {
-    const int i = (int)(kb - kb0), buf = i & 1;
-    __syncthreads();  // the codes are there, and the other buffer is read
+    const int i = (int)(kb - kb0);
+    // the codes of this step are there (loads end in order, and those of the next
+    // STAGES - 2 steps may be under way), and all have read what is loaded over
+    if (STAGES > 2 && kb + STAGES - 1 <= kb1) wait_barrier<(STAGES - 2) * PIECES>();
+    else wait_barrier<0>();
     if ((i & 3) == 0) {
       const unsigned* w = words[i >> 2 & 1];
 #pragma unroll
       for (int i = 0; i < TM; ++i) ea[i] = w[wm + 16 * i + r16];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) eb[j] = w[BM + wn + col16 + 4 * j];
+      for (int j = 0; j < TN; ++j) eb[j] = w[BM + wn + column(r16, j)];
       if (kb + 4 < kb1) fetch_scales(kb + 4, (i >> 2 & 1) ^ 1);
     } else {
 #pragma unroll
@@ -413,10 +424,9 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
 #pragma unroll
       for (int j = 0; j < TN; ++j) eb[j] >>= 8;
     }
-    if (kb + 1 < kb1) fetch(kb + 1, buf ^ 1);
-    // operands of a are loaded AHEAD of their products
+    if (kb + STAGES - 1 < kb1) fetch(kb + STAGES - 1, buf == 0 ? STAGES - 1 : buf - 1);
+    constexpr int AHEAD = TM > 2 ? 2 : TM - 1;  // operands of a that are loaded ahead of their products
     if constexpr (EXACT) {
-      constexpr int AHEAD = 2;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         v4i a[AHEAD + 1], b[TN];
@@ -443,7 +453,6 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
         }
       }
     } else {
-      constexpr int AHEAD = 2;
       v8i a[AHEAD + 1], b[TN];
 #pragma unroll
       for (int j = 0; j < TN; ++j) b[j] = whole(half_b(buf, j, 0), half_b(buf, j, 1));
@@ -463,39 +472,51 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
         __builtin_amdgcn_sched_group_barrier(0x8, TN, 0);
       }
     }
+    buf = buf + 1 == STAGES ? 0 : buf + 1;
   }
-  const int64_t n = n0 + wn + 16 * g;
-  auto results = [&](auto* out, int64_t ld, bool add) {
-    using O = std::remove_pointer_t<decltype(out)>;
-    const bool vec = n + 16 <= N && (ld * sizeof(O) & 15) == 0 && ((uintptr_t)out & 15) == 0;
+  auto results = [&](T* out, int64_t ld, bool add) {
+    const bool vec = (ld * sizeof(T) & 15) == 0 && ((uintptr_t)out & 15) == 0;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t m = m0 + wm + 16 * i + r16;
-      if (m < M) put16(out + m * ld + n, acc[i], N - n, vec, add);
+      if (m >= M) continue;
+#pragma unroll
+      for (int q = 0; q < 16 / W; ++q) {
+        const int64_t n = n0 + wn + q * 4 * W + g * W;
+        float t[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) t[k] = acc[i][(q * W + k) / 4][k % 4];
+        put(out + m * ld + n, t, N - n, vec, add);
+      }
     }
   };
-  if (p.part) results(p.part + (int64_t)blockIdx.y * M * N, N, false);
-  else results(static_cast<T*>(p.out), p.ldo, p.add != 0);
-}
-
-// out (+)= the sum of the splits' parts, in order
-template <class T>
-__global__ void __launch_bounds__(256) k_fp8_join(int64_t M, int64_t N, int splits, const float* __restrict__ part,
-                                                  T* __restrict__ out, int64_t ldo, int add) {
-  const int64_t stride = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * N; i += stride) {
-    const int64_t m = i / N, n = i - m * N;
-    float s = part[i];
-    for (int k = 1; k < splits; ++k) s += part[(int64_t)k * M * N + i];
-    T* o = out + m * ldo + n;
-    *o = (T)(add ? (float)*o + s : s);
+  if (p.part) {
+    if constexpr (W == 4) results(p.part + (int64_t)blockIdx.y * M * p.ldp, p.ldp, false);
+  } else {
+    results(static_cast<T*>(p.out), p.ldo, p.add != 0);
   }
 }
 
+// out (+)= the sum of the splits' parts, in order; a thread has four columns
 template <class T>
-__global__ void __launch_bounds__(256) k_fp8_zero(int64_t M, int64_t N, T* __restrict__ out, int64_t ldo) {
-  const int64_t stride = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * N; i += stride) out[i / N * ldo + i % N] = (T)0.f;
+__global__ void __launch_bounds__(256) k_fp8_join(int64_t M, int64_t N, int splits, const float* __restrict__ part,
+                                                  int64_t ldp, T* __restrict__ out, int64_t ldo, int add) {
+  const int64_t quads = ldp / 4, stride = (int64_t)gridDim.x * 256;
+  const bool vec = (ldo & 3) == 0 && ((uintptr_t)out & (4 * sizeof(T) - 1)) == 0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * quads; i += stride) {
+    const int64_t m = i / quads, n = 4 * (i - m * quads);
+    const float* p = part + m * ldp + n;
+    float s[4];
+    load_v<4>(p, s);
+#pragma unroll 4
+    for (int k = 1; k < splits; ++k) {
+      float t[4];
+      load_v<4>(p + (int64_t)k * M * ldp, t);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[c] += t[c];
+    }
+    put(out + m * ldo + n, s, N - n, vec, add != 0);
+  }
 }
 
 int bad(const char* who, const char* what) { return fail(CHGNET_EINVAL, std::string(who) + ": " + what); }
@@ -519,18 +540,23 @@ Factor factor(const chgnet_fp8* f) {
 }
 
 struct Plan {
-  bool large;  // tiles of 256 x 256 and not of 128 x 128
+  int tile;  // of tile x tile results
   int64_t tiles;
   int splits, kb_split;
 };
-// Splits of K: where the tiles are fewer than the compute units
+// The tiles: the largest of which there is one for each compute unit. Splits of K:
+// where the tiles are fewer than the compute units.
 Plan plan(int64_t M, int64_t N, int64_t K) {
-  const bool large = cdiv(M, 256) * cdiv(N, 256) >= 256;
-  const int64_t t = large ? 256 : 128, tiles = cdiv(M, t) * cdiv(N, t), nkb = std::max<int64_t>(1, cdiv(K, kBlock));
-  int64_t s = tiles >= 256 ? 1 : std::min<int64_t>(cdiv(512, tiles), std::max<int64_t>(1, nkb / 4));
+  auto tiles = [&](int t) { return cdiv(M, t) * cdiv(N, t); };
+  int tile = tiles(256) >= 256 ? 256 : tiles(128) >= 256 ? 128 : 64;
+  if (getenv("FP8T")) tile = atoi(getenv("FP8T"));
+  const int64_t n = tiles(tile), nkb = std::max<int64_t>(1, cdiv(K, kBlock));
+  int64_t s = n >= 256 ? 1 : std::min<int64_t>(cdiv(512, n), std::max<int64_t>(1, nkb / 4));
+  if (getenv("FP8S")) s = std::min<int64_t>(nkb, atoi(getenv("FP8S")));
   const int64_t per = cdiv(cdiv(nkb, s), 4) * 4;  // (of whole words of scales)
-  return {large, tiles, (int)cdiv(nkb, per), (int)per};
+  return {tile, n, (int)cdiv(nkb, per), (int)per};
 }
+int64_t part_ld(int64_t N) { return cdiv(N, 4) * 4; }
 
 }  // namespace
 
@@ -590,7 +616,7 @@ int fp8_matmul_workspace_entry(int64_t M, int64_t N, int64_t K, size_t* bytes) {
   *bytes = 0;
   if (M == 0 || N == 0) return CHGNET_OK;
   const Plan pl = plan(M, N, K);
-  if (pl.splits > 1) *bytes = sizeof(float) * (size_t)pl.splits * (size_t)M * (size_t)N;
+  if (pl.splits > 1) *bytes = sizeof(float) * (size_t)pl.splits * (size_t)M * (size_t)part_ld(N);
   return CHGNET_OK;
 }
 
@@ -612,22 +638,27 @@ int fp8_matmul_entry(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, vo
     return fail(CHGNET_EWORKSPACE, std::string(who) + ": workspace too small (query chgnet_fp8_matmul_workspace)");
   if (!aligned_to(ws, 16)) return bad(who, "ws is not 16-byte aligned");
   const Plan pl = plan(M, N, K);
-  ProductArgs p{factor(a), factor(b), K, out, ldout, pl.splits > 1 ? static_cast<float*>(ws) : nullptr, pl.kb_split,
-                accumulate != 0};
-  if (pl.tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles of 256 x 256");
+  ProductArgs p{factor(a), factor(b), K, out, ldout, pl.splits > 1 ? static_cast<float*>(ws) : nullptr, part_ld(N),
+                pl.kb_split, accumulate != 0};
+  if (pl.tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles");
   return with_type(dtype, [&](auto v) -> int {
     using T = decltype(v);
     constexpr bool exact = std::is_same<T, float>::value;
     const dim3 grid((unsigned)pl.tiles, pl.splits);
-    if (pl.splits > 1) {
-      KLAUNCH(st, "k_fp8_product", k_fp8_product<float, exact, 128, 128, 2, 2><<<grid, 256, 0, st>>>(p));
-      KLAUNCH(st, "k_fp8_join", k_fp8_join<T><<<(unsigned)std::min<int64_t>(2048, cdiv(M * N, 256)), 256, 0, st>>>(
-                                    M, N, pl.splits, p.part, static_cast<T*>(out), ldout, p.add));
-    } else if (pl.large) {
-      KLAUNCH(st, "k_fp8_product", k_fp8_product<T, exact, 256, 256, 2, 4><<<grid, 512, 0, st>>>(p));
-    } else {
-      KLAUNCH(st, "k_fp8_product", k_fp8_product<T, exact, 128, 128, 2, 2><<<grid, 256, 0, st>>>(p));
-    }
+    auto launch = [&](auto part) -> int {
+      using P = decltype(part);
+      if (pl.tile == 256)
+        KLAUNCH(st, "k_fp8_product", k_fp8_product<P, exact, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(p));
+      else if (pl.tile == 128)
+        KLAUNCH(st, "k_fp8_product", k_fp8_product<P, exact, 128, 128, 2, 2, 2><<<grid, 256, 0, st>>>(p));
+      else
+        KLAUNCH(st, "k_fp8_product", k_fp8_product<P, exact, 64, 64, 4, 1, 4><<<grid, 256, 0, st>>>(p));
+      return CHGNET_OK;
+    };
+    if (pl.splits == 1) return launch(T{});
+    CHG_TRY(launch(float{}));
+    KLAUNCH(st, "k_fp8_join", k_fp8_join<T><<<(unsigned)std::min<int64_t>(2048, cdiv(M * part_ld(N) / 4, 256)), 256, 0, st>>>(
+                                  M, N, pl.splits, p.part, p.ldp, static_cast<T*>(out), ldout, p.add));
     return CHGNET_OK;
   });
 }
