@@ -18,7 +18,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "common.hpp"
@@ -115,105 +114,199 @@ __global__ void __launch_bounds__(256) k_fp8_rows(int64_t rows, int64_t cols, co
   }
 }
 
-// A tile of 128 x 128 a block, codes of it and of its transpose (either may be
-// left out). SQUARE: one scale for the tile, which both share; else 1 x 128 of
-// the rows of each. A thread has 8 x 8 values; the transposed codes go through
-// LDS, in units of the 8 bytes that a thread has of a column, unit u of column c
-// at u ^ (c / 8 % 16), so that 16 lanes write to 16 banks' pairs.
+// Eight values of a row as they are stored, in words, and the order of their
+// magnitudes without conversions: that of the bits below the sign.
+template <class T>
+struct Eight {
+  static constexpr int NW = 2 * sizeof(T);
+  typedef unsigned short pair __attribute__((ext_vector_type(2)));
+  unsigned w[NW];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int q = 0; q < NW / 4; ++q) {
+      const uint4 t = reinterpret_cast<const uint4*>(p)[q];
+      w[4 * q] = t.x;
+      w[4 * q + 1] = t.y;
+      w[4 * q + 2] = t.z;
+      w[4 * q + 3] = t.w;
+    }
+  }
+  // the first n of them, 0 for the others
+  __device__ __forceinline__ void load_some(const T* p, int64_t n) {
+    typedef typename std::conditional<sizeof(T) == 4, unsigned, unsigned short>::type bits;
+    const bits* b = reinterpret_cast<const bits*>(p);
+#pragma unroll
+    for (int q = 0; q < NW; ++q) w[q] = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < n) w[k * NW / 8] |= (unsigned)b[k] << (sizeof(T) == 2 && k % 2 ? 16 : 0);
+  }
+  __device__ __forceinline__ float get(int k) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
+    else return bits16(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu);
+  }
+  // the value of 16 bits
+  static __device__ __forceinline__ float bits16(unsigned b) {
+    if constexpr (std::is_same<T, bf16_t>::value) return __uint_as_float(b << 16);
+    else return (float)__builtin_bit_cast(f16_t, (unsigned short)b);
+  }
+  static __device__ __forceinline__ unsigned below_sign(unsigned w) { return w & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu); }
+  // of words without signs, half by half
+  static __device__ __forceinline__ unsigned larger(unsigned a, unsigned b) {
+    if constexpr (sizeof(T) == 4) return max(a, b);
+    else return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(pair, a), __builtin_bit_cast(pair, b)));
+  }
+  // fp32 bits of the larger value of a word, and of half h
+  static __device__ __forceinline__ unsigned largest(unsigned w) {
+    if constexpr (sizeof(T) == 4) return w;
+    else return __float_as_uint(bits16(max(w & 0xffffu, w >> 16)));
+  }
+  static __device__ __forceinline__ unsigned half(unsigned w, int h) {
+    if constexpr (sizeof(T) == 4) return w;
+    else return __float_as_uint(bits16(h ? w >> 16 : w & 0xffffu));
+  }
+  // kept from being converted once for all uses: the floats of 64 values have no room
+  __device__ __forceinline__ void fence() {
+#pragma unroll
+    for (int q = 0; q < NW; ++q) asm volatile("" : "+v"(w[q]));
+  }
+};
+
+// Tiles of 128 x 128, `count` (1 or 4) below each other a block: codes of them and
+// of their transpose (either may be left out). SQUARE: one scale for a tile, which
+// both share; else 1 x 128 of the rows of each. A thread has 8 x 8 values; the
+// transposed codes go through LDS, in units of the 8 bytes that a thread has of a
+// column, unit u of column c at u ^ (c / 8 % 16), so that 16 lanes write to 16
+// banks' pairs. Four tiles a block, so that the transpose's scales are written in
+// words: single bytes far from each other were a third of all writes, and took
+// twice the time (397,934 x 512 in bf16, both forms: 278 us).
 template <class T, bool VEC, bool SQUARE>
-__global__ void __launch_bounds__(256) k_fp8_tile(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
-                                                  uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scale,
-                                                  int64_t lds, uint8_t* __restrict__ codes_t, int64_t ldct,
-                                                  uint8_t* __restrict__ scale_t, int64_t ldst) {
+__global__ void __launch_bounds__(256, 4) k_fp8_tile(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
+                                                     uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scale,
+                                                     int64_t lds, uint8_t* __restrict__ codes_t, int64_t ldct,
+                                                     uint8_t* __restrict__ scale_t, int64_t ldst, int count) {
   __shared__ uint2 tile[128][16];
   __shared__ unsigned colmax[4][128];
-  const int64_t tiles_c = (cols + 127) / 128;
-  const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
+  __shared__ unsigned words[128];  // a column's scale bytes in the block's tiles
+  const int64_t tiles_c = (cols + 127) / 128, tiles_r = (rows + 127) / 128;
+  const int64_t tc = blockIdx.x % tiles_c, tr0 = blockIdx.x / tiles_c * count;
   const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t r0 = tr * 128 + rg * 8, c0 = tc * 128 + cg * 8;
-  float v[8][8];
+  const int64_t c0 = tc * 128 + cg * 8;
+  const int64_t end_c = (cols + 15) / 16 * 16, end_r = (rows + 15) / 16 * 16;
+  for (int t = 0; t < count && tr0 + t < tiles_r; ++t) {
+    asm volatile("" : "+s"(t));  // addresses are formed for each tile, not kept for all
+    const int64_t tr = tr0 + t, r0 = tr * 128 + rg * 8;
+    using E = Eight<T>;
+    constexpr int NW = E::NW;
+    E v[8];
+    {
+      const T* p = x + r0 * ldx + c0;
+      const int there = (int)(rows - r0 < 8 ? rows - r0 : 8);  // rows of this thread's (may be none)
+      if (VEC && c0 + 8 <= cols && there == 8) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (r0 + i < rows) {
-      load8<T, VEC>(x + (r0 + i) * ldx, c0, cols, v[i]);
+        for (int i = 0; i < 8; ++i) v[i].load(p + i * ldx);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i].load_some(p + i * ldx, i < there ? cols - c0 : 0);
+      }
+    }
+    unsigned col[NW];
+#pragma unroll
+    for (int q = 0; q < NW; ++q) {
+      col[q] = E::below_sign(v[0].w[q]);
+#pragma unroll
+      for (int i = 1; i < 8; ++i) col[q] = E::larger(col[q], E::below_sign(v[i].w[q]));
+    }
+    unsigned whole = 0;
+    if constexpr (SQUARE) {
+#pragma unroll
+      for (int q = 1; q < NW; ++q) col[0] = E::larger(col[0], col[q]);
+      whole = groupmax_bits(rowmax_bits<16>(E::largest(col[0])));
+      if (lane == 0) colmax[wave][0] = whole;
     } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+      for (int q = 0; q < NW; ++q) {
+        const auto a = __builtin_amdgcn_permlane16_swap(col[q], col[q], false, false);
+        const unsigned m = E::larger(a[0], a[1]);
+        const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+        if (lane < 16) colmax[wave][cg * NW + q] = E::larger(b[0], b[1]);
+      }
     }
-  }
-  unsigned whole = 0;
-  unsigned col[8] = {};
+    __syncthreads();  // (the last tile's codes are read, too)
+    if constexpr (SQUARE) whole = max(max(colmax[0][0], colmax[1][0]), max(colmax[2][0], colmax[3][0]));
+    const unsigned all = scale_byte(whole);
+    if (codes) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 8; ++i) {
+        unsigned byte = all;
+        v[i].fence();
+        if constexpr (!SQUARE) {
+          unsigned big = E::below_sign(v[i].w[0]);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) col[k] = max(col[k], magnitude(v[i][k]));
-  if constexpr (SQUARE) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) whole = max(whole, col[k]);
-    whole = groupmax_bits(rowmax_bits<16>(whole));
-    if (lane == 0) colmax[wave][0] = whole;
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      col[k] = groupmax_bits(col[k]);
-      if (lane < 16) colmax[wave][cg * 8 + k] = col[k];
+          for (int q = 1; q < NW; ++q) big = E::larger(big, E::below_sign(v[i].w[q]));
+          byte = scale_byte(rowmax_bits<16>(E::largest(big)));
+        }
+        const float inv = scale_inverse(byte);
+        if (r0 + i < rows) {
+          if (c0 < end_c) {
+            const E& r = v[i];
+            uint2 q;
+            q.x = codes4(r.get(0) * inv, r.get(1) * inv, r.get(2) * inv, r.get(3) * inv);
+            q.y = codes4(r.get(4) * inv, r.get(5) * inv, r.get(6) * inv, r.get(7) * inv);
+            *reinterpret_cast<uint2*>(codes + (r0 + i) * ldc + c0) = q;
+          }
+          if (!SQUARE && cg == 0) scale[(r0 + i) * lds + tc] = (uint8_t)byte;
+        }
+      }
+      if (SQUARE && threadIdx.x == 0) scale[tr * lds + tc] = (uint8_t)all;
     }
-  }
-  __syncthreads();
-  if constexpr (SQUARE) {
-    whole = max(max(colmax[0][0], colmax[1][0]), max(colmax[2][0], colmax[3][0]));
-  } else {
+    if (!codes_t) {
+      __syncthreads();  // colmax is read
+      continue;
+    }
+    if constexpr (!SQUARE) {
+#pragma unroll
+      for (int q = 0; q < NW; ++q) {
+        const int c = cg * NW + q;
+        col[q] = E::larger(E::larger(colmax[0][c], colmax[1][c]), E::larger(colmax[2][c], colmax[3][c]));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i].fence();
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int c = cg * 8 + k;
-      col[k] = max(max(colmax[0][c], colmax[1][c]), max(colmax[2][c], colmax[3][c]));
-    }
-  }
-  const unsigned all = scale_byte(whole);
-  if (codes) {
-    const int64_t end = (cols + 15) / 16 * 16;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
       unsigned byte = all;
       if constexpr (!SQUARE) {
-        unsigned big = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) big = max(big, magnitude(v[i][k]));
-        byte = scale_byte(rowmax_bits<16>(big));
+        byte = scale_byte(E::half(col[k * NW / 8], k & 1));
+        if (rg == 0) words[c] = (t ? words[c] : 0u) | byte << (8 * t);
       }
       const float inv = scale_inverse(byte);
-      if (r0 + i < rows) {
-        if (c0 < end) {
-          uint2 q;
-          q.x = codes4(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
-          q.y = codes4(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
-          *reinterpret_cast<uint2*>(codes + (r0 + i) * ldc + c0) = q;
-        }
-        if (!SQUARE && cg == 0) scale[(r0 + i) * lds + tc] = (uint8_t)byte;
-      }
+      uint2 q;
+      q.x = codes4(v[0].get(k) * inv, v[1].get(k) * inv, v[2].get(k) * inv, v[3].get(k) * inv);
+      q.y = codes4(v[4].get(k) * inv, v[5].get(k) * inv, v[6].get(k) * inv, v[7].get(k) * inv);
+      tile[c][rg ^ cg] = q;
     }
-    if (SQUARE && threadIdx.x == 0) scale[tr * lds + tc] = (uint8_t)all;
-  }
-  if (!codes_t) return;
+    if (SQUARE && threadIdx.x == 0) scale_t[tc * ldst + tr] = (uint8_t)all;
+    __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const unsigned byte = SQUARE ? all : scale_byte(col[k]);
-    const float inv = scale_inverse(byte);
-    uint2 q;
-    q.x = codes4(v[0][k] * inv, v[1][k] * inv, v[2][k] * inv, v[3][k] * inv);
-    q.y = codes4(v[4][k] * inv, v[5][k] * inv, v[6][k] * inv, v[7][k] * inv);
-    tile[cg * 8 + k][rg ^ cg] = q;
-    if (!SQUARE && rg == 0 && c0 + k < cols) scale_t[(c0 + k) * ldst + tr] = (uint8_t)byte;
+    for (int i = 0; i < 4; ++i) {
+      const int p = i * 256 + threadIdx.x, c = p >> 3, u = p & 7, g = c >> 3;
+      const int64_t cc = tc * 128 + c, rr = tr * 128 + u * 16;
+      const uint2 a = tile[c][(2 * u) ^ g], b = tile[c][(2 * u + 1) ^ g];
+      if (cc < cols && rr < end_r) *reinterpret_cast<uint4*>(codes_t + cc * ldct + rr) = make_uint4(a.x, a.y, b.x, b.y);
+    }
   }
-  if (SQUARE && threadIdx.x == 0) scale_t[tc * ldst + tr] = (uint8_t)all;
-  __syncthreads();
-  const int64_t end = (rows + 15) / 16 * 16;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int t = i * 256 + threadIdx.x, c = t >> 3, u = t & 7, g = c >> 3;
-    const int64_t cc = tc * 128 + c, rr = tr * 128 + u * 16;
-    const uint2 a = tile[c][(2 * u) ^ g], b = tile[c][(2 * u + 1) ^ g];
-    if (cc < cols && rr < end) *reinterpret_cast<uint4*>(codes_t + cc * ldct + rr) = make_uint4(a.x, a.y, b.x, b.y);
+  if constexpr (!SQUARE) {
+    if (!codes_t || threadIdx.x >= 128 || tc * 128 + threadIdx.x >= cols) return;
+    // (the words are this thread's block's: written before its last barrier)
+    uint8_t* p = scale_t + (tc * 128 + threadIdx.x) * ldst + tr0;
+    const unsigned w = words[threadIdx.x];
+    if (count == 4) {
+      *reinterpret_cast<unsigned*>(p) = w;  // (a row of scales has whole words)
+    } else {
+      *p = (uint8_t)w;
+    }
   }
 }
 
@@ -544,15 +637,19 @@ struct Plan {
   int64_t tiles;
   int splits, kb_split;
 };
-// The tiles: the largest of which there is one for each compute unit. Splits of K:
-// where the tiles are fewer than the compute units.
+// The tiles: the largest of which there is one for each compute unit, where K may
+// be divided into parts of kLeastSteps blocks or more. 256 x 512 x 397,934 took
+// 159 us in 2 tiles of 256 x 128 parts, 185 in 8 of 128 x 32, 190 in 32 of 64 x
+// 16; 512 x 4,096 x 4,096 19 us in 512 tiles of 64, 26 in 128 of 128, 24 in twice
+// as many halves; 128 x 8,192 x 8,192 25 us in 256 tiles of 64 and two parts, 29 in one,
+// 33 in 64 of 128 and two.
+constexpr int64_t kLeastSteps = 24, kUnits = 256;
 Plan plan(int64_t M, int64_t N, int64_t K) {
+  const int64_t nkb = std::max<int64_t>(1, cdiv(K, kBlock)), most = std::max<int64_t>(1, nkb / kLeastSteps);
   auto tiles = [&](int t) { return cdiv(M, t) * cdiv(N, t); };
-  int tile = tiles(256) >= 256 ? 256 : tiles(128) >= 256 ? 128 : 64;
-  if (getenv("FP8T")) tile = atoi(getenv("FP8T"));
-  const int64_t n = tiles(tile), nkb = std::max<int64_t>(1, cdiv(K, kBlock));
-  int64_t s = n >= 256 ? 1 : std::min<int64_t>(cdiv(512, n), std::max<int64_t>(1, nkb / 4));
-  if (getenv("FP8S")) s = std::min<int64_t>(nkb, atoi(getenv("FP8S")));
+  const int tile = tiles(256) * most >= kUnits ? 256 : tiles(128) * most >= kUnits ? 128 : 64;
+  const int64_t n = tiles(tile), want = tile == 64 ? 2 * kUnits / n : cdiv(kUnits, n);
+  const int64_t s = std::max<int64_t>(1, std::min(want, most));
   const int64_t per = cdiv(cdiv(nkb, s), 4) * 4;  // (of whole words of scales)
   return {tile, n, (int)cdiv(nkb, per), (int)per};
 }
@@ -594,12 +691,15 @@ int fp8_quantize_entry(int64_t rows, int64_t cols, int32_t dtype, const void* x,
 #undef CHG_ROWS
       return CHGNET_OK;
     }
-    const int64_t tiles = cdiv(rows, 128) * cdiv(cols, 128);
+    // four tiles a block where that leaves a block for each compute unit
+    const int count = cdiv(rows, 512) * cdiv(cols, 128) >= 256 ? 4 : 1;
+    const int64_t tiles = cdiv(rows, 128 * count) * cdiv(cols, 128);
     if (tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles of 128 x 128");
     const chgnet_fp8 none{}, &a = q ? *q : none, &b = t ? *t : none;
 #define CHG_TILE(V, S)                                                                                                     \
   KLAUNCH(st, "k_fp8_tile", k_fp8_tile<T, V, S><<<(unsigned)tiles, 256, 0, st>>>(                                          \
-                                rows, cols, p, ldx, a.codes, a.ld, a.scale, a.ld_scale, b.codes, b.ld, b.scale, b.ld_scale))
+                                rows, cols, p, ldx, a.codes, a.ld, a.scale, a.ld_scale, b.codes, b.ld, b.scale, b.ld_scale, \
+                                count))
     if (vec && square) CHG_TILE(true, true);
     else if (vec) CHG_TILE(true, false);
     else if (square) CHG_TILE(false, true);
@@ -671,7 +771,7 @@ struct LinearWs {
 static LinearWs linear_ws(int64_t M, int64_t K, size_t product, void* ws) {
   LinearWs w{};
   w.q.rows = M, w.q.cols = K, w.q.block_rows = 1;
-  w.q.ld = cdiv(K, 16) * 16, w.q.ld_scale = cdiv(cdiv(K, kBlock), 4) * 4;
+  w.q.ld = K <= kBlock ? cdiv(K, 16) * 16 : cdiv(K, kBlock) * kBlock, w.q.ld_scale = cdiv(cdiv(K, kBlock), 4) * 4;
   const size_t codes = align_up((size_t)M * w.q.ld, 256), scale = align_up((size_t)M * w.q.ld_scale, 256);
   w.q.codes = static_cast<uint8_t*>(ws);
   w.q.scale = static_cast<uint8_t*>(ws) + codes;

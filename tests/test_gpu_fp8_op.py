@@ -31,7 +31,7 @@ def _check_matrix(m, x, block_rows, what=""):
     got = m.codes.cpu().float().double()
     assert torch.equal(torch.where(fine, got, 0.0), torch.where(fine, q, 0.0)), what
     if m._data is not None and m.cols % 16 and m.rows:
-        raw = m._data[:m.rows * m._c.ld].view(m.rows, -1)[:, m.cols:]
+        raw = m._data[:m.rows * m._c.ld].view(m.rows, -1)[:, m.cols:-(-m.cols // 16) * 16]
         assert not raw.any(), what
     return ref.values(q, byte, block_rows)
 
@@ -149,7 +149,8 @@ def test_both_blocks_of_128_rows():
     _check_product(a, va, b, vb)
 
 
-@pytest.mark.parametrize("M,N,K", [(256, 512, 20000), (40, 50, 70001), (1, 1, 100000), (300, 200, 9000), (128, 128, 4096)])
+@pytest.mark.parametrize("M,N,K", [(256, 512, 20000), (40, 50, 70001), (1, 1, 100000), (300, 200, 9000), (128, 128, 4096),
+                                   (1000, 500, 24600), (1000, 1030, 49200)])
 def test_long_sums(M, N, K):
     """Products whose K is divided."""
     a, va = _random(M, K, 1, 5)
