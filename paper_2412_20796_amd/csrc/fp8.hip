@@ -328,7 +328,7 @@ struct ProductArgs {
   int64_t ldo;
   float* part;  // [split][M][ldp] partial sums, or NULL: `out` is written
   int64_t ldp;
-  int kb_split;  // blocks of 128 along K that one split has
+  int splits, kb_split;  // parts of K, and blocks of 128 along it that one has
   int add;
 };
 
@@ -399,47 +399,85 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
   constexpr int W = 16 / sizeof(T);                // results in 16 bytes
   static_assert(TN == 4 && THREADS % 256 == 0, "64 columns a wavefront");
   __shared__ __align__(1024) uint8_t lds[STAGES][(BM + BN) * kBlock];
-  __shared__ unsigned words[2][BM + BN];
+  __shared__ unsigned words[STAGES][BM + BN];
   const int64_t M = p.a.rows, N = p.b.rows;
-  const int64_t tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
-  // tiles: each of the 8 chiplets has a run of them, in groups of 8 rows of tiles
-  int64_t tile = blockIdx.x;
-  {
-    const int64_t n = tiles_m * tiles_n, q = n / 8, r = n % 8, x = tile % 8;
-    tile = x * q + (x < r ? x : r) + tile / 8;
-  }
-  int64_t tm, tn;
-  {
-    const int64_t group = 8 * tiles_n, g = tile / group, first = g * 8, size = tiles_m - first < 8 ? tiles_m - first : 8;
-    const int64_t in = tile - g * group;
-    tm = first + in % size;
-    tn = in / size;
-  }
-  const int64_t m0 = tm * BM, n0 = tn * BN;
+  const int64_t tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN, tiles = tiles_m * tiles_n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
-  const int64_t nkb = (p.K + kBlock - 1) / kBlock;
-  const int64_t kb0 = (int64_t)blockIdx.y * p.kb_split;
-  const int64_t kb1 = kb0 + p.kb_split < nkb ? kb0 + p.kb_split : nkb;
+  const int nkb = (int)((p.K + kBlock - 1) / kBlock);
 
-  // this thread's pieces, as offsets from the tile's first rows: rows past the
-  // end are the last one again
-  constexpr int A_PIECES = BM * 8 / THREADS;
+  // Items: the tiles of each part of K. Each of the 8 chiplets has a run of tiles,
+  // in groups of 8 rows of tiles.
+  struct Item {
+    int64_t m0, n0;
+    int split, kb0, kb1;
+  };
+  const int64_t items = tiles * p.splits;
+  auto item_at = [&](int64_t item) -> Item {
+    Item t;
+    t.split = (int)(item / tiles);
+    int64_t tile = item - t.split * tiles;
+    const int64_t q = tiles / 8, r = tiles % 8, x = tile % 8;
+    tile = x * q + (x < r ? x : r) + tile / 8;
+    const int64_t group = 8 * tiles_n, gr = tile / group, first = gr * 8, size = tiles_m - first < 8 ? tiles_m - first : 8;
+    const int64_t in = tile - gr * group;
+    t.m0 = (first + in % size) * BM;
+    t.n0 = in / size * BN;
+    t.kb0 = t.split * p.kb_split;
+    t.kb1 = t.kb0 + p.kb_split < nkb ? t.kb0 + p.kb_split : nkb;
+    return t;
+  };
+
+  // The loads run STAGES - 1 steps ahead of the products, into the next item where
+  // this one has no more: its first codes arrive while results are stored.
+  // Pieces and scales are at offsets from the item's first rows: rows past the end
+  // are the last one again. A word of scales has a row's bytes of four blocks of K.
+  constexpr int A_PIECES = BM * 8 / THREADS, WORDS = (BM + BN + THREADS - 1) / THREADS;
   static_assert(BM * 8 % THREADS == 0 && BN * 8 % THREADS == 0, "a step's pieces are of one factor");
-  const int last_a = (int)(M - m0 < BM ? M - m0 : BM) - 1, last_b = (int)(N - n0 < BN ? N - n0 : BN) - 1;
-  const uint8_t *const codes_a = p.a.codes + m0 * p.a.ldc, *const codes_b = p.b.codes + n0 * p.b.ldc;
-  unsigned src[PIECES];
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int row = (i * THREADS + threadIdx.x) / 8 - (i < A_PIECES ? 0 : BM), last = i < A_PIECES ? last_a : last_b;
-    src[i] = (unsigned)(row < last ? row : last) * (unsigned)(i < A_PIECES ? p.a.ldc : p.b.ldc);
-  }
+  int64_t ahead_item = blockIdx.x;
+  int ahead_kb, ahead_kb0, ahead_kb1, ahead_words = 0, issued = 0;
+  const uint8_t *codes_a, *codes_b, *scale_a, *scale_b;
+  unsigned src[PIECES], word_src[WORDS];
   auto piece = [&](int i) -> unsigned {
     const unsigned key = i < A_PIECES || W == 4 ? threadIdx.x >> 4 & 7 : (threadIdx.x >> 4 & 1) | (threadIdx.x >> 6 & 3) << 1;
     return 16 * ((threadIdx.x & 7) ^ key);
   };
-  auto fetch = [&](int64_t kb, int buf) {
-    const int64_t at = kb * kBlock;
+  auto load_item = [&]() {
+    const Item t = item_at(ahead_item);
+    ahead_kb = ahead_kb0 = t.kb0;
+    ahead_kb1 = t.kb1;
+    const int last_a = (int)(M - t.m0 < BM ? M - t.m0 : BM) - 1, last_b = (int)(N - t.n0 < BN ? N - t.n0 : BN) - 1;
+    codes_a = p.a.codes + t.m0 * p.a.ldc;
+    codes_b = p.b.codes + t.n0 * p.b.ldc;
+    scale_a = p.a.scale + (t.m0 >> p.a.shift) * p.a.lds;
+    scale_b = p.b.scale + (t.n0 >> p.b.shift) * p.b.lds;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int row = (i * THREADS + threadIdx.x) / 8 - (i < A_PIECES ? 0 : BM), last = i < A_PIECES ? last_a : last_b;
+      src[i] = (unsigned)(row < last ? row : last) * (unsigned)(i < A_PIECES ? p.a.ldc : p.b.ldc);
+    }
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      const int row = i * THREADS + threadIdx.x;
+      const bool is_a = row < BM;
+      const Factor& f = is_a ? p.a : p.b;
+      const int r = is_a ? row : row - BM, last = is_a ? last_a : last_b;
+      // (an item starts at a row of blocks)
+      word_src[i] = (unsigned)((r < last ? r : last) >> f.shift) * (unsigned)f.lds;
+    }
+  };
+  auto load_step = [&](int buf) {
+    if (ahead_item >= items || ahead_kb >= ahead_kb1) return;
+    if (((ahead_kb - ahead_kb0) & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        if (i * THREADS + wave * 64 >= BM + BN) break;
+        to_lds4((i * THREADS + wave * 64 < BM ? scale_a : scale_b) + ahead_kb + word_src[i],
+                words[ahead_words] + i * THREADS + wave * 64);
+      }
+      ahead_words = ahead_words + 1 == STAGES ? 0 : ahead_words + 1;
+    }
+    const int64_t at = (int64_t)ahead_kb * kBlock;
     uint8_t* to = lds[buf] + wave * 1024;
     if (at + kBlock <= p.K) {
 #pragma unroll
@@ -454,34 +492,15 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
           *reinterpret_cast<uint4*>(to + i * THREADS * 16 + (threadIdx.x & 63) * 16) = make_uint4(0, 0, 0, 0);
       }
     }
-  };
-  // scales: a word has a row's bytes of four blocks of K
-  const int64_t sm0 = m0 >> p.a.shift, sn0 = n0 >> p.b.shift;
-  constexpr int WORDS = (BM + BN + THREADS - 1) / THREADS;
-  unsigned word_src[WORDS];
-#pragma unroll
-  for (int i = 0; i < WORDS; ++i) {
-    const int row = i * THREADS + threadIdx.x;
-    const bool is_a = row < BM;
-    const Factor& f = is_a ? p.a : p.b;
-    const int r = is_a ? row : row - BM, last = is_a ? last_a : last_b;
-    word_src[i] = (unsigned)((((is_a ? m0 : n0) + (r < last ? r : last)) >> f.shift) - (is_a ? sm0 : sn0)) * (unsigned)f.lds;
-  }
-  auto fetch_scales = [&](int64_t kb, int buf) {
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-      if (i * THREADS + wave * 64 >= BM + BN) break;
-      const uint8_t* base = (i * THREADS + wave * 64 < BM ? p.a.scale + sm0 * p.a.lds : p.b.scale + sn0 * p.b.lds) + kb;
-      to_lds4(base + word_src[i], words[buf] + i * THREADS + wave * 64);
+    ++issued;
+    if (++ahead_kb == ahead_kb1) {
+      ahead_item += gridDim.x;
+      if (ahead_item < items) load_item();
     }
   };
   const int r16 = lane & 15, g = lane >> 4;
   unsigned ea[TM], eb[TN];
   v4f acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
   // half h of a lane's 32 codes of an operand: piece g + 4 h of its row
   auto column = [](int row, int j) { return (row >> 2) * W + (row & 3) + j / (W / 4) * 4 * W + j % (W / 4) * 4; };
   const int key = r16 >> 1;
@@ -492,101 +511,114 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
     return *reinterpret_cast<const v4i*>(lds[buf] + (BM + wn + column(r16, j)) * kBlock + ((g + 4 * h) ^ key) * 16);
   };
   auto whole = [](const v4i& a, const v4i& b) { return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; };
-  static_assert(STAGES >= 2 && STAGES <= 5, "a word of scales arrives in the four steps before its own");
-  if (kb0 < kb1) fetch_scales(kb0, 0);
+  // the first loads, and then for each item its steps and results
+  constexpr int MAY = (STAGES - 2) * PIECES, STORES = TM * (16 / W);
+  load_item();
 #pragma unroll
-  for (int i = 0; i < STAGES - 1; ++i)
-    if (kb0 + i < kb1) fetch(kb0 + i, i);
-  int buf = 0;
-  for (int64_t kb = kb0; kb < kb1; ++kb) {
-    const int i = (int)(kb - kb0);
-    // the codes of this step are there (loads end in order, and those of the next
-    // STAGES - 2 steps may be under way), and all have read what is loaded over
-    if (STAGES > 2 && kb + STAGES - 1 <= kb1) wait_barrier<(STAGES - 2) * PIECES>();
-    else wait_barrier<0>();
-    if ((i & 3) == 0) {
-      const unsigned* w = words[i >> 2 & 1];
+  for (int i = 0; i < STAGES - 1; ++i) load_step(i);
+  int buf = 0, word = 0, done = 0;
+  bool stored = false;  // STORES stores are the last that this wavefront did
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const Item t = item_at(item);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) ea[i] = w[wm + 16 * i + r16];
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) eb[j] = w[BM + wn + column(r16, j)];
-      if (kb + 4 < kb1) fetch_scales(kb + 4, (i >> 2 & 1) ^ 1);
-    } else {
+      for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int kb = t.kb0; kb < t.kb1; ++kb) {
+      // the codes of this step are there (loads and stores end in order; the loads of
+      // the next STAGES - 2 steps and the last item's stores may be under way), and
+      // all have read what is loaded over
+      if (issued - done <= STAGES - 2) wait_barrier<0>();
+      else if (stored) wait_barrier<MAY + STORES>();
+      else wait_barrier<MAY>();
+      stored = false;
+      ++done;
+      if (((kb - t.kb0) & 3) == 0) {
+        const unsigned* w = words[word];
+        word = word + 1 == STAGES ? 0 : word + 1;
 #pragma unroll
-      for (int i = 0; i < TM; ++i) ea[i] >>= 8;
+        for (int i = 0; i < TM; ++i) ea[i] = w[wm + 16 * i + r16];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) eb[j] >>= 8;
-    }
-    if (kb + STAGES - 1 < kb1) fetch(kb + STAGES - 1, buf == 0 ? STAGES - 1 : buf - 1);
-    constexpr int AHEAD = TM > 2 ? 2 : TM - 1;  // operands of a that are loaded ahead of their products
-    if constexpr (EXACT) {
+        for (int j = 0; j < TN; ++j) eb[j] = w[BM + wn + column(r16, j)];
+      } else {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        v4i a[AHEAD + 1], b[TN];
-        v8b bw[TN][2];
+        for (int i = 0; i < TM; ++i) ea[i] >>= 8;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) b[j] = half_b(buf, j, h);
+        for (int j = 0; j < TN; ++j) eb[j] >>= 8;
+      }
+      load_step(buf == 0 ? STAGES - 1 : buf - 1);
+      constexpr int AHEAD = TM > 2 ? 2 : TM - 1;  // operands of a that are loaded ahead of their products
+      if constexpr (EXACT) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) a[i] = half_a(buf, i, h);
+        for (int h = 0; h < 2; ++h) {
+          v4i a[AHEAD + 1], b[TN];
+          v8b bw[TN][2];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          bw[j][0] = wide(make_uint2(b[j][0], b[j][1]), scale_value(eb[j]));
-          bw[j][1] = wide(make_uint2(b[j][2], b[j][3]), scale_value(eb[j]));
+          for (int j = 0; j < TN; ++j) b[j] = half_b(buf, j, h);
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i) a[i] = half_a(buf, i, h);
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            bw[j][0] = wide(make_uint2(b[j][0], b[j][1]), scale_value(eb[j]));
+            bw[j][1] = wide(make_uint2(b[j][2], b[j][3]), scale_value(eb[j]));
+          }
+#pragma unroll
+          for (int i = 0; i < TM; ++i) {
+            if (i + AHEAD < TM) a[(i + AHEAD) % (AHEAD + 1)] = half_a(buf, i + AHEAD, h);
+            const v4i q = a[i % (AHEAD + 1)];
+            const v8b w0 = wide(make_uint2(q[0], q[1]), scale_value(ea[i]));
+            const v8b w1 = wide(make_uint2(q[2], q[3]), scale_value(ea[i]));
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][0], w0, acc[i][j], 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][1], w1, acc[i][j], 0, 0, 0);
+          }
         }
+      } else {
+        v8i a[AHEAD + 1], b[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) b[j] = whole(half_b(buf, j, 0), half_b(buf, j, 1));
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) a[i] = whole(half_a(buf, i, 0), half_a(buf, i, 1));
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * (TN + AHEAD), 0);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-          if (i + AHEAD < TM) a[(i + AHEAD) % (AHEAD + 1)] = half_a(buf, i + AHEAD, h);
-          const v4i q = a[i % (AHEAD + 1)];
-          const v8b w0 = wide(make_uint2(q[0], q[1]), scale_value(ea[i]));
-          const v8b w1 = wide(make_uint2(q[2], q[3]), scale_value(ea[i]));
+          if (i + AHEAD < TM) {
+            a[(i + AHEAD) % (AHEAD + 1)] = whole(half_a(buf, i + AHEAD, 0), half_a(buf, i + AHEAD, 1));
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+          }
 #pragma unroll
-          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][0], w0, acc[i][j], 0, 0, 0);
-#pragma unroll
-          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[j][1], w1, acc[i][j], 0, 0, 0);
+          for (int j = 0; j < TN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i % (AHEAD + 1)], acc[i][j], 0, 0, 0, eb[j], 0,
+                                                                         ea[i]);
+          __builtin_amdgcn_sched_group_barrier(0x8, TN, 0);
         }
       }
-    } else {
-      v8i a[AHEAD + 1], b[TN];
-#pragma unroll
-      for (int j = 0; j < TN; ++j) b[j] = whole(half_b(buf, j, 0), half_b(buf, j, 1));
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) a[i] = whole(half_a(buf, i, 0), half_a(buf, i, 1));
-      __builtin_amdgcn_sched_group_barrier(0x100, 2 * (TN + AHEAD), 0);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        if (i + AHEAD < TM) {
-          a[(i + AHEAD) % (AHEAD + 1)] = whole(half_a(buf, i + AHEAD, 0), half_a(buf, i + AHEAD, 1));
-          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i % (AHEAD + 1)], acc[i][j], 0, 0, 0, eb[j], 0,
-                                                                       ea[i]);
-        __builtin_amdgcn_sched_group_barrier(0x8, TN, 0);
+      buf = buf + 1 == STAGES ? 0 : buf + 1;
+    }
+    T* out = static_cast<T*>(p.out);
+    int64_t ld = p.ldo;
+    if constexpr (W == 4) {
+      if (p.part) {
+        out = p.part + (int64_t)t.split * M * p.ldp;
+        ld = p.ldp;
       }
     }
-    buf = buf + 1 == STAGES ? 0 : buf + 1;
-  }
-  auto results = [&](T* out, int64_t ld, bool add) {
-    const bool vec = (ld * sizeof(T) & 15) == 0 && ((uintptr_t)out & 15) == 0;
+    const bool vec = (ld * sizeof(T) & 15) == 0 && ((uintptr_t)out & 15) == 0, add = p.add && !p.part;
+    stored = vec && !add && t.m0 + BM <= M && t.n0 + BN <= N;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int64_t m = m0 + wm + 16 * i + r16;
-      if (m >= M) continue;
+      const int64_t m = t.m0 + wm + 16 * i + r16;
 #pragma unroll
       for (int q = 0; q < 16 / W; ++q) {
-        const int64_t n = n0 + wn + q * 4 * W + g * W;
-        float t[W];
+        const int64_t n = t.n0 + wn + q * 4 * W + g * W;
+        float v[W];
 #pragma unroll
-        for (int k = 0; k < W; ++k) t[k] = acc[i][(q * W + k) / 4][k % 4];
-        put(out + m * ld + n, t, N - n, vec, add);
+        for (int k = 0; k < W; ++k) v[k] = acc[i][(q * W + k) / 4][k % 4];
+        if (stored) store_v<W>(out + m * ld + n, v);
+        else if (m < M) put(out + m * ld + n, v, N - n, vec, add);
       }
     }
-  };
-  if (p.part) {
-    if constexpr (W == 4) results(p.part + (int64_t)blockIdx.y * M * p.ldp, p.ldp, false);
-  } else {
-    results(static_cast<T*>(p.out), p.ldo, p.add != 0);
   }
 }
 
@@ -739,20 +771,20 @@ int fp8_matmul_entry(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, vo
   if (!aligned_to(ws, 16)) return bad(who, "ws is not 16-byte aligned");
   const Plan pl = plan(M, N, K);
   ProductArgs p{factor(a), factor(b), K, out, ldout, pl.splits > 1 ? static_cast<float*>(ws) : nullptr, part_ld(N),
-                pl.kb_split, accumulate != 0};
-  if (pl.tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles");
+                pl.splits, pl.kb_split, accumulate != 0};
   return with_type(dtype, [&](auto v) -> int {
     using T = decltype(v);
     constexpr bool exact = std::is_same<T, float>::value;
-    const dim3 grid((unsigned)pl.tiles, pl.splits);
     auto launch = [&](auto part) -> int {
       using P = decltype(part);
+      // as many blocks as have room at a time
+      auto blocks = [&](int64_t a_unit) { return (unsigned)std::min<int64_t>(pl.tiles * pl.splits, a_unit * kUnits); };
       if (pl.tile == 256)
-        KLAUNCH(st, "k_fp8_product", k_fp8_product<P, exact, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(p));
+        KLAUNCH(st, "k_fp8_product", k_fp8_product<P, exact, 256, 256, 2, 4, 2><<<blocks(1), 512, 0, st>>>(p));
       else if (pl.tile == 128)
-        KLAUNCH(st, "k_fp8_product", k_fp8_product<P, exact, 128, 128, 2, 2, 2><<<grid, 256, 0, st>>>(p));
+        KLAUNCH(st, "k_fp8_product", k_fp8_product<P, exact, 128, 128, 2, 2, 2><<<blocks(2), 256, 0, st>>>(p));
       else
-        KLAUNCH(st, "k_fp8_product", k_fp8_product<P, exact, 64, 64, 4, 1, 4><<<grid, 256, 0, st>>>(p));
+        KLAUNCH(st, "k_fp8_product", k_fp8_product<P, exact, 64, 64, 4, 1, 4><<<blocks(2), 256, 0, st>>>(p));
       return CHGNET_OK;
     };
     if (pl.splits == 1) return launch(T{});
