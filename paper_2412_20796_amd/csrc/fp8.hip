@@ -622,6 +622,287 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
   }
 }
 
+// Up to 16 rows of a, where what takes the time is b's codes: a block has NT x 16
+// columns, and its eight wavefronts the blocks of K in turn; b goes from memory to
+// registers, two blocks of K at a time. QUANT: a is rows of T in place of codes
+// (x), quantised by each wavefront as it needs them, which costs less than a launch:
+// lane group g of a block of K has the values 32 g .. 32 g + 31 of row lane % 16, and
+// the largest of the four groups is the block's.
+template <class T, bool EXACT, bool QUANT, bool VEC, int NT>
+__global__ void __launch_bounds__(512) k_fp8_few(ProductArgs p, const T* __restrict__ x, int64_t ldx) {
+  constexpr int WAVES = 8;
+  __shared__ v4f parts[WAVES][NT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, g = lane >> 4;
+  const int64_t M = p.a.rows, N = p.b.rows, K = p.K, n0 = (int64_t)blockIdx.x * 16 * NT;
+  const int64_t m = r16 < M ? r16 : M - 1;  // rows past the end: the last one again
+  const int nkb = (int)((K + kBlock - 1) / kBlock);
+  const uint8_t *b[NT], *sb[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int64_t n = n0 + 16 * j + r16 < N ? n0 + 16 * j + r16 : N - 1;
+    b[j] = p.b.codes + n * p.b.ldc + 32 * g;
+    sb[j] = p.b.scale + (n >> p.b.shift) * p.b.lds;
+  }
+  const uint8_t* a = QUANT ? nullptr : p.a.codes + m * p.a.ldc;
+  const uint8_t* sa = QUANT ? nullptr : p.a.scale + (m >> p.a.shift) * p.a.lds;
+  const T* xr = QUANT ? x + m * ldx : nullptr;
+  v4f acc[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) acc[j] = v4f{0.f, 0.f, 0.f, 0.f};
+  struct In {
+    uint4 b[NT][2];
+    Eight<T> x[QUANT ? 4 : 1];
+    uint4 a[QUANT ? 1 : 2];
+    unsigned eb[NT], ea;
+  };
+  auto load = [&](int kb, In& in) {
+    const int64_t c = (int64_t)kb * kBlock + 32 * g;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool there = c + 16 * h < K;  // (bytes between K and the next multiple of 16 are 0)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        in.b[j][h] = there ? *reinterpret_cast<const uint4*>(b[j] + (int64_t)kb * kBlock + 16 * h) : zero;
+      if constexpr (!QUANT) in.a[h] = there ? *reinterpret_cast<const uint4*>(a + c + 16 * h) : zero;
+    }
+    if constexpr (QUANT) {
+      if (VEC && c + 32 <= K) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) in.x[q].load(xr + c + 8 * q);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) in.x[q].load_some(xr + c + 8 * q, K - c - 8 * q);
+      }
+    } else {
+      in.ea = sa[kb];
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) in.eb[j] = sb[j][kb];
+  };
+  auto multiply = [&](In& in) {
+    uint2 qa[4];
+    if constexpr (QUANT) {
+      using E = Eight<T>;
+      unsigned big = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int k = 0; k < E::NW; ++k) big = E::larger(big, E::below_sign(in.x[q].w[k]));
+      in.ea = scale_byte(groupmax_bits(E::largest(big)));
+      const float inv = scale_inverse(in.ea);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const E& v = in.x[q];
+        qa[q].x = codes4(v.get(0) * inv, v.get(1) * inv, v.get(2) * inv, v.get(3) * inv);
+        qa[q].y = codes4(v.get(4) * inv, v.get(5) * inv, v.get(6) * inv, v.get(7) * inv);
+      }
+    } else {
+      qa[0] = make_uint2(in.a[0].x, in.a[0].y);
+      qa[1] = make_uint2(in.a[0].z, in.a[0].w);
+      qa[2] = make_uint2(in.a[1].x, in.a[1].y);
+      qa[3] = make_uint2(in.a[1].z, in.a[1].w);
+    }
+    const v8i wa = {(int)qa[0].x, (int)qa[0].y, (int)qa[1].x, (int)qa[1].y, (int)qa[2].x, (int)qa[2].y, (int)qa[3].x, (int)qa[3].y};
+    v8b xa[EXACT ? 4 : 1];
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) xa[q] = wide(qa[q], scale_value(in.ea));
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const uint4 lo = in.b[j][0], hi = in.b[j][1];
+      if constexpr (EXACT) {
+        const float f = scale_value(in.eb[j]);
+        const uint2 qb[4] = {make_uint2(lo.x, lo.y), make_uint2(lo.z, lo.w), make_uint2(hi.x, hi.y), make_uint2(hi.z, hi.w)};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide(qb[q], f), xa[q], acc[j], 0, 0, 0);
+      } else {
+        const v8i wb = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+        acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[j], 0, 0, 0, in.eb[j], 0, in.ea);
+      }
+    }
+  };
+  In first, second;
+  int kb = wave;
+  if (kb < nkb) load(kb, first);
+  for (; kb < nkb; kb += 2 * WAVES) {
+    if (kb + WAVES < nkb) load(kb + WAVES, second);
+    multiply(first);
+    if (kb + 2 * WAVES < nkb) load(kb + 2 * WAVES, first);
+    if (kb + WAVES < nkb) multiply(second);
+  }
+  // columns n0 + 16 j + 4 g .. of row r16, summed over the wavefronts in order
+#pragma unroll
+  for (int j = 0; j < NT; ++j) parts[wave][j][lane] = acc[j];
+  __syncthreads();
+  if (wave >= NT || r16 >= M) return;
+  v4f sum = parts[0][wave][lane];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) sum += parts[w][wave][lane];
+  const int64_t n = n0 + 16 * wave + 4 * g;
+  float t[4] = {sum[0], sum[1], sum[2], sum[3]};
+  put(static_cast<T*>(p.out) + r16 * p.ldo + n, t, N - n, (p.ldo & 3) == 0 && ((uintptr_t)p.out & (4 * sizeof(T) - 1)) == 0,
+      p.add != 0);
+}
+
+// Linear layer of many rows to up to BN columns: a block has 64 rows of x, each
+// read once and quantised on its way to LDS, and all columns. Sixteen threads have
+// a row's 128 values of a step; those of the next step arrive while this one's are
+// multiplied. Places in LDS and operands are k_fp8_product's. x's codes have one
+// buffer, which all read before they multiply: two blocks have room on a compute unit.
+template <class T, bool EXACT, bool VEC, int BN>
+__global__ void __launch_bounds__(2 * BN, 4) k_fp8_rows_product(ProductArgs p, const T* __restrict__ x, int64_t ldx) {
+  constexpr int BM = 64, WN = BN / 64, THREADS = 2 * BN, TM = 2, TN = 4, W = 16 / sizeof(T);
+  constexpr int PIECES = BN * 8 / THREADS, XP = BM * 16 / THREADS, LOADS = XP * sizeof(T) / 2;
+  __shared__ __align__(1024) uint8_t la[BM * kBlock], lb[2][BN * kBlock];
+  __shared__ uint8_t scales[BM];
+  const int64_t M = p.a.rows, N = p.b.rows, K = p.K, m0 = (int64_t)blockIdx.x * BM;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN * 32, wn = wave % WN * 64, r16 = lane & 15, g = lane >> 4, key = r16 >> 1;
+  const int nkb = (int)((K + kBlock - 1) / kBlock);
+  const bool inside = VEC && m0 + BM <= M;
+
+  // b's codes, as in k_fp8_product
+  unsigned src[PIECES];
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    const int row = (i * THREADS + threadIdx.x) / 8, last = (int)N - 1;
+    src[i] = (unsigned)(row < last ? row : last) * (unsigned)p.b.ldc;
+  }
+  const unsigned key_b = W == 4 ? threadIdx.x >> 4 & 7 : (threadIdx.x >> 4 & 1) | (threadIdx.x >> 6 & 3) << 1;
+  const unsigned piece = 16 * ((threadIdx.x & 7) ^ key_b);
+  auto load_b = [&](int kb) {
+    const int64_t at = (int64_t)kb * kBlock;
+    uint8_t* to = lb[kb & 1] + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      if (at + piece < K) to_lds16(p.b.codes + at + (src[i] + piece), to + i * THREADS * 16);
+      else *reinterpret_cast<uint4*>(to + i * THREADS * 16 + lane * 16) = make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto column = [](int row, int j) { return (row >> 2) * W + (row & 3) + j / (W / 4) * 4 * W + j % (W / 4) * 4; };
+  const uint8_t* sb[TN];
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int n = wn + column(r16, j);
+    sb[j] = p.b.scale + ((n < N ? n : N - 1) >> p.b.shift) * p.b.lds;
+  }
+  // rows of x: row xr + i THREADS / 16, values 8 xc ..
+  const int xr = threadIdx.x >> 4, xc = threadIdx.x & 15;
+  Eight<T> v[XP];
+  auto load_x = [&](int kb) {
+    const int64_t c = (int64_t)kb * kBlock + 8 * xc;
+#pragma unroll
+    for (int i = 0; i < XP; ++i) {
+      const int64_t m = m0 + xr + i * (THREADS / 16);
+      const T* q = x + m * ldx + c;
+      if (inside && c + 8 <= K) v[i].load(q);
+      else v[i].load_some(q, m < M ? K - c : 0);
+    }
+  };
+  v4f acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+  if (nkb) {
+    load_b(0);
+    load_x(0);
+  }
+  for (int kb = 0; kb < nkb; ++kb) {
+#pragma unroll
+    for (int i = 0; i < XP; ++i) {
+      using E = Eight<T>;
+      const int row = xr + i * (THREADS / 16);
+      unsigned big = E::below_sign(v[i].w[0]);
+#pragma unroll
+      for (int q = 1; q < E::NW; ++q) big = E::larger(big, E::below_sign(v[i].w[q]));
+      const unsigned byte = scale_byte(rowmax_bits<16>(E::largest(big)));
+      const float inv = scale_inverse(byte);
+      const E& r = v[i];
+      uint2 q;
+      q.x = codes4(r.get(0) * inv, r.get(1) * inv, r.get(2) * inv, r.get(3) * inv);
+      q.y = codes4(r.get(4) * inv, r.get(5) * inv, r.get(6) * inv, r.get(7) * inv);
+      *reinterpret_cast<uint2*>(la + row * kBlock + ((xc >> 1) ^ (row >> 1 & 7)) * 16 + (xc & 1) * 8) = q;
+      if (xc == 0) scales[row] = (uint8_t)byte;
+    }
+    unsigned ea[TM], eb[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) eb[j] = sb[j][kb];
+    const bool more = kb + 1 < nkb;
+    if (more) load_x(kb + 1);
+    // b's codes are there (the rows of x loaded after them may be under way), and
+    // all have written theirs of a
+    if (more && inside && (int64_t)(kb + 2) * kBlock <= K) wait_barrier<LOADS>();
+    else wait_barrier<0>();
+    if (more) load_b(kb + 1);
+    v4i ra[TM][2];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      ea[i] = scales[wm + 16 * i + r16];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        ra[i][h] = *reinterpret_cast<const v4i*>(la + (wm + 16 * i + r16) * kBlock + ((g + 4 * h) ^ key) * 16);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // x's codes are read
+    auto half_b = [&](int j, int h) {
+      return *reinterpret_cast<const v4i*>(lb[kb & 1] + (wn + column(r16, j)) * kBlock + ((g + 4 * h) ^ key) * 16);
+    };
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        v8b aw[TM][2];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          const v4i q = ra[i][h];
+          aw[i][0] = wide(make_uint2(q[0], q[1]), scale_value(ea[i]));
+          aw[i][1] = wide(make_uint2(q[2], q[3]), scale_value(ea[i]));
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const v4i q = half_b(j, h);
+          const v8b b0 = wide(make_uint2(q[0], q[1]), scale_value(eb[j])), b1 = wide(make_uint2(q[2], q[3]), scale_value(eb[j]));
+#pragma unroll
+          for (int i = 0; i < TM; ++i) {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, aw[i][0], acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, aw[i][1], acc[i][j], 0, 0, 0);
+          }
+        }
+      }
+    } else {
+      v8i a[TM];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const v4i q = ra[i][0], r = ra[i][1];
+        a[i] = v8i{q[0], q[1], q[2], q[3], r[0], r[1], r[2], r[3]};
+      }
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const v4i q = half_b(j, 0), r = half_b(j, 1);
+        const v8i b = {q[0], q[1], q[2], q[3], r[0], r[1], r[2], r[3]};
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a[i], acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+      }
+    }
+  }
+  const bool vec = (p.ldo * sizeof(T) & 15) == 0 && ((uintptr_t)p.out & 15) == 0;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t m = m0 + wm + 16 * i + r16;
+#pragma unroll
+    for (int q = 0; q < 16 / W; ++q) {
+      const int64_t n = wn + q * 4 * W + g * W;
+      float t[W];
+#pragma unroll
+      for (int k = 0; k < W; ++k) t[k] = acc[i][(q * W + k) / 4][k % 4];
+      if (m < M) put(static_cast<T*>(p.out) + m * p.ldo + n, t, N - n, vec, false);
+    }
+  }
+}
+
 // out (+)= the sum of the splits' parts, in order; a thread has four columns
 template <class T>
 __global__ void __launch_bounds__(256) k_fp8_join(int64_t M, int64_t N, int splits, const float* __restrict__ part,
@@ -664,8 +945,10 @@ Factor factor(const chgnet_fp8* f) {
   return {f->codes, f->scale, f->ld, f->ld_scale, f->rows, f->block_rows == kBlock ? 7 : 0};
 }
 
+constexpr int64_t kFewRows = 16;
+
 struct Plan {
-  int tile;  // of tile x tile results
+  int tile;  // of tile x tile results; 0: few rows
   int64_t tiles;
   int splits, kb_split;
 };
@@ -678,6 +961,7 @@ struct Plan {
 constexpr int64_t kLeastSteps = 24, kUnits = 256;
 Plan plan(int64_t M, int64_t N, int64_t K) {
   const int64_t nkb = std::max<int64_t>(1, cdiv(K, kBlock)), most = std::max<int64_t>(1, nkb / kLeastSteps);
+  if (M <= kFewRows) return {0, 0, 1, (int)nkb};
   auto tiles = [&](int t) { return cdiv(M, t) * cdiv(N, t); };
   const int tile = tiles(256) * most >= kUnits ? 256 : tiles(128) * most >= kUnits ? 128 : 64;
   const int64_t n = tiles(tile), want = tile == 64 ? 2 * kUnits / n : cdiv(kUnits, n);
@@ -685,6 +969,37 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
   const int64_t per = cdiv(cdiv(nkb, s), 4) * 4;  // (of whole words of scales)
   return {tile, n, (int)cdiv(nkb, per), (int)per};
 }
+// Columns of a block: twice as many where that leaves a block for each compute unit
+// (16 rows of 8,192 to 8,192 in bf16: 31 us in blocks of 16 columns, 24 of 32, 32 of
+// 64; one row of 4,096 to 4,096: 8.3, 8.4, 12)
+template <class T, bool QUANT, bool VEC>
+int launch_few(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
+  constexpr bool exact = std::is_same<T, float>::value;
+  auto launch = [&](auto nt) -> int {
+    KLAUNCH(st, "k_fp8_few", k_fp8_few<T, exact, QUANT, VEC, nt.value>
+                             <<<(unsigned)cdiv(p.b.rows, 16 * nt.value), 512, 0, st>>>(p, x, ldx));
+    return CHGNET_OK;
+  };
+  if (p.b.rows >= 32 * kUnits) return launch(std::integral_constant<int, 2>{});
+  return launch(std::integral_constant<int, 1>{});
+}
+
+// Whether a linear layer quantises its rows on the way: where each is needed once
+// and the blocks fill the GPU (us of a call against quantiser and product, bf16: 397,934
+// rows of 512 to 256 187 and 227, to 128 114 and 211, 85,274 of 256 to 128 18 and 32; fp32 rows
+// 326 and 392, 196 and 354, 27 and 48; 5,000 of 512 to 256 9 and 11, in fp32 14 and 12)
+bool on_the_way(int64_t M, int64_t N) { return N <= 256 && cdiv(M, 64) >= kUnits; }
+template <class T, bool VEC>
+int launch_rows_product(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
+  constexpr bool exact = std::is_same<T, float>::value;
+  const unsigned blocks = (unsigned)cdiv(p.a.rows, 64);
+  if (p.b.rows <= 128)
+    KLAUNCH(st, "k_fp8_rows_product", k_fp8_rows_product<T, exact, VEC, 128><<<blocks, 256, 0, st>>>(p, x, ldx));
+  else
+    KLAUNCH(st, "k_fp8_rows_product", k_fp8_rows_product<T, exact, VEC, 256><<<blocks, 512, 0, st>>>(p, x, ldx));
+  return CHGNET_OK;
+}
+
 int64_t part_ld(int64_t N) { return cdiv(N, 4) * 4; }
 
 }  // namespace
@@ -775,6 +1090,9 @@ int fp8_matmul_entry(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, vo
   return with_type(dtype, [&](auto v) -> int {
     using T = decltype(v);
     constexpr bool exact = std::is_same<T, float>::value;
+    if (pl.tile == 0) {
+      return launch_few<T, false, true>(p, nullptr, 0, st);
+    }
     auto launch = [&](auto part) -> int {
       using P = decltype(part);
       // as many blocks as have room at a time
@@ -816,7 +1134,7 @@ int fp8_linear_workspace_entry(int64_t M, int64_t N, int64_t K, size_t* bytes) {
   size_t product = 0;
   CHG_TRY(fp8_matmul_workspace_entry(M, N, K, &product));
   if (!bytes) return bad("fp8_linear_workspace", "bytes is NULL");
-  *bytes = M && N && K ? linear_ws(M, K, product, nullptr).total : 0;
+  *bytes = M > kFewRows && N && K && !on_the_way(M, N) ? linear_ws(M, K, product, nullptr).total : 0;
   return CHGNET_OK;
 }
 
@@ -831,6 +1149,19 @@ int fp8_linear_entry(int64_t rows, int32_t dtype, const void* x, int64_t ldx, co
   const size_t es = elem_size(dtype);
   if (!out || (!x && w->cols)) return bad(who, "null argument");
   if (!aligned_to(x, es) || !aligned_to(out, es)) return bad(who, "an array is not aligned to its values");
+  if (rows <= kFewRows || on_the_way(rows, w->rows)) {
+    ProductArgs p{};
+    p.a.rows = rows, p.b = factor(w), p.K = w->cols, p.out = out, p.ldo = ldout;
+    const bool vec = ldx * es % 16 == 0 && aligned_to(x, 16);
+    return with_type(dtype, [&](auto v) -> int {
+      using T = decltype(v);
+      if (rows > kFewRows)
+        return vec ? launch_rows_product<T, true>(p, static_cast<const T*>(x), ldx, st)
+                   : launch_rows_product<T, false>(p, static_cast<const T*>(x), ldx, st);
+      return vec ? launch_few<T, true, true>(p, static_cast<const T*>(x), ldx, st)
+                 : launch_few<T, true, false>(p, static_cast<const T*>(x), ldx, st);
+    });
+  }
   size_t product = 0;
   CHG_TRY(fp8_matmul_workspace_entry(rows, w->rows, w->cols, &product));
   const LinearWs l = linear_ws(rows, w->cols, product, ws);
