@@ -13,7 +13,7 @@ B = dict(A, rows=9, block_rows=128)
 T = dict(rows=200, cols=8, codes=P, ld=16, scale=P, ld_scale=4, block_rows=1)
 QUANT = dict(rows=8, cols=200, dtype=0, x=P, ldx=200, q=A, t=T, stream=None)
 MUL = dict(a=A, b=B, dtype=0, out=P, ldout=9, accumulate=0, ws=None, ws_bytes=0, stream=None)
-LIN = dict(rows=8, dtype=1, x=P, ldx=200, w=B, out=P, ldout=9, ws=P, ws_bytes=1 << 20, stream=None)
+LIN = dict(rows=100, dtype=1, x=P, ldx=200, w=B, out=P, ldout=9, ws=P, ws_bytes=1 << 20, stream=None)
 
 
 def _call(fn, base, **kw):
@@ -59,7 +59,7 @@ def test_bad_arguments(fn, base, kw):
 def test_small_workspace():
     assert _call("chgnet_fp8_linear", LIN, rows=300, ws_bytes=100) == bd.CHGNET_EWORKSPACE
     assert _call("chgnet_fp8_linear", LIN, rows=300, ws=None) == bd.CHGNET_EWORKSPACE
-    long = dict(a_cols=1 << 20, a_ld=1 << 20, a_ld_scale=1 << 13, b_cols=1 << 20, b_ld=1 << 20, b_ld_scale=1 << 13)
+    long = dict(a_rows=100, a_cols=1 << 20, a_ld=1 << 20, a_ld_scale=1 << 13, b_cols=1 << 20, b_ld=1 << 20, b_ld_scale=1 << 13)
     assert _call("chgnet_fp8_matmul", MUL, **long) == bd.CHGNET_EWORKSPACE
 
 
