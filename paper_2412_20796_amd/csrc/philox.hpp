@@ -55,14 +55,20 @@ struct Philox {
     w[2] = a2;
     w[3] = a3;
   }
+  // whether the upper (lower) 16 bits of a word are at least `cut`: one comparison
+  // each (a cut of 65,536 is above both)
+  static __device__ __forceinline__ bool upper(uint32_t w, uint32_t cut) { return cut <= 65535u && w >= cut << 16; }
+  static __device__ __forceinline__ bool lower(uint32_t w, uint32_t cut) {
+    return cut <= 65535u && (uint16_t)w >= (uint16_t)cut;
+  }
   // bit k: column 8 group + k is kept
   __device__ __forceinline__ uint32_t mask8(uint32_t row, uint32_t group, uint32_t cut) const {
     uint32_t w[4], m = 0;
     words(row, group, w);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      m |= (uint32_t)((w[k] & 0xffffu) >= cut) << (2 * k);
-      m |= (uint32_t)((w[k] >> 16) >= cut) << (2 * k + 1);
+      m |= (uint32_t)lower(w[k], cut) << (2 * k);
+      m |= (uint32_t)upper(w[k], cut) << (2 * k + 1);
     }
     return m;
   }

@@ -63,6 +63,27 @@ struct Row {
       for (int k = 0; k < VEC; ++k) v[q * VEC + k] = t[k];
     }
   }
+  // the same as they are stored, for rows that are loaded ahead
+  template <class T>
+  struct Raw {
+    typedef T vec __attribute__((ext_vector_type(VEC)));
+    vec q[NQ];
+  };
+  template <class T>
+  __device__ __forceinline__ void load(const T* p, Raw<T>& r) const {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      r.q[q] = typename Raw<T>::vec{};
+      if (has(q)) r.q[q] = *reinterpret_cast<const typename Raw<T>::vec*>(p + col(q));
+    }
+  }
+  template <class T>
+  __device__ __forceinline__ void values(const Raw<T>& r, float (&v)[CPL]) const {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) v[q * VEC + k] = (float)r.q[q][k];
+  }
   template <class T>
   __device__ __forceinline__ void store(T* p, const float (&v)[CPL]) const {
 #pragma unroll
@@ -111,7 +132,12 @@ struct Row {
     return s;
   }
   // x 2^-h, less the mean for a LayerNorm (0 in columns past d)
-  __device__ __forceinline__ void center(float (&x)[CPL], float mean, const Scale& sc) const {
+  __device__ __forceinline__ void center(float (&x)[CPL], bool layer, float mean, const Scale& sc) const {
+    if (!layer) {
+#pragma unroll
+      for (int k = 0; k < CPL; ++k) x[k] *= sc.dev;
+      return;
+    }
     const float m = mean * sc.dev;
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
@@ -127,16 +153,57 @@ struct Row {
     for (int k = 0; k < CPL; ++k) s = fmaf(a[k], b[k], s);
     return s;
   }
-  // which of the thread's values a dropout keeps, a bit each
-  __device__ __forceinline__ uint32_t kept(const Philox& rng, int64_t row, uint32_t cut) const {
-    uint32_t m = 0;
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      const int c = col(q);
-      const uint32_t b = rng.mask8((uint32_t)row, (uint32_t)c >> 3, cut) >> (c & 7);
-      m |= (b & ((1u << VEC) - 1)) << (q * VEC);
+  // Which of the thread's values a dropout keeps: the generator's words of groups of
+  // 8 columns (of 4: the half of them), compared where they are used; or a bit each,
+  // where a thread has single columns. There each of 8 lanes beside each other, which
+  // share their groups, forms another one's mask, and they exchange them.
+  struct Keep {
+    static constexpr int WORDS = VEC >= 4 ? NQ * VEC / 2 : 1;
+    uint32_t w[WORDS], cut;
+    __device__ __forceinline__ bool operator()(int k) const {
+      if constexpr (VEC >= 4) return k & 1 ? Philox::upper(w[k / 2], cut) : Philox::lower(w[k / 2], cut);
+      else return w[0] >> k & 1;
     }
-    return m;
+  };
+  __device__ __forceinline__ void kept(const Philox& rng, int64_t row, uint32_t cut, Keep& keep) const {
+    keep.cut = cut;
+    if constexpr (VEC >= 4) {
+      if (!cut) {
+#pragma unroll
+        for (int k = 0; k < Keep::WORDS; ++k) keep.w[k] = 0;
+        return;
+      }
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        uint32_t w[4];
+        rng.words((uint32_t)row, (uint32_t)col(q) >> 3, w);
+        if constexpr (VEC == 8) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) keep.w[4 * q + k] = w[k];
+        } else {
+          const bool second = col(q) & 4;
+          keep.w[2 * q] = second ? w[2] : w[0];
+          keep.w[2 * q + 1] = second ? w[3] : w[1];
+        }
+      }
+    } else {
+      keep.w[0] = ~0u;
+      if (!cut) return;
+      uint32_t bits = 0;
+      const int lane = threadIdx.x & 63;
+#pragma unroll
+      for (int q0 = 0; q0 < NQ; q0 += 8) {
+        constexpr int S = NQ < 8 ? NQ : 8;
+        const int q = q0 + (j & (S - 1));
+        const uint32_t mine = rng.mask8((uint32_t)row, (uint32_t)(q * TPR + j) >> 3, cut);
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+          const uint32_t m = (uint32_t)__builtin_amdgcn_ds_bpermute(((lane & ~7) + i) * 4, (int)mine);
+          bits |= (m >> (j & 7) & 1) << (q0 + i);
+        }
+      }
+      keep.w[0] = bits;
+    }
   }
 };
 
@@ -168,12 +235,18 @@ __device__ __forceinline__ float stored(float v) {
   return (float)(T)v;
 }
 
+// Threads of a forward block: a row of more than a wavefront has one to itself,
+// whose barriers are its sums'
+template <int TPR>
+constexpr int fwd_threads() {
+  return TPR > 64 ? TPR : 256;
+}
 // RES false: a norm alone, h = w n(x) + b
 template <class T, int VEC, int TPR, int NQ, bool RES>
-__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) k_residual_fwd(ResArgs a) {
+__global__ void __launch_bounds__(fwd_threads<TPR>()) k_residual_fwd(ResArgs a) {
   using R = Row<VEC, TPR, NQ>;
   constexpr int CPL = R::CPL;
-  constexpr int ROWS = (TPR > 256 ? TPR : 256) / TPR;  // of a block
+  constexpr int ROWS = fwd_threads<TPR>() / TPR;  // of a block
   __shared__ float red[2][4][16];
   const R row{(int)threadIdx.x % TPR, a.d};
   const Scale sc(a.d);
@@ -202,18 +275,19 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) k_residual_fwd(ResArgs 
           s[0] = row.part_sum(t, sc);
           row.sums(s, red, turn);
         }
-        row.center(t, s[0] * sc.mean, sc);
+        row.center(t, a.post_kind == kLayer, s[0] * sc.mean, sc);
         s[0] = row.part_dot(t, t);
         row.sums(s, red, turn);
         dev = deviation(s[0], a.eps, sc);
       }
       const float s1 = a.gate == 1 ? sigm(g1) : 1.f;
-      const uint32_t m = a.drop.cut ? row.kept(rng, r, a.drop.cut) : ~0u;
+      typename R::Keep keep;
+      row.kept(rng, r, a.drop.cut, keep);
       const float beta = a.beta * a.drop.scale;
 #pragma unroll
       for (int k = 0; k < CPL; ++k) {
         const float u = fmaf(wp[k], t[k] * dev, bp[k]) * (a.gate == 2 ? sigm(g[k]) : s1);
-        y[k] = fmaf(a.alpha, y[k], m >> k & 1 ? beta * u : 0.f);
+        y[k] = fmaf(a.alpha, y[k], keep(k) ? beta * u : 0.f);
         y[k] = stored<T>(y[k]);
       }
       row.store(static_cast<T*>(a.o0) + r * a.ld0, y);
@@ -224,7 +298,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) k_residual_fwd(ResArgs 
         s[0] = row.part_sum(y, sc);
         row.sums(s, red, turn);
       }
-      row.center(y, s[0] * sc.mean, sc);
+      row.center(y, a.pre_kind == kLayer, s[0] * sc.mean, sc);
       s[0] = row.part_dot(y, y);
       row.sums(s, red, turn);
       const float dev = deviation(s[0], a.eps, sc);
@@ -276,14 +350,19 @@ __device__ __forceinline__ void join(const Row<VEC, TPR, NQ>& row, const float (
   }
 }
 
+// The next row is loaded before the present one is worked on where a thread has
+// registers for it (one group of a row); with 1,024 threads a row, which have 128
+// registers each, the norms' parameters make room for it in LDS.
 template <class T, int VEC, int TPR, int NQ, bool RES>
 __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) {
   using R = Row<VEC, TPR, NQ>;
   constexpr int CPL = R::CPL, ROWS = bwd_threads<TPR>() / TPR, G = bwd_threads<TPR>() / (TPR > 64 ? TPR : 64);
+  constexpr bool PARAMS_IN_LDS = RES && TPR == 1024 && VEC > 1 && CPL <= 8, AHEAD = VEC > 1 && NQ == 1;
   // several rows of more than a wavefront in a block would not meet at the
   // barriers of their sums: each has its own buffers, and all walk as many rows
   __shared__ float red_all[TPR > 64 ? ROWS : 1][2][4][16];
   __shared__ float join_s[G > 1 ? G * VEC * TPR * NQ : 1];
+  __shared__ float params[PARAMS_IN_LDS ? 3 : 1][PARAMS_IN_LDS ? VEC * TPR * NQ : 1];
   float(*red)[4][16] = red_all[TPR > 64 ? threadIdx.x / TPR : 0];
   const R row{(int)threadIdx.x % TPR, a.d};
   const Scale sc(a.d);
@@ -295,33 +374,73 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
     row.load_any(a.post_rows == 2 ? a.post + a.d : nullptr, bp, 0.f);
   }
   row.load_any(a.pre, w, 1.f);
+  if constexpr (PARAMS_IN_LDS) {  // (each thread reads what it wrote itself)
+#pragma unroll
+    for (int k = 0; k < CPL; ++k) {
+      params[0][threadIdx.x * CPL + k] = wp[k];
+      params[1][threadIdx.x * CPL + k] = bp[k];
+      params[2][threadIdx.x * CPL + k] = w[k];
+    }
+  }
+  int lds_at = threadIdx.x * CPL;
+  auto param = [&](int which, float (&v)[CPL]) {
+    if constexpr (PARAMS_IN_LDS) {
+      asm volatile("" : "+v"(lds_at));  // read for each row: kept from moving out of the loop into registers
+#pragma unroll
+      for (int k = 0; k < CPL; ++k) v[k] = params[which][lds_at + k];
+    }
+  };
   float awp[CPL] = {}, abp[CPL] = {}, aw[CPL] = {}, ab[CPL] = {};
   const Philox rng(a.drop);
   const int64_t stride = (int64_t)gridDim.x * ROWS;
-  for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += stride) {
-    const int64_t r = first + threadIdx.x / TPR;
-    const bool live = r < a.rows;
-    const int64_t at = live ? r : a.rows - 1;  // a row again, whose results go nowhere
-    float D[CPL] = {}, y[CPL] = {}, dh[CPL] = {}, f[CPL] = {}, g[CPL] = {};
-    float s1 = 1.f;
-    if (a.dy) row.load(static_cast<const T*>(a.dy) + at * a.lddy, D);
+  struct In {
+    typename R::template Raw<T> dy, y, dh, f, g;
+    float g1;
+  } in;
+  auto load = [&](int64_t at) {
+    if (a.dy) row.load(static_cast<const T*>(a.dy) + at * a.lddy, in.dy);
     if (a.pre) {
-      row.load(static_cast<const T*>(a.x) + at * a.ldx, y);
-      row.load(static_cast<const T*>(a.dh) + at * a.lddh, dh);
+      row.load(static_cast<const T*>(a.x) + at * a.ldx, in.y);
+      row.load(static_cast<const T*>(a.dh) + at * a.lddh, in.dh);
     }
     if constexpr (RES) {
-      if (a.f) row.load(static_cast<const T*>(a.f) + at * a.ldf, f);
-      if (a.gate == 2) row.load(static_cast<const T*>(a.g) + at * a.ldg, g);
-      if (a.gate == 1) s1 = sigm((float)static_cast<const T*>(a.g)[at * a.ldg]);
+      if (a.f) row.load(static_cast<const T*>(a.f) + at * a.ldf, in.f);
+      if (a.gate == 2) row.load(static_cast<const T*>(a.g) + at * a.ldg, in.g);
+      if (a.gate == 1) in.g1 = (float)static_cast<const T*>(a.g)[at * a.ldg];
     }
-    const bool norm_f = RES && a.post_kind != kNoNorm;
+  };
+  auto row_of = [&](int64_t first) {  // or the last row again, whose results go nowhere
+    const int64_t r = first + threadIdx.x / TPR;
+    return r < a.rows ? r : a.rows - 1;
+  };
+  if (AHEAD && (int64_t)blockIdx.x * ROWS < a.rows) load(row_of((int64_t)blockIdx.x * ROWS));
+  for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += stride) {
+    const int64_t r = first + threadIdx.x / TPR, at = row_of(first);
+    const bool live = r < a.rows;
+    float D[CPL] = {}, y[CPL] = {}, dh[CPL] = {}, f[CPL] = {}, g[CPL] = {};
+    float s1 = 1.f;
+    if (!AHEAD) load(at);
+    if (a.dy) row.values(in.dy, D);
+    if (a.pre) {
+      row.values(in.y, y);
+      row.values(in.dh, dh);
+    }
+    if constexpr (RES) {
+      if (a.f) row.values(in.f, f);
+      if (a.gate == 2) row.values(in.g, g);
+      if (a.gate == 1) s1 = sigm(in.g1);
+    }
+    if (AHEAD && first + stride < a.rows) load(row_of(first + stride));
+    const bool norm_f = RES && a.post_kind != kNoNorm, pre_layer = a.pre && a.pre_kind == kLayer,
+               post_layer = norm_f && a.post_kind == kLayer;
+    param(2, w);
     float mean[3] = {0.f, 0.f, 0.f};  // of y, f and w dh
-    if ((a.pre && a.pre_kind == kLayer) || (norm_f && a.post_kind == kLayer)) {
-      if (a.pre && a.pre_kind == kLayer) {
+    if (pre_layer || post_layer) {
+      if (pre_layer) {
         mean[0] = row.part_sum(y, sc);
         mean[2] = row.part_dot(w, dh);
       }
-      if (norm_f && a.post_kind == kLayer) mean[1] = row.part_sum(f, sc);
+      if (post_layer) mean[1] = row.part_sum(f, sc);
       row.sums(mean, red, turn);
       mean[0] *= sc.mean;
       mean[1] *= sc.mean;
@@ -331,13 +450,13 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
     {
       float q[3] = {0.f, 0.f, 0.f};  // squares of y and f, product of y and w dh
       if (a.pre) {
-        row.center(y, mean[0], sc);
+        row.center(y, pre_layer, mean[0], sc);
         q[0] = row.part_dot(y, y);
 #pragma unroll
         for (int k = 0; k < CPL; ++k) q[2] = fmaf(w[k] * dh[k], y[k], q[2]);
       }
       if (norm_f) {
-        row.center(f, mean[1], sc);
+        row.center(f, post_layer, mean[1], sc);
         q[1] = row.part_dot(f, f);
       }
       if (a.pre || norm_f) row.sums(q, red, turn);
@@ -345,46 +464,69 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
       if (a.pre) {
         const float dev = deviation(q[0], a.eps, sc), r1 = dev * sc.dev;
         const float c = dev > 0.f ? dev * q[2] * inv_d : 0.f;
+        if (live && a.pre_rows == 2) {
+#pragma unroll
+          for (int k = 0; k < CPL; ++k) ab[k] += dh[k];
+        }
 #pragma unroll
         for (int k = 0; k < CPL; ++k) {
           const float n = y[k] * dev;
-          if (live) {
-            aw[k] = fmaf(dh[k], n, aw[k]);
-            ab[k] += dh[k];
-          }
-          D[k] = fmaf(r1, fmaf(w[k], dh[k], -mean[2]) - n * c, D[k]);
+          if (live) aw[k] = fmaf(dh[k], n, aw[k]);
+          D[k] = fmaf(r1, fmaf(-n, c, fmaf(w[k], dh[k], -mean[2])), D[k]);
         }
       }
     }
     if constexpr (!RES) {
       if (live) row.store(static_cast<T*>(a.o0) + r * a.ld0, D);
     } else {
-      const uint32_t m = a.drop.cut ? row.kept(rng, at, a.drop.cut) : ~0u;
+      typename R::Keep keep;
+      row.kept(rng, at, a.drop.cut, keep);
       const float beta = a.beta * a.drop.scale;
+      param(0, wp);
+      param(1, bp);
       float q[3] = {0.f, 0.f, 0.f};  // of dm, dm n_p, and the one gate's gradient
+      if (a.post) {
 #pragma unroll
-      for (int k = 0; k < CPL; ++k) {
-        const bool keep = m >> k & 1;
-        const float du = beta * D[k], n = f[k] * dev_f;
-        D[k] *= a.alpha;
-        const float s = a.gate == 2 ? sigm(g[k]) : s1;
-        if (a.gate) {
-          const float dg = keep ? du * fmaf(wp[k], n, bp[k]) * s * (1.0f - s) : 0.f;
-          g[k] = dg;
-          q[2] += row.has(k / VEC) ? dg : 0.f;
-        }
-        const float dt = keep ? du * s : 0.f;
-        if (live && a.post) {
-          awp[k] = fmaf(dt, keep ? n : 0.f, awp[k]);
-          abp[k] += dt;
-        }
-        y[k] = wp[k] * dt;
-        f[k] = n;
+        for (int k = 0; k < CPL; ++k) f[k] *= dev_f;
       }
+      // y: the gradient of t
+      if (a.gate) {
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) {
+          const float du = beta * D[k], s = a.gate == 2 ? sigm(g[k]) : s1, dt = du * s;
+          g[k] = keep(k) ? dt * (1.0f - s) * fmaf(wp[k], f[k], bp[k]) : 0.f;
+          y[k] = keep(k) ? dt : 0.f;
+        }
+        if (a.gate == 2 && live) row.store(static_cast<T*>(a.o2) + r * a.ld2, g);
+        if (a.gate == 1) {
+#pragma unroll
+          for (int k = 0; k < CPL; ++k) q[2] += row.has(k / VEC) ? g[k] : 0.f;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) y[k] = keep(k) ? beta * D[k] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < CPL; ++k) D[k] *= a.alpha;
       if (live) row.store(static_cast<T*>(a.o0) + r * a.ld0, D);
-      if (a.gate == 2 && live) row.store(static_cast<T*>(a.o2) + r * a.ld2, g);
+      if (a.post) {
+        if (!norm_f) {  // what is dropped of f may be anything
+#pragma unroll
+          for (int k = 0; k < CPL; ++k) f[k] = keep(k) ? f[k] : 0.f;
+        }
+        if (live) {
+#pragma unroll
+          for (int k = 0; k < CPL; ++k) awp[k] = fmaf(y[k], f[k], awp[k]);
+          if (a.post_rows == 2) {
+#pragma unroll
+            for (int k = 0; k < CPL; ++k) abp[k] += y[k];
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) y[k] *= wp[k];
+      }
       if (norm_f) {
-        if (a.post_kind == kLayer)
+        if (post_layer)
 #pragma unroll
           for (int k = 0; k < CPL; ++k) q[0] += y[k];
         q[1] = row.part_dot(y, f);
@@ -394,7 +536,7 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
       if (norm_f) {
         const float r1 = dev_f * sc.dev, m0 = q[0] * inv_d, m1 = q[1] * inv_d;
 #pragma unroll
-        for (int k = 0; k < CPL; ++k) y[k] = r1 * (y[k] - m0 - f[k] * m1);
+        for (int k = 0; k < CPL; ++k) y[k] = r1 * fmaf(-f[k], m1, y[k] - m0);
       }
       if (live) row.store(static_cast<T*>(a.o1) + r * a.ld1, y);
     }
@@ -452,7 +594,7 @@ int with_layout(int d, bool vec, F&& f) {
       CHG_ROW(8, 16, 1)
       CHG_ROW(8, 32, 1)
       CHG_ROW(8, 64, 1)
-      CHG_ROW(8, 64, 2)
+      CHG_ROW(8, 128, 1)
       CHG_ROW(8, 256, 1)
       CHG_ROW(8, 512, 1)
       CHG_ROW(8, 1024, 1)
@@ -539,7 +681,7 @@ int launch_fwd(bool res, int32_t dtype, bool vec, const ResArgs& a, hipStream_t 
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
     return with_layout<T>(a.d, vec, [&](auto V, auto L, auto N) -> int {
-      constexpr int threads = L.value > 256 ? L.value : 256, rows = threads / L.value;
+      constexpr int threads = fwd_threads<L.value>(), rows = threads / L.value;
       const unsigned blocks = (unsigned)std::min<int64_t>(256 * 2048 / threads, cdiv(a.rows, rows));
       if (res)
         KLAUNCH(st, "k_residual_fwd", k_residual_fwd<T, V.value, L.value, N.value, true><<<blocks, threads, 0, st>>>(a));
