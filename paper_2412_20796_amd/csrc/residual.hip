@@ -419,16 +419,28 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
     const bool live = r < a.rows;
     float D[CPL] = {}, y[CPL] = {}, dh[CPL] = {}, f[CPL] = {}, g[CPL] = {};
     float s1 = 1.f;
-    if (!AHEAD) load(at);
-    if (a.dy) row.values(in.dy, D);
-    if (a.pre) {
-      row.values(in.y, y);
-      row.values(in.dh, dh);
-    }
-    if constexpr (RES) {
-      if (a.f) row.values(in.f, f);
-      if (a.gate == 2) row.values(in.g, g);
-      if (a.gate == 1) s1 = sigm(in.g1);
+    if constexpr (AHEAD) {
+      if (a.dy) row.values(in.dy, D);
+      if (a.pre) {
+        row.values(in.y, y);
+        row.values(in.dh, dh);
+      }
+      if constexpr (RES) {
+        if (a.f) row.values(in.f, f);
+        if (a.gate == 2) row.values(in.g, g);
+        if (a.gate == 1) s1 = sigm(in.g1);
+      }
+    } else {
+      if (a.dy) row.load(static_cast<const T*>(a.dy) + at * a.lddy, D);
+      if (a.pre) {
+        row.load(static_cast<const T*>(a.x) + at * a.ldx, y);
+        row.load(static_cast<const T*>(a.dh) + at * a.lddh, dh);
+      }
+      if constexpr (RES) {
+        if (a.f) row.load(static_cast<const T*>(a.f) + at * a.ldf, f);
+        if (a.gate == 2) row.load(static_cast<const T*>(a.g) + at * a.ldg, g);
+        if (a.gate == 1) s1 = sigm((float)static_cast<const T*>(a.g)[at * a.ldg]);
+      }
     }
     if (AHEAD && first + stride < a.rows) load(row_of(first + stride));
     const bool norm_f = RES && a.post_kind != kNoNorm, pre_layer = a.pre && a.pre_kind == kLayer,

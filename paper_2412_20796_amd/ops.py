@@ -430,7 +430,11 @@ def _residual(f, post, post_kind, gate, pre, pre_kind, alpha, beta, p, seed, cal
 
 
 def _any_followed(*tensors):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def residual_forward(x, f, post=None, post_kind=None, gate=None, pre=None, pre_kind="rms", alpha=1.0, beta=1.0, p=0.0, seed=0,
