@@ -45,53 +45,123 @@ struct Scale {
   }
 };
 
-// Row of d values in TPR threads: thread j holds the NQ groups of VEC values at
-// columns (q TPR + j) VEC.
-template <int VEC, int TPR, int NQ>
+// Row of d values in TPR threads: thread j holds the NQ groups of VEC values (16
+// bytes) at columns (q TPR + j) VEC. ANY: rows at any value's address, and a last
+// group that is short; the hardware takes 16 bytes at any address. A short group is
+// loaded whole where the array goes on behind it (the next row's values), and what
+// is past the row is cleared; it is stored in 8, 4 and 2 bytes. (Single values took
+// 265 and 203 us forward and backward for 40,000 rows of 1,001 in bf16 with all parts;
+// short groups value by value 131 and 310.)
+template <int VEC, int TPR, int NQ, bool ANY>
 struct Row {
-  static constexpr int CPL = VEC * NQ, WAVES = TPR > 64 ? TPR / 64 : 1, RPW = TPR > 64 ? 1 : 64 / TPR;
+  static constexpr int CPL = VEC * NQ, WAVES = TPR > 64 ? TPR / 64 : 1;
+  static constexpr int WHOLE = NQ / 2;  // groups that are never short: the next narrower layout holds them
   int j, d;
-  __device__ __forceinline__ int col(int q) const { return (q * TPR + j) * VEC; }
-  __device__ __forceinline__ bool has(int q) const { return col(q) < d; }
-  template <class T>
-  __device__ __forceinline__ void load(const T* p, float (&v)[CPL]) const {
+  uint32_t mask[ANY ? NQ - WHOLE : 1][4];
+  __device__ __forceinline__ Row(int thread, int width) : j(thread), d(width) {
+    if constexpr (ANY) {
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      float t[VEC] = {};
-      if (has(q)) load_v<VEC>(p + col(q), t);
+      for (int q = WHOLE; q < NQ; ++q)
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) v[q * VEC + k] = t[k];
+        for (int k = 0; k < 4; ++k) {
+          if constexpr (VEC == 8) mask[q - WHOLE][k] = (has(q, 2 * k) ? 0xffffu : 0u) | (has(q, 2 * k + 1) ? 0xffff0000u : 0u);
+          else mask[q - WHOLE][k] = has(q, k) ? ~0u : 0u;
+        }
     }
   }
-  // the same as they are stored, for rows that are loaded ahead
+  __device__ __forceinline__ int col(int q) const { return (q * TPR + j) * VEC; }
+  __device__ __forceinline__ bool has(int q, int k) const { return col(q) + (ANY ? k : 0) < d; }
+  // rows as they are stored, which may be loaded ahead
+  typedef uint32_t words __attribute__((ext_vector_type(4)));
   template <class T>
   struct Raw {
-    typedef T vec __attribute__((ext_vector_type(VEC)));
-    vec q[NQ];
+    words q[NQ];
   };
+  // `behind`: rows of the array after this one
   template <class T>
-  __device__ __forceinline__ void load(const T* p, Raw<T>& r) const {
+  __device__ __forceinline__ void load(const T* p, int64_t behind, int64_t ld, Raw<T>& r) const {
+    typedef words any __attribute__((aligned(2)));
+    typedef typename std::conditional<sizeof(T) == 4, uint32_t, uint16_t>::type bits;
+    const bool goes_on = behind * ld >= VEC - 1;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      r.q[q] = typename Raw<T>::vec{};
-      if (has(q)) r.q[q] = *reinterpret_cast<const typename Raw<T>::vec*>(p + col(q));
+      const int c = col(q);
+      r.q[q] = words{};
+      if constexpr (ANY) {
+        if (c + VEC <= d || (goes_on && c < d)) {
+          r.q[q] = *reinterpret_cast<const any*>(p + c);
+        } else {
+#pragma unroll
+          for (int k = 0; k < VEC - 1; ++k)
+            if (c + k < d)
+              r.q[q][k * 4 / VEC] |= (uint32_t)reinterpret_cast<const bits*>(p)[c + k] << (VEC == 8 && k % 2 ? 16 : 0);
+        }
+        if (q >= WHOLE) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) r.q[q][k] &= mask[q - WHOLE < 0 ? 0 : q - WHOLE][k];
+        }
+      } else if (c < d) {
+        r.q[q] = *reinterpret_cast<const words*>(p + c);
+      }
     }
   }
   template <class T>
   __device__ __forceinline__ void values(const Raw<T>& r, float (&v)[CPL]) const {
+    typedef T vec __attribute__((ext_vector_type(VEC)));
 #pragma unroll
-    for (int q = 0; q < NQ; ++q)
+    for (int q = 0; q < NQ; ++q) {
+      const vec t = __builtin_bit_cast(vec, r.q[q]);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) v[q * VEC + k] = (float)r.q[q][k];
+      for (int k = 0; k < VEC; ++k) v[q * VEC + k] = (float)t[k];
+    }
+  }
+  template <class T>
+  __device__ __forceinline__ void load(const T* p, int64_t behind, int64_t ld, float (&v)[CPL]) const {
+    Raw<T> r;
+    load(p, behind, ld, r);
+    values(r, v);
   }
   template <class T>
   __device__ __forceinline__ void store(T* p, const float (&v)[CPL]) const {
+    typedef T vec __attribute__((ext_vector_type(VEC)));
+    typedef words any __attribute__((aligned(2)));
+    typedef uint32_t two __attribute__((ext_vector_type(2)));
+    typedef two any2 __attribute__((aligned(2)));
+    typedef uint32_t any1 __attribute__((aligned(2)));
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      float t[VEC];
+      const int c = col(q);
+      vec t;
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) t[k] = v[q * VEC + k];
-      if (has(q)) store_v<VEC>(p + col(q), t);
+      for (int k = 0; k < VEC; ++k) t[k] = (T)v[q * VEC + k];
+      const words w = __builtin_bit_cast(words, t);
+      if constexpr (ANY) {
+        if (c + VEC <= d) {
+          *reinterpret_cast<any*>(p + c) = w;
+        } else if (c < d) {
+          const int n = d % VEC;  // values of the short group; `at`: words that are stored
+          const int half = VEC / 2;
+          int at = 0;
+          if (n >= half) {
+            *reinterpret_cast<any2*>(p + c) = two{w[0], w[1]};
+            at = 2;
+          }
+          if constexpr (VEC == 8) {
+            if (n & 2) {
+              *reinterpret_cast<any1*>(p + c + 2 * at) = at ? w[2] : w[0];
+              ++at;
+            }
+            if (n & 1) {
+              const uint32_t last = at == 0 ? w[0] : at == 1 ? w[1] : at == 2 ? w[2] : w[3];
+              *reinterpret_cast<uint16_t*>(p + c + 2 * at) = (uint16_t)last;
+            }
+          } else if (n & 1) {
+            *reinterpret_cast<uint32_t*>(p + c + at) = at ? w[2] : w[0];
+          }
+        }
+      } else if (c < d) {
+        *reinterpret_cast<words*>(p + c) = w;
+      }
     }
   }
   // parameters, which may sit at any float; `other` where there are none
@@ -99,7 +169,7 @@ struct Row {
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) v[q * VEC + k] = !has(q) ? 0.f : p ? p[col(q) + k] : other;
+      for (int k = 0; k < VEC; ++k) v[q * VEC + k] = !has(q, k) ? 0.f : p ? p[col(q) + k] : other;
   }
   // sums over the row of N values a thread, in every thread. The two buffers of
   // wide rows take turns: whoever writes to one has passed the barrier of the
@@ -144,7 +214,7 @@ struct Row {
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {
         float& y = x[q * VEC + k];
-        y = has(q) ? fmaf(y, sc.dev, -m) : 0.f;
+        y = has(q, k) ? fmaf(y, sc.dev, -m) : 0.f;
       }
   }
   __device__ __forceinline__ float part_dot(const float (&a)[CPL], const float (&b)[CPL]) const {
@@ -154,55 +224,32 @@ struct Row {
     return s;
   }
   // Which of the thread's values a dropout keeps: the generator's words of groups of
-  // 8 columns (of 4: the half of them), compared where they are used; or a bit each,
-  // where a thread has single columns. There each of 8 lanes beside each other, which
-  // share their groups, forms another one's mask, and they exchange them.
+  // 8 columns (of 4: the half of them), compared where they are used.
   struct Keep {
-    static constexpr int WORDS = VEC >= 4 ? NQ * VEC / 2 : 1;
-    uint32_t w[WORDS], cut;
+    uint32_t w[CPL / 2], cut;
     __device__ __forceinline__ bool operator()(int k) const {
-      if constexpr (VEC >= 4) return k & 1 ? Philox::upper(w[k / 2], cut) : Philox::lower(w[k / 2], cut);
-      else return w[0] >> k & 1;
+      return k & 1 ? Philox::upper(w[k / 2], cut) : Philox::lower(w[k / 2], cut);
     }
   };
   __device__ __forceinline__ void kept(const Philox& rng, int64_t row, uint32_t cut, Keep& keep) const {
     keep.cut = cut;
-    if constexpr (VEC >= 4) {
-      if (!cut) {
+    if (!cut) {
 #pragma unroll
-        for (int k = 0; k < Keep::WORDS; ++k) keep.w[k] = 0;
-        return;
+      for (int k = 0; k < CPL / 2; ++k) keep.w[k] = 0;
+      return;
+    }
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      uint32_t w[4];
+      rng.words((uint32_t)row, (uint32_t)col(q) >> 3, w);
+      if constexpr (VEC == 8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) keep.w[4 * q + k] = w[k];
+      } else {
+        const bool second = col(q) & 4;
+        keep.w[2 * q] = second ? w[2] : w[0];
+        keep.w[2 * q + 1] = second ? w[3] : w[1];
       }
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        uint32_t w[4];
-        rng.words((uint32_t)row, (uint32_t)col(q) >> 3, w);
-        if constexpr (VEC == 8) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) keep.w[4 * q + k] = w[k];
-        } else {
-          const bool second = col(q) & 4;
-          keep.w[2 * q] = second ? w[2] : w[0];
-          keep.w[2 * q + 1] = second ? w[3] : w[1];
-        }
-      }
-    } else {
-      keep.w[0] = ~0u;
-      if (!cut) return;
-      uint32_t bits = 0;
-      const int lane = threadIdx.x & 63;
-#pragma unroll
-      for (int q0 = 0; q0 < NQ; q0 += 8) {
-        constexpr int S = NQ < 8 ? NQ : 8;
-        const int q = q0 + (j & (S - 1));
-        const uint32_t mine = rng.mask8((uint32_t)row, (uint32_t)(q * TPR + j) >> 3, cut);
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-          const uint32_t m = (uint32_t)__builtin_amdgcn_ds_bpermute(((lane & ~7) + i) * 4, (int)mine);
-          bits |= (m >> (j & 7) & 1) << (q0 + i);
-        }
-      }
-      keep.w[0] = bits;
     }
   }
 };
@@ -242,13 +289,13 @@ constexpr int fwd_threads() {
   return TPR > 64 ? TPR : 256;
 }
 // RES false: a norm alone, h = w n(x) + b
-template <class T, int VEC, int TPR, int NQ, bool RES>
+template <class T, int VEC, int TPR, int NQ, bool ANY, bool RES>
 __global__ void __launch_bounds__(fwd_threads<TPR>()) k_residual_fwd(ResArgs a) {
-  using R = Row<VEC, TPR, NQ>;
+  using R = Row<VEC, TPR, NQ, ANY>;
   constexpr int CPL = R::CPL;
   constexpr int ROWS = fwd_threads<TPR>() / TPR;  // of a block
   __shared__ float red[2][4][16];
-  const R row{(int)threadIdx.x % TPR, a.d};
+  const R row((int)threadIdx.x % TPR, a.d);
   const Scale sc(a.d);
   int turn = 0;
   float wp[CPL], bp[CPL], w[CPL], b[CPL];
@@ -261,12 +308,13 @@ __global__ void __launch_bounds__(fwd_threads<TPR>()) k_residual_fwd(ResArgs a) 
   const Philox rng(a.drop);
   for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; r < a.rows; r += (int64_t)gridDim.x * ROWS) {
     float y[CPL];
-    row.load(static_cast<const T*>(a.x) + r * a.ldx, y);
+    const int64_t behind = a.rows - 1 - r;
+    row.load(static_cast<const T*>(a.x) + r * a.ldx, behind, a.ldx, y);
     if constexpr (RES) {
       float t[CPL];
-      row.load(static_cast<const T*>(a.f) + r * a.ldf, t);
+      row.load(static_cast<const T*>(a.f) + r * a.ldf, behind, a.ldf, t);
       float g[CPL] = {};
-      if (a.gate == 2) row.load(static_cast<const T*>(a.g) + r * a.ldg, g);
+      if (a.gate == 2) row.load(static_cast<const T*>(a.g) + r * a.ldg, behind, a.ldg, g);
       const float g1 = a.gate == 1 ? (float)static_cast<const T*>(a.g)[r * a.ldg] : 0.f;
       float dev = 1.f;
       if (a.post_kind != kNoNorm) {
@@ -319,8 +367,8 @@ constexpr int kBwdBlocks = 512;
 // Adds the block's sums of one parameter row into `o` (its row of the partial
 // sums, or with one block the destination itself): rows of one wavefront by lane
 // swaps, rows of several through LDS, in order.
-template <int VEC, int TPR, int NQ>
-__device__ __forceinline__ void join(const Row<VEC, TPR, NQ>& row, const float (&acc)[VEC * NQ], float* red, float* o,
+template <int VEC, int TPR, int NQ, bool ANY>
+__device__ __forceinline__ void join(const Row<VEC, TPR, NQ, ANY>& row, const float (&acc)[VEC * NQ], float* red, float* o,
                                      bool add) {
   constexpr int W = VEC * TPR * NQ, G = bwd_threads<TPR>() / (TPR > 64 ? TPR : 64);
   const int g = threadIdx.x / (TPR > 64 ? TPR : 64);
@@ -353,18 +401,18 @@ __device__ __forceinline__ void join(const Row<VEC, TPR, NQ>& row, const float (
 // The next row is loaded before the present one is worked on where a thread has
 // registers for it (one group of a row); with 1,024 threads a row, which have 128
 // registers each, the norms' parameters make room for it in LDS.
-template <class T, int VEC, int TPR, int NQ, bool RES>
+template <class T, int VEC, int TPR, int NQ, bool ANY, bool RES>
 __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) {
-  using R = Row<VEC, TPR, NQ>;
+  using R = Row<VEC, TPR, NQ, ANY>;
   constexpr int CPL = R::CPL, ROWS = bwd_threads<TPR>() / TPR, G = bwd_threads<TPR>() / (TPR > 64 ? TPR : 64);
-  constexpr bool PARAMS_IN_LDS = RES && TPR == 1024 && VEC > 1 && CPL <= 8, AHEAD = VEC > 1 && NQ == 1;
+  constexpr bool PARAMS_IN_LDS = RES && TPR == 1024 && CPL <= 8, AHEAD = NQ == 1;
   // several rows of more than a wavefront in a block would not meet at the
   // barriers of their sums: each has its own buffers, and all walk as many rows
   __shared__ float red_all[TPR > 64 ? ROWS : 1][2][4][16];
   __shared__ float join_s[G > 1 ? G * VEC * TPR * NQ : 1];
   __shared__ float params[PARAMS_IN_LDS ? 3 : 1][PARAMS_IN_LDS ? VEC * TPR * NQ : 1];
   float(*red)[4][16] = red_all[TPR > 64 ? threadIdx.x / TPR : 0];
-  const R row{(int)threadIdx.x % TPR, a.d};
+  const R row((int)threadIdx.x % TPR, a.d);
   const Scale sc(a.d);
   const float inv_d = 1.0f / (float)a.d;
   int turn = 0;
@@ -398,14 +446,14 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
     float g1;
   } in;
   auto load = [&](int64_t at) {
-    if (a.dy) row.load(static_cast<const T*>(a.dy) + at * a.lddy, in.dy);
+    if (a.dy) row.load(static_cast<const T*>(a.dy) + at * a.lddy, a.rows - 1 - at, a.lddy, in.dy);
     if (a.pre) {
-      row.load(static_cast<const T*>(a.x) + at * a.ldx, in.y);
-      row.load(static_cast<const T*>(a.dh) + at * a.lddh, in.dh);
+      row.load(static_cast<const T*>(a.x) + at * a.ldx, a.rows - 1 - at, a.ldx, in.y);
+      row.load(static_cast<const T*>(a.dh) + at * a.lddh, a.rows - 1 - at, a.lddh, in.dh);
     }
     if constexpr (RES) {
-      if (a.f) row.load(static_cast<const T*>(a.f) + at * a.ldf, in.f);
-      if (a.gate == 2) row.load(static_cast<const T*>(a.g) + at * a.ldg, in.g);
+      if (a.f) row.load(static_cast<const T*>(a.f) + at * a.ldf, a.rows - 1 - at, a.ldf, in.f);
+      if (a.gate == 2) row.load(static_cast<const T*>(a.g) + at * a.ldg, a.rows - 1 - at, a.ldg, in.g);
       if (a.gate == 1) in.g1 = (float)static_cast<const T*>(a.g)[at * a.ldg];
     }
   };
@@ -431,14 +479,14 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
         if (a.gate == 1) s1 = sigm(in.g1);
       }
     } else {
-      if (a.dy) row.load(static_cast<const T*>(a.dy) + at * a.lddy, D);
+      if (a.dy) row.load(static_cast<const T*>(a.dy) + at * a.lddy, a.rows - 1 - at, a.lddy, D);
       if (a.pre) {
-        row.load(static_cast<const T*>(a.x) + at * a.ldx, y);
-        row.load(static_cast<const T*>(a.dh) + at * a.lddh, dh);
+        row.load(static_cast<const T*>(a.x) + at * a.ldx, a.rows - 1 - at, a.ldx, y);
+        row.load(static_cast<const T*>(a.dh) + at * a.lddh, a.rows - 1 - at, a.lddh, dh);
       }
       if constexpr (RES) {
-        if (a.f) row.load(static_cast<const T*>(a.f) + at * a.ldf, f);
-        if (a.gate == 2) row.load(static_cast<const T*>(a.g) + at * a.ldg, g);
+        if (a.f) row.load(static_cast<const T*>(a.f) + at * a.ldf, a.rows - 1 - at, a.ldf, f);
+        if (a.gate == 2) row.load(static_cast<const T*>(a.g) + at * a.ldg, a.rows - 1 - at, a.ldg, g);
         if (a.gate == 1) s1 = sigm((float)static_cast<const T*>(a.g)[at * a.ldg]);
       }
     }
@@ -512,7 +560,7 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
         if (a.gate == 2 && live) row.store(static_cast<T*>(a.o2) + r * a.ld2, g);
         if (a.gate == 1) {
 #pragma unroll
-          for (int k = 0; k < CPL; ++k) q[2] += row.has(k / VEC) ? g[k] : 0.f;
+          for (int k = 0; k < CPL; ++k) q[2] += row.has(k / VEC, k % VEC) ? g[k] : 0.f;
         }
       } else {
 #pragma unroll
@@ -557,14 +605,14 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
   const bool one = gridDim.x == 1;
   if constexpr (RES) {
     if (a.post) {
-      join<VEC, TPR, NQ>(row, awp, join_s, one ? a.dpost : o, one && a.add);
-      if (a.post_rows == 2) join<VEC, TPR, NQ>(row, abp, join_s, one ? a.dpost + a.d : o + a.d, one && a.add);
+      join(row, awp, join_s, one ? a.dpost : o, one && a.add);
+      if (a.post_rows == 2) join(row, abp, join_s, one ? a.dpost + a.d : o + a.d, one && a.add);
     }
   }
   if (a.pre) {
     o += a.post_rows * a.d;
-    join<VEC, TPR, NQ>(row, aw, join_s, one ? a.dpre : o, one && a.add);
-    if (a.pre_rows == 2) join<VEC, TPR, NQ>(row, ab, join_s, one ? a.dpre + a.d : o + a.d, one && a.add);
+    join(row, aw, join_s, one ? a.dpre : o, one && a.add);
+    if (a.pre_rows == 2) join(row, ab, join_s, one ? a.dpre + a.d : o + a.d, one && a.add);
   }
 }
 
@@ -593,47 +641,38 @@ __global__ void __launch_bounds__(256) k_residual_zero(int n, float* __restrict_
   if (i < n) p[i] = 0.f;
 }
 
-// Calls f with the narrowest layout that holds rows of width d: 16 bytes a load
-// where alignment allows it, else single values.
+// Calls f with the narrowest layout that holds rows of width d.
 template <class T, class F>
 int with_layout(int d, bool vec, F&& f) {
   using std::integral_constant;
-#define CHG_ROW(V, TPR, NQ) \
-  if (d <= V * TPR * NQ) return f(integral_constant<int, V>{}, integral_constant<int, TPR>{}, integral_constant<int, NQ>{});
-  if (vec) {
-    if constexpr (sizeof(T) == 2) {
-      CHG_ROW(8, 8, 1)
-      CHG_ROW(8, 16, 1)
-      CHG_ROW(8, 32, 1)
-      CHG_ROW(8, 64, 1)
-      CHG_ROW(8, 128, 1)
-      CHG_ROW(8, 256, 1)
-      CHG_ROW(8, 512, 1)
-      CHG_ROW(8, 1024, 1)
-      CHG_ROW(8, 1024, 2)
-    } else {
-      CHG_ROW(4, 8, 1)
-      CHG_ROW(4, 16, 1)
-      CHG_ROW(4, 32, 1)
-      CHG_ROW(4, 64, 1)
-      CHG_ROW(4, 64, 2)
-      CHG_ROW(4, 256, 1)
-      CHG_ROW(4, 256, 2)
-      CHG_ROW(4, 512, 2)
-      CHG_ROW(4, 1024, 2)
-      CHG_ROW(4, 1024, 4)
-    }
+#define CHG_ROW(V, TPR, NQ)                                                                                              \
+  if (d <= V * TPR * NQ) {                                                                                               \
+    const integral_constant<int, V> v;                                                                                   \
+    const integral_constant<int, TPR> l;                                                                                 \
+    const integral_constant<int, NQ> n;                                                                                  \
+    return vec ? f(v, l, n, std::false_type{}) : f(v, l, n, std::true_type{});                                           \
+  }
+  if constexpr (sizeof(T) == 2) {
+    CHG_ROW(8, 8, 1)
+    CHG_ROW(8, 16, 1)
+    CHG_ROW(8, 32, 1)
+    CHG_ROW(8, 64, 1)
+    CHG_ROW(8, 128, 1)
+    CHG_ROW(8, 256, 1)
+    CHG_ROW(8, 512, 1)
+    CHG_ROW(8, 1024, 1)
+    CHG_ROW(8, 1024, 2)
   } else {
-    CHG_ROW(1, 16, 1)
-    CHG_ROW(1, 16, 4)
-    CHG_ROW(1, 32, 4)
-    CHG_ROW(1, 32, 8)
-    CHG_ROW(1, 64, 8)
-    CHG_ROW(1, 256, 4)
-    CHG_ROW(1, 256, 8)
-    CHG_ROW(1, 512, 8)
-    CHG_ROW(1, 1024, 8)
-    CHG_ROW(1, 1024, 16)
+    CHG_ROW(4, 8, 1)
+    CHG_ROW(4, 16, 1)
+    CHG_ROW(4, 32, 1)
+    CHG_ROW(4, 64, 1)
+    CHG_ROW(4, 64, 2)
+    CHG_ROW(4, 256, 1)
+    CHG_ROW(4, 256, 2)
+    CHG_ROW(4, 512, 2)
+    CHG_ROW(4, 1024, 2)
+    CHG_ROW(4, 1024, 4)
   }
 #undef CHG_ROW
   return fail(CHGNET_EINVAL, "residual: d must be in 1..16384");
@@ -692,13 +731,13 @@ int bwd_blocks(int64_t rows, int rows_a_block) {
 int launch_fwd(bool res, int32_t dtype, bool vec, const ResArgs& a, hipStream_t st) {
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    return with_layout<T>(a.d, vec, [&](auto V, auto L, auto N) -> int {
+    return with_layout<T>(a.d, vec, [&](auto V, auto L, auto N, auto any) -> int {
       constexpr int threads = fwd_threads<L.value>(), rows = threads / L.value;
       const unsigned blocks = (unsigned)std::min<int64_t>(256 * 2048 / threads, cdiv(a.rows, rows));
       if (res)
-        KLAUNCH(st, "k_residual_fwd", k_residual_fwd<T, V.value, L.value, N.value, true><<<blocks, threads, 0, st>>>(a));
+        KLAUNCH(st, "k_residual_fwd", k_residual_fwd<T, V.value, L.value, N.value, any.value, true><<<blocks, threads, 0, st>>>(a));
       else
-        KLAUNCH(st, "k_norm_fwd", k_residual_fwd<T, V.value, L.value, N.value, false><<<blocks, threads, 0, st>>>(a));
+        KLAUNCH(st, "k_norm_fwd", k_residual_fwd<T, V.value, L.value, N.value, any.value, false><<<blocks, threads, 0, st>>>(a));
       return CHGNET_OK;
     });
   });
@@ -708,13 +747,13 @@ int launch_bwd(bool res, int32_t dtype, bool vec, ResArgs a, hipStream_t st) {
   int blocks = 1;
   CHG_TRY(with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    return with_layout<T>(a.d, vec, [&](auto V, auto L, auto N) -> int {
+    return with_layout<T>(a.d, vec, [&](auto V, auto L, auto N, auto any) -> int {
       constexpr int threads = bwd_threads<L.value>();
       blocks = bwd_blocks(a.rows, threads / L.value);
       if (res)
-        KLAUNCH(st, "k_residual_bwd", k_residual_bwd<T, V.value, L.value, N.value, true><<<blocks, threads, 0, st>>>(a));
+        KLAUNCH(st, "k_residual_bwd", k_residual_bwd<T, V.value, L.value, N.value, any.value, true><<<blocks, threads, 0, st>>>(a));
       else
-        KLAUNCH(st, "k_norm_bwd", k_residual_bwd<T, V.value, L.value, N.value, false><<<blocks, threads, 0, st>>>(a));
+        KLAUNCH(st, "k_norm_bwd", k_residual_bwd<T, V.value, L.value, N.value, any.value, false><<<blocks, threads, 0, st>>>(a));
       return CHGNET_OK;
     });
   }));
