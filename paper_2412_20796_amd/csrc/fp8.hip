@@ -76,44 +76,6 @@ __device__ __forceinline__ unsigned groupmax_bits(unsigned v) {
   return b[0] > b[1] ? b[0] : b[1];
 }
 
-// Values x[0 .. 7] at column c of a row of n columns; 0 past its end
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int64_t c, int64_t n, float (&v)[8]) {
-  if (VEC && c + 8 <= n) {
-    load_v<8>(p + c, v);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = c + k < n ? (float)p[c + k] : 0.f;
-  }
-}
-
-// Rows under 1 x 128 scales: 16 lanes have a block, 8 values each.
-template <class T, bool VEC>
-__global__ void __launch_bounds__(256) k_fp8_rows(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
-                                                  uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scale,
-                                                  int64_t lds) {
-  const int64_t nb = (cols + kBlock - 1) / kBlock, end = (cols + 15) / 16 * 16;
-  const int j = threadIdx.x & 15;
-  const int64_t stride = (int64_t)gridDim.x * 16;
-  for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < rows * nb; i += stride) {
-    const int64_t row = i / nb, b = i - row * nb, c = b * kBlock + 8 * j;
-    float v[8];
-    load8<T, VEC>(x + row * ldx, c, cols, v);
-    unsigned big = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) big = max(big, magnitude(v[k]));
-    const unsigned byte = scale_byte(rowmax_bits<16>(big));
-    const float inv = scale_inverse(byte);
-    if (c < end) {
-      uint2 q;
-      q.x = codes4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-      q.y = codes4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
-      *reinterpret_cast<uint2*>(codes + row * ldc + c) = q;
-    }
-    if (j == 0) scale[row * lds + b] = (uint8_t)byte;
-  }
-}
-
 // Eight values of a row as they are stored, in words, and the order of their
 // magnitudes without conversions: that of the bits below the sign.
 template <class T>
@@ -121,14 +83,15 @@ struct Eight {
   static constexpr int NW = 2 * sizeof(T);
   typedef unsigned short pair __attribute__((ext_vector_type(2)));
   unsigned w[NW];
+  // (the hardware takes 16 bytes at any address)
   __device__ __forceinline__ void load(const T* p) {
+    typedef unsigned words __attribute__((ext_vector_type(4)));
+    typedef words any __attribute__((aligned(2)));
 #pragma unroll
     for (int q = 0; q < NW / 4; ++q) {
-      const uint4 t = reinterpret_cast<const uint4*>(p)[q];
-      w[4 * q] = t.x;
-      w[4 * q + 1] = t.y;
-      w[4 * q + 2] = t.z;
-      w[4 * q + 3] = t.w;
+      const words t = reinterpret_cast<const any*>(p)[q];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[4 * q + k] = t[k];
     }
   }
   // the first n of them, 0 for the others
@@ -172,6 +135,35 @@ struct Eight {
   }
 };
 
+// Rows under 1 x 128 scales: 16 lanes have a block, 8 values each.
+template <class T>
+__global__ void __launch_bounds__(256) k_fp8_rows(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
+                                                  uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scale,
+                                                  int64_t lds) {
+  const int64_t nb = (cols + kBlock - 1) / kBlock, end = (cols + 15) / 16 * 16;
+  const int j = threadIdx.x & 15;
+  const int64_t stride = (int64_t)gridDim.x * 16;
+  for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < rows * nb; i += stride) {
+    const int64_t row = i / nb, b = i - row * nb, c = b * kBlock + 8 * j;
+    using E = Eight<T>;
+    E v;
+    if (c + 8 <= cols) v.load(x + row * ldx + c);
+    else v.load_some(x + row * ldx + c, cols - c);
+    unsigned big = E::below_sign(v.w[0]);
+#pragma unroll
+    for (int k = 1; k < E::NW; ++k) big = E::larger(big, E::below_sign(v.w[k]));
+    const unsigned byte = scale_byte(rowmax_bits<16>(E::largest(big)));
+    const float inv = scale_inverse(byte);
+    if (c < end) {
+      uint2 q;
+      q.x = codes4(v.get(0) * inv, v.get(1) * inv, v.get(2) * inv, v.get(3) * inv);
+      q.y = codes4(v.get(4) * inv, v.get(5) * inv, v.get(6) * inv, v.get(7) * inv);
+      *reinterpret_cast<uint2*>(codes + row * ldc + c) = q;
+    }
+    if (j == 0) scale[row * lds + b] = (uint8_t)byte;
+  }
+}
+
 // Tiles of 128 x 128, `count` (1 or 4) below each other a block: codes of them and
 // of their transpose (either may be left out). SQUARE: one scale for a tile, which
 // both share; else 1 x 128 of the rows of each. A thread has 8 x 8 values; the
@@ -180,7 +172,7 @@ struct Eight {
 // banks' pairs. Four tiles a block, so that the transpose's scales are written in
 // words: single bytes far from each other were a third of all writes, and took
 // twice the time (397,934 x 512 in bf16, both forms: 278 us).
-template <class T, bool VEC, bool SQUARE>
+template <class T, bool SQUARE>
 __global__ void __launch_bounds__(256, 4) k_fp8_tile(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
                                                      uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scale,
                                                      int64_t lds, uint8_t* __restrict__ codes_t, int64_t ldct,
@@ -202,7 +194,7 @@ __global__ void __launch_bounds__(256, 4) k_fp8_tile(int64_t rows, int64_t cols,
     {
       const T* p = x + r0 * ldx + c0;
       const int there = (int)(rows - r0 < 8 ? rows - r0 : 8);  // rows of this thread's (may be none)
-      if (VEC && c0 + 8 <= cols && there == 8) {
+      if (c0 + 8 <= cols && there == 8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i].load(p + i * ldx);
       } else {
@@ -302,10 +294,10 @@ __global__ void __launch_bounds__(256, 4) k_fp8_tile(int64_t rows, int64_t cols,
     // (the words are this thread's block's: written before its last barrier)
     uint8_t* p = scale_t + (tc * 128 + threadIdx.x) * ldst + tr0;
     const unsigned w = words[threadIdx.x];
-    if (count == 4) {
-      *reinterpret_cast<unsigned*>(p) = w;  // (a row of scales has whole words)
+    if (count == 4 && tr0 + 4 <= tiles_r) {
+      *reinterpret_cast<unsigned*>(p) = w;
     } else {
-      *p = (uint8_t)w;
+      for (int t = 0; t < count && tr0 + t < tiles_r; ++t) p[t] = (uint8_t)(w >> (8 * t));
     }
   }
 }
@@ -628,7 +620,7 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
 // (x), quantised by each wavefront as it needs them, which costs less than a launch:
 // lane group g of a block of K has the values 32 g .. 32 g + 31 of row lane % 16, and
 // the largest of the four groups is the block's.
-template <class T, bool EXACT, bool QUANT, bool VEC, int NT>
+template <class T, bool EXACT, bool QUANT, int NT>
 __global__ void __launch_bounds__(512) k_fp8_few(ProductArgs p, const T* __restrict__ x, int64_t ldx) {
   constexpr int WAVES = 8;
   __shared__ v4f parts[WAVES][NT][64];
@@ -668,7 +660,7 @@ __global__ void __launch_bounds__(512) k_fp8_few(ProductArgs p, const T* __restr
       if constexpr (!QUANT) in.a[h] = there ? *reinterpret_cast<const uint4*>(a + c + 16 * h) : zero;
     }
     if constexpr (QUANT) {
-      if (VEC && c + 32 <= K) {
+      if (c + 32 <= K) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) in.x[q].load(xr + c + 8 * q);
       } else {
@@ -752,7 +744,7 @@ __global__ void __launch_bounds__(512) k_fp8_few(ProductArgs p, const T* __restr
 // a row's 128 values of a step; those of the next step arrive while this one's are
 // multiplied. Places in LDS and operands are k_fp8_product's. x's codes have one
 // buffer, which all read before they multiply: two blocks have room on a compute unit.
-template <class T, bool EXACT, bool VEC, int BN>
+template <class T, bool EXACT, int BN>
 __global__ void __launch_bounds__(2 * BN, 4) k_fp8_rows_product(ProductArgs p, const T* __restrict__ x, int64_t ldx) {
   constexpr int BM = 64, WN = BN / 64, THREADS = 2 * BN, TM = 2, TN = 4, W = 16 / sizeof(T);
   constexpr int PIECES = BN * 8 / THREADS, XP = BM * 16 / THREADS, LOADS = XP * sizeof(T) / 2;
@@ -762,7 +754,7 @@ __global__ void __launch_bounds__(2 * BN, 4) k_fp8_rows_product(ProductArgs p, c
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN * 32, wn = wave % WN * 64, r16 = lane & 15, g = lane >> 4, key = r16 >> 1;
   const int nkb = (int)((K + kBlock - 1) / kBlock);
-  const bool inside = VEC && m0 + BM <= M;
+  const bool inside = m0 + BM <= M;
 
   // b's codes, as in k_fp8_product
   unsigned src[PIECES];
@@ -945,7 +937,7 @@ Factor factor(const chgnet_fp8* f) {
   return {f->codes, f->scale, f->ld, f->ld_scale, f->rows, f->block_rows == kBlock ? 7 : 0};
 }
 
-constexpr int64_t kFewRows = 16;
+constexpr int64_t kFewRows = 16, kUnits = 256;  // (compute units)
 
 struct Plan {
   int tile;  // of tile x tile results; 0: few rows
@@ -958,7 +950,7 @@ struct Plan {
 // 16; 512 x 4,096 x 4,096 19 us in 512 tiles of 64, 26 in 128 of 128, 24 in twice
 // as many halves; 128 x 8,192 x 8,192 25 us in 256 tiles of 64 and two parts, 29 in one,
 // 33 in 64 of 128 and two.
-constexpr int64_t kLeastSteps = 24, kUnits = 256;
+constexpr int64_t kLeastSteps = 24;
 Plan plan(int64_t M, int64_t N, int64_t K) {
   const int64_t nkb = std::max<int64_t>(1, cdiv(K, kBlock)), most = std::max<int64_t>(1, nkb / kLeastSteps);
   if (M <= kFewRows) return {0, 0, 1, (int)nkb};
@@ -972,11 +964,11 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
 // Columns of a block: twice as many where that leaves a block for each compute unit
 // (16 rows of 8,192 to 8,192 in bf16: 31 us in blocks of 16 columns, 24 of 32, 32 of
 // 64; one row of 4,096 to 4,096: 8.3, 8.4, 12)
-template <class T, bool QUANT, bool VEC>
+template <class T, bool QUANT>
 int launch_few(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
   constexpr bool exact = std::is_same<T, float>::value;
   auto launch = [&](auto nt) -> int {
-    KLAUNCH(st, "k_fp8_few", k_fp8_few<T, exact, QUANT, VEC, nt.value>
+    KLAUNCH(st, "k_fp8_few", k_fp8_few<T, exact, QUANT, nt.value>
                              <<<(unsigned)cdiv(p.b.rows, 16 * nt.value), 512, 0, st>>>(p, x, ldx));
     return CHGNET_OK;
   };
@@ -989,14 +981,14 @@ int launch_few(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
 // rows of 512 to 256 187 and 227, to 128 114 and 211, 85,274 of 256 to 128 18 and 32; fp32 rows
 // 326 and 392, 196 and 354, 27 and 48; 5,000 of 512 to 256 9 and 11, in fp32 14 and 12)
 bool on_the_way(int64_t M, int64_t N) { return N <= 256 && cdiv(M, 64) >= kUnits; }
-template <class T, bool VEC>
+template <class T>
 int launch_rows_product(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
   constexpr bool exact = std::is_same<T, float>::value;
   const unsigned blocks = (unsigned)cdiv(p.a.rows, 64);
   if (p.b.rows <= 128)
-    KLAUNCH(st, "k_fp8_rows_product", k_fp8_rows_product<T, exact, VEC, 128><<<blocks, 256, 0, st>>>(p, x, ldx));
+    KLAUNCH(st, "k_fp8_rows_product", k_fp8_rows_product<T, exact, 128><<<blocks, 256, 0, st>>>(p, x, ldx));
   else
-    KLAUNCH(st, "k_fp8_rows_product", k_fp8_rows_product<T, exact, VEC, 256><<<blocks, 512, 0, st>>>(p, x, ldx));
+    KLAUNCH(st, "k_fp8_rows_product", k_fp8_rows_product<T, exact, 256><<<blocks, 512, 0, st>>>(p, x, ldx));
   return CHGNET_OK;
 }
 
@@ -1024,33 +1016,28 @@ int fp8_quantize_entry(int64_t rows, int64_t cols, int32_t dtype, const void* x,
   const size_t es = elem_size(dtype);
   if (!x) return bad(who, "null argument");
   if (!aligned_to(x, es)) return bad(who, "x is not aligned to its values");
-  const bool vec = ldx * es % 16 == 0 && aligned_to(x, 16);
   const bool square = (q ? q : t)->block_rows == kBlock;
   return with_type(dtype, [&](auto v) -> int {
     using T = decltype(v);
     const T* p = static_cast<const T*>(x);
     if (!square && !t) {
       const unsigned blocks = (unsigned)std::min<int64_t>(4096, cdiv(rows * cdiv(cols, kBlock), 16));
-#define CHG_ROWS(V) \
-  KLAUNCH(st, "k_fp8_rows", k_fp8_rows<T, V><<<blocks, 256, 0, st>>>(rows, cols, p, ldx, q->codes, q->ld, q->scale, q->ld_scale))
-      if (vec) CHG_ROWS(true);
-      else CHG_ROWS(false);
-#undef CHG_ROWS
+KLAUNCH(st, "k_fp8_rows",
+              k_fp8_rows<T><<<blocks, 256, 0, st>>>(rows, cols, p, ldx, q->codes, q->ld, q->scale, q->ld_scale));
       return CHGNET_OK;
     }
-    // four tiles a block where that leaves a block for each compute unit
-    const int count = cdiv(rows, 512) * cdiv(cols, 128) >= 256 ? 4 : 1;
+    // four tiles a block where that leaves four blocks for each compute unit (4,096 x
+    // 4,096 in bf16, both forms: 19 us in blocks of one tile, 22 of four)
+    const int count = cdiv(rows, 512) * cdiv(cols, 128) >= 4 * kUnits ? 4 : 1;
     const int64_t tiles = cdiv(rows, 128 * count) * cdiv(cols, 128);
     if (tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles of 128 x 128");
     const chgnet_fp8 none{}, &a = q ? *q : none, &b = t ? *t : none;
-#define CHG_TILE(V, S)                                                                                                     \
-  KLAUNCH(st, "k_fp8_tile", k_fp8_tile<T, V, S><<<(unsigned)tiles, 256, 0, st>>>(                                          \
+#define CHG_TILE(S)                                                                                                     \
+  KLAUNCH(st, "k_fp8_tile", k_fp8_tile<T, S><<<(unsigned)tiles, 256, 0, st>>>(                                          \
                                 rows, cols, p, ldx, a.codes, a.ld, a.scale, a.ld_scale, b.codes, b.ld, b.scale, b.ld_scale, \
                                 count))
-    if (vec && square) CHG_TILE(true, true);
-    else if (vec) CHG_TILE(true, false);
-    else if (square) CHG_TILE(false, true);
-    else CHG_TILE(false, false);
+    if (square) CHG_TILE(true);
+    else CHG_TILE(false);
 #undef CHG_TILE
     return CHGNET_OK;
   });
@@ -1091,7 +1078,7 @@ int fp8_matmul_entry(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, vo
     using T = decltype(v);
     constexpr bool exact = std::is_same<T, float>::value;
     if (pl.tile == 0) {
-      return launch_few<T, false, true>(p, nullptr, 0, st);
+      return launch_few<T, false>(p, nullptr, 0, st);
     }
     auto launch = [&](auto part) -> int {
       using P = decltype(part);
@@ -1152,14 +1139,10 @@ int fp8_linear_entry(int64_t rows, int32_t dtype, const void* x, int64_t ldx, co
   if (rows <= kFewRows || on_the_way(rows, w->rows)) {
     ProductArgs p{};
     p.a.rows = rows, p.b = factor(w), p.K = w->cols, p.out = out, p.ldo = ldout;
-    const bool vec = ldx * es % 16 == 0 && aligned_to(x, 16);
     return with_type(dtype, [&](auto v) -> int {
       using T = decltype(v);
-      if (rows > kFewRows)
-        return vec ? launch_rows_product<T, true>(p, static_cast<const T*>(x), ldx, st)
-                   : launch_rows_product<T, false>(p, static_cast<const T*>(x), ldx, st);
-      return vec ? launch_few<T, true, true>(p, static_cast<const T*>(x), ldx, st)
-                 : launch_few<T, true, false>(p, static_cast<const T*>(x), ldx, st);
+      const T* t = static_cast<const T*>(x);
+      return rows > kFewRows ? launch_rows_product<T>(p, t, ldx, st) : launch_few<T, true>(p, t, ldx, st);
     });
   }
   size_t product = 0;

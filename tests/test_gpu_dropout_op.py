@@ -109,6 +109,21 @@ def test_a_replayed_graph_draws_anew():
         assert float(x.sum()) == float(xc.cpu().sum())
 
 
+def test_sizes_past_32_bits():
+    rows, d = 70000, 32776
+    x = torch.ones(rows, d, dtype=torch.bfloat16, device="cuda")
+    out = ops.dropout(x, 0.5, 7, 1)
+    for r in (0, 40000, 65535, rows - 1):
+        n = ref.kept(1, d, 0.5, 7, 1)[0] if r == 0 else None
+        got = out[r].cpu()
+        if n is not None:
+            assert torch.equal(got != 0, n[0])
+        g = ref.philox(range((d + 7) // 8), [r] * ((d + 7) // 8), [1] * ((d + 7) // 8), [0] * ((d + 7) // 8), 7, 0)
+        low, high = [(w.astype('int64') & 0xFFFF) >= 32768 for w in g], [(w.astype('int64') >> 16) >= 32768 for w in g]
+        want = torch.tensor([v for k in range(len(low[0])) for i in range(4) for v in (low[i][k], high[i][k])])[:d]
+        assert torch.equal(got != 0, want), r
+
+
 def test_refusals():
     x = torch.zeros(4, 8, device="cuda")
     for call in (lambda: ops.dropout(x, 1.5, 0), lambda: ops.dropout(x, float("nan"), 0), lambda: ops.dropout(x, 0.1, -1),

@@ -358,6 +358,45 @@ def test_replayed_graph():
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
 
 
+def test_scales_behind_the_last_block_stay():
+    """A matrix of the caller's, whose rows of scales are in a wider buffer: four row blocks a word, and the rest."""
+    rows, cols = 512 * 40 + 300, 128 * 40
+    x = _x(300, 128).repeat(rows // 300 + 1, 40)[:rows].to(torch.bfloat16)
+    codes = torch.zeros(cols, -(-rows // 16) * 16, device="cuda").to(torch.float8_e4m3fn)
+    buf = torch.full((cols, 172), 9, dtype=torch.uint8, device="cuda")
+    nb = -(-rows // 128)
+    t = ops.Fp8Matrix(codes[:, :rows], buf.view(torch.float8_e8m0fnu)[:, 4:4 + nb])
+    ops.fp8_quantize(x.cuda(), transposed=True, out=t)
+    assert nb % 4 and bool((buf[:, :4] == 9).all()) and bool((buf[:, 4 + nb:] == 9).all())
+    some = torch.arange(0, cols, 777)
+    q, byte = ref.quantize(x.T[some])
+    assert torch.equal(buf[:, 4:4 + nb].cpu()[some].long(), byte)
+    assert torch.equal(codes[:, :rows].cpu()[some].float().double(), q)
+
+
+def test_sizes_past_32_bits():
+    """Codes, values and results at offsets of more than 2^32 bytes and 2^31 values."""
+    M, K = 1 << 19, 8320
+    x = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    part = _x(512, K, torch.bfloat16).cuda()
+    for i in range(0, M, 512):
+        x[i:i + 512] = part
+    q, t = ops.fp8_quantize_both(x)
+    w = _x(40, K, seed=3)
+    m = ops.fp8_quantize(w.cuda())
+    last = slice(M - 200, M)
+    held = ref.values(*ref.quantize(part.cpu()[-200:]))
+    for out in (ops.fp8_matmul(q, m), ops.fp8_linear(x, m)):
+        r, b = ref.product(held, ref.values(*ref.quantize(w)), torch.bfloat16)
+        assert_within(out[last], r, b, torch.bfloat16)
+    tq, tb = ref.quantize(part.cpu()[-128:, -30:].T)
+    assert torch.equal(t.codes[-30:, -128:].cpu().float().double(), tq)
+    assert torch.equal(t.scale[-30:, -1:].cpu().view(torch.uint8).long(), tb)
+    few = ops.fp8_matmul(m, q, torch.float32)
+    r, b = ref.product(ref.values(*ref.quantize(w)), held)
+    assert_within(few[:, last], r, b)
+
+
 def test_two_at_once():
     w = ops.fp8_quantize(_x(256, 4096).cuda(), 128)
     xs = [_x(n, 4096, torch.bfloat16, n).cuda() for n in (2, 40, 300)]

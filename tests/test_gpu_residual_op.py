@@ -340,6 +340,23 @@ def test_a_function_of_the_callers():
     assert all(torch.equal(t.grad, g) for t, g in zip(leaves, want))
 
 
+def test_sizes_past_32_bits():
+    rows, d = 270000, 8200
+    x, f, dy, dh, gate, post, pre = _inputs(512, d, torch.bfloat16, cols=1, post=1, pre=1)
+    big = lambda t: t.cuda().repeat(rows // 512 + 1, 1)[:rows]
+    how = dict(post=post.cuda(), pre=pre.cuda())
+    xb, fb, gb = big(x), big(f), big(gate)
+    y, h = ops.residual_forward(xb, fb, gate=gb, **how)
+    some = slice(rows - 100, rows)
+    small = ops.residual_forward(xb[some].contiguous(), fb[some].contiguous(), gate=gb[some].contiguous(), **how)
+    assert torch.equal(y[some], small[0]) and torch.equal(h[some], small[1])
+    dyb, dhb = big(dy), big(dh)
+    got = ops.residual_backward(y, fb, dyb, dhb, gate=gb, **how)
+    part = ops.residual_backward(small[0], fb[some].contiguous(), dyb[some].contiguous(), dhb[some].contiguous(),
+                                 gate=gb[some].contiguous(), **how)
+    assert all(torch.equal(getattr(got, n)[some], getattr(part, n)) for n in ("dx", "df", "dgate"))
+
+
 def test_refusals():
     x, f, dy, dh, gate, post, pre = (_cuda(t) for t in _inputs(8, 64, torch.float32, cols=64, post=2, pre=2))
     z = lambda *s, **k: torch.zeros(*s, device="cuda", **k)
