@@ -895,6 +895,156 @@ __global__ void __launch_bounds__(2 * BN, 4) k_fp8_rows_product(ProductArgs p, c
   }
 }
 
+// The same where all of b's codes have room in LDS beside x's: 256 columns of up to
+// 512 values. A block, one a compute unit, keeps them and walks the rows, 64 at a
+// time; the values of a step are loaded for the block's next rows as soon as they are
+// coded, a whole tile ahead, and a step waits for no load of codes. (397,934 rows of
+// 512 to 256 180 -> 152 us in bf16, 4.0 TB/s, 308 -> 245 in fp32, 5.0.)
+template <class T, bool EXACT>
+__global__ void __launch_bounds__(512, 2) k_fp8_rows_resident(ProductArgs p, const T* __restrict__ x, int64_t ldx) {
+  constexpr int BM = 64, BN = 256, WN = 4, THREADS = 512, TM = 2, TN = 4, W = 16 / sizeof(T), KB = 4, XP = 2;
+  using E = Eight<T>;
+  __shared__ __align__(1024) uint8_t lb[KB][BN * kBlock], la[2][BM * kBlock];
+  __shared__ uint8_t scales[2][BM];
+  const int64_t M = p.a.rows, N = p.b.rows, K = p.K, tiles = (M + BM - 1) / BM;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN * 32, wn = wave % WN * 64, r16 = lane & 15, g = lane >> 4, key = r16 >> 1;
+  const int nkb = (int)((K + kBlock - 1) / kBlock);
+  auto column = [](int row, int j) { return (row >> 2) * W + (row & 3) + j / (W / 4) * 4 * W + j % (W / 4) * 4; };
+  {  // b's codes, as in k_fp8_product
+    const unsigned key_b = W == 4 ? threadIdx.x >> 4 & 7 : (threadIdx.x >> 4 & 1) | (threadIdx.x >> 6 & 3) << 1;
+    const unsigned piece = 16 * ((threadIdx.x & 7) ^ key_b);
+    for (int kb = 0; kb < nkb; ++kb) {
+      const int64_t at = (int64_t)kb * kBlock;
+      uint8_t* to = lb[kb] + wave * 1024;
+#pragma unroll
+      for (int i = 0; i < BN * 8 / THREADS; ++i) {
+        const int row = (i * THREADS + threadIdx.x) / 8, last = (int)N - 1;
+        if (at + piece < K) to_lds16(p.b.codes + (int64_t)(row < last ? row : last) * p.b.ldc + at + piece, to + i * THREADS * 16);
+        else *reinterpret_cast<uint4*>(to + i * THREADS * 16 + lane * 16) = make_uint4(0, 0, 0, 0);
+      }
+    }
+  }
+  // b's scales: a word has the bytes of the four blocks of K
+  unsigned eb[TN];
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int n = wn + column(r16, j);
+    eb[j] = *reinterpret_cast<const unsigned*>(p.b.scale + ((n < N ? n : N - 1) >> p.b.shift) * p.b.lds);
+  }
+  // rows of x: row xr + 32 i of a tile, values 8 xc .. of a block of K
+  const int xr = threadIdx.x >> 4, xc = threadIdx.x & 15;
+  E v[KB][XP];
+  auto load_x = [&](int64_t tile, int kb, E (&v)[XP]) {
+    const int64_t c = (int64_t)kb * kBlock + 8 * xc;
+#pragma unroll
+    for (int i = 0; i < XP; ++i) {
+      const int64_t m = tile * BM + xr + i * (THREADS / 16);
+      const T* q = x + m * ldx + c;
+      if (m < M && c + 8 <= K) v[i].load(q);
+      else v[i].load_some(q, m < M ? K - c : 0);
+    }
+  };
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+    if (kb < nkb) load_x(blockIdx.x, kb, v[kb]);
+  wait_barrier<0>();  // b's codes are there
+  const bool vec = (p.ldo * sizeof(T) & 15) == 0 && ((uintptr_t)p.out & 15) == 0;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    v4f acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    int step = 0;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      if (kb >= nkb) break;
+      // (the buffers take turns over the tiles' ends)
+      const int buf = (int)((tile / gridDim.x * nkb + step++) & 1);
+#pragma unroll
+      for (int i = 0; i < XP; ++i) {
+        const int row = xr + i * (THREADS / 16);
+        const E& r = v[kb][i];
+        unsigned big = E::below_sign(r.w[0]);
+#pragma unroll
+        for (int q = 1; q < E::NW; ++q) big = E::larger(big, E::below_sign(r.w[q]));
+        const unsigned byte = scale_byte(rowmax_bits<16>(E::largest(big)));
+        const float inv = scale_inverse(byte);
+        uint2 q;
+        q.x = codes4(r.get(0) * inv, r.get(1) * inv, r.get(2) * inv, r.get(3) * inv);
+        q.y = codes4(r.get(4) * inv, r.get(5) * inv, r.get(6) * inv, r.get(7) * inv);
+        *reinterpret_cast<uint2*>(la[buf] + row * kBlock + ((xc >> 1) ^ (row >> 1 & 7)) * 16 + (xc & 1) * 8) = q;
+        if (xc == 0) scales[buf][row] = (uint8_t)byte;
+      }
+      if (tile + gridDim.x < tiles) load_x(tile + gridDim.x, kb, v[kb]);
+      // x's codes are written (and those of the last step but one read by all)
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      unsigned ea[TM];
+      v4i ra[TM][2];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        ea[i] = scales[buf][wm + 16 * i + r16];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          ra[i][h] = *reinterpret_cast<const v4i*>(la[buf] + (wm + 16 * i + r16) * kBlock + ((g + 4 * h) ^ key) * 16);
+      }
+      auto half_b = [&](int j, int h) {
+        return *reinterpret_cast<const v4i*>(lb[kb] + (wn + column(r16, j)) * kBlock + ((g + 4 * h) ^ key) * 16);
+      };
+      if constexpr (EXACT) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          v8b aw[TM][2];
+#pragma unroll
+          for (int i = 0; i < TM; ++i) {
+            aw[i][0] = wide(make_uint2(ra[i][h][0], ra[i][h][1]), scale_value(ea[i]));
+            aw[i][1] = wide(make_uint2(ra[i][h][2], ra[i][h][3]), scale_value(ea[i]));
+          }
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const v4i q = half_b(j, h);
+            const float f = scale_value(eb[j] >> (8 * kb));
+            const v8b b0 = wide(make_uint2(q[0], q[1]), f), b1 = wide(make_uint2(q[2], q[3]), f);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b0, aw[i][0], acc[i][j], 0, 0, 0);
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b1, aw[i][1], acc[i][j], 0, 0, 0);
+            }
+          }
+        }
+      } else {
+        v8i a[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          const v4i q = ra[i][0], r = ra[i][1];
+          a[i] = v8i{q[0], q[1], q[2], q[3], r[0], r[1], r[2], r[3]};
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const v4i q = half_b(j, 0), r = half_b(j, 1);
+          const v8i b = {q[0], q[1], q[2], q[3], r[0], r[1], r[2], r[3]};
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a[i], acc[i][j], 0, 0, 0, eb[j] >> (8 * kb), 0, ea[i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int64_t m = tile * BM + wm + 16 * i + r16;
+#pragma unroll
+      for (int q = 0; q < 16 / W; ++q) {
+        const int64_t n = wn + q * 4 * W + g * W;
+        float t[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) t[k] = acc[i][(q * W + k) / 4][k % 4];
+        if (m < M) put(static_cast<T*>(p.out) + m * p.ldo + n, t, N - n, vec, false);
+      }
+    }
+  }
+}
+
 // out (+)= the sum of the splits' parts, in order; a thread has four columns
 template <class T>
 __global__ void __launch_bounds__(256) k_fp8_join(int64_t M, int64_t N, int splits, const float* __restrict__ part,
@@ -978,14 +1128,17 @@ int launch_few(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
 
 // Whether a linear layer quantises its rows on the way: where each is needed once
 // and the blocks fill the GPU (us of a call against quantiser and product, bf16: 397,934
-// rows of 512 to 256 187 and 227, to 128 114 and 211, 85,274 of 256 to 128 18 and 32; fp32 rows
-// 326 and 392, 196 and 354, 27 and 48; 5,000 of 512 to 256 9 and 11, in fp32 14 and 12)
+// rows of 512 to 256 152 and 227, to 128 115 and 211, 85,274 of 256 to 128 18 and 32; fp32 rows
+// 245 and 392, 189 and 354, 27 and 48; 5,000 of 512 to 256 9 and 11, in fp32 14 and 12)
 bool on_the_way(int64_t M, int64_t N) { return N <= 256 && cdiv(M, 64) >= kUnits; }
 template <class T>
 int launch_rows_product(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
   constexpr bool exact = std::is_same<T, float>::value;
   const unsigned blocks = (unsigned)cdiv(p.a.rows, 64);
-  if (p.b.rows <= 128)
+  if (p.b.rows > 128 && p.K <= 4 * kBlock)
+    KLAUNCH(st, "k_fp8_rows_resident",
+            k_fp8_rows_resident<T, exact><<<(unsigned)std::min<int64_t>(blocks, kUnits), 512, 0, st>>>(p, x, ldx));
+  else if (p.b.rows <= 128)
     KLAUNCH(st, "k_fp8_rows_product", k_fp8_rows_product<T, exact, 128><<<blocks, 256, 0, st>>>(p, x, ldx));
   else
     KLAUNCH(st, "k_fp8_rows_product", k_fp8_rows_product<T, exact, 256><<<blocks, 512, 0, st>>>(p, x, ldx));

@@ -241,7 +241,8 @@ def test_linear(rows, N, K, br, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,K,N,br", [(16400, 128, 256, 128), (16385, 100, 1, 1), (16500, 520, 128, 128), (17001, 300, 130, 1),
-                                         (16384, 384, 200, 1)])
+                                         (16384, 384, 200, 1), (16390, 640, 250, 128), (40001, 512, 256, 128),
+                                         (20000, 16, 129, 1)])
 def test_linear_of_many_rows(rows, K, N, br, dtype):
     x, w = _x(rows, K, dtype), _x(N, K, torch.float32, 5) / 8
     x[2] = 0
