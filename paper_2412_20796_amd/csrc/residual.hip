@@ -362,7 +362,14 @@ template <int TPR>
 constexpr int bwd_threads() {
   return TPR > 512 ? TPR : 512;
 }
+// Blocks of a backward launch, which each end in one partial row of the parameters'
+// gradients: as many as run at a time, two a compute unit where registers and
+// threads allow it
 constexpr int kBwdBlocks = 512;
+template <class T, int TPR, int NQ, bool RES>
+constexpr int bwd_blocks_at_most() {
+  return TPR == 1024 || (RES && (sizeof(T) == 2 || NQ > 1)) ? kBwdBlocks / 2 : kBwdBlocks;
+}
 
 // Adds the block's sums of one parameter row into `o` (its row of the partial
 // sums, or with one block the destination itself): rows of one wavefront by lane
@@ -723,9 +730,9 @@ int check_arrays(const char* who, std::initializer_list<Array> arrays, int d, si
 
 // Blocks of a backward launch: rows of a block walked in turn; more than two
 // turns are worth a second launch that adds the blocks' sums.
-int bwd_blocks(int64_t rows, int rows_a_block) {
+int bwd_blocks(int64_t rows, int rows_a_block, int at_most) {
   const int64_t turns = cdiv(rows, rows_a_block);
-  return turns <= 2 ? 1 : (int)std::min<int64_t>(kBwdBlocks, turns);
+  return turns <= 2 ? 1 : (int)std::min<int64_t>(at_most, turns);
 }
 
 int launch_fwd(bool res, int32_t dtype, bool vec, const ResArgs& a, hipStream_t st) {
@@ -749,7 +756,8 @@ int launch_bwd(bool res, int32_t dtype, bool vec, ResArgs a, hipStream_t st) {
     using T = decltype(t);
     return with_layout<T>(a.d, vec, [&](auto V, auto L, auto N, auto any) -> int {
       constexpr int threads = bwd_threads<L.value>();
-      blocks = bwd_blocks(a.rows, threads / L.value);
+      blocks = bwd_blocks(a.rows, threads / L.value,
+                          res ? bwd_blocks_at_most<T, L.value, N.value, true>() : bwd_blocks_at_most<T, L.value, N.value, false>());
       if (res)
         KLAUNCH(st, "k_residual_bwd", k_residual_bwd<T, V.value, L.value, N.value, any.value, true><<<blocks, threads, 0, st>>>(a));
       else
