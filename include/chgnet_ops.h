@@ -1,13 +1,16 @@
 /*
  * chgnet_ops.h - operators of the training step for models of the caller's own.
  *
- * Two pieces of the step in chgnet.h as calls on plain arrays: the gate of the
+ * Pieces of the step in chgnet.h, and what a deep network out of them needs around
+ * them, as calls on plain arrays. The first two: the gate of the
  * gated MLP (GatedMLP of Eq. 4-6: LayerNorm, SiLU and sigmoid, product) with an
  * 8-bit checkpoint of its input for the backward pass, and the embedding lookup
  * (Eq. 2) with a scale, and its gradient. chgnet_step, chgnet_forward and
  * chgnet_backward keep their pre-activations in the same checkpoint with
  * chgnet_hparams.act_bits = 8, and sum the element table's gradient with
- * chgnet_embed_backward's kernels on large batches.
+ * chgnet_embed_backward's kernels on large batches. Then: norms, the residual
+ * connection around a block with its gate and dropout, dropout alone, and matrices
+ * in 8-bit floating point with their products, for linear layers.
  *
  * The conventions of chgnet.h hold: device pointers owned by the caller, no
  * allocation, work enqueued on `stream` of the current device, error codes,

