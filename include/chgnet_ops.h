@@ -192,7 +192,7 @@ int chgnet_fp8_quantize(int64_t rows, int64_t cols, int32_t dtype, const void* x
  * what it holds with accumulate != 0. A linear layer's y = x w^T, dx = dy w and dw =
  * dy^T x are this with the forms of chgnet_fp8_quantize: (x, w), (dy, w^T), (dy^T,
  * x^T). For 16-bit results the products of a block are added eight at a time, cut
- * off at 2^-13 of the largest one's power of two (of normal values some 1e-4 of a
+ * off at 2^-13 of the largest one's power of two (of normal values some 2e-5 of a
  * result); for fp32 results they are exact, for values that are fp32 numbers (past
  * its largest they count as infinite, below 2^-126 they may count as 0). ws: at least
  * chgnet_fp8_matmul_workspace(M, N, K) bytes, 16-byte aligned (none where that is 0). */
