@@ -114,6 +114,16 @@ def test_values_that_are_not_finite(value):
         assert bool(torch.isnan(out[2]).all()) and not bool(torch.isnan(out[torch.arange(out.shape[0]) != 2]).any())
 
 
+@pytest.mark.parametrize("N,K", [(100, 200), (200, 200), (200, 700)])
+def test_values_that_are_not_finite_in_many_rows(N, K):
+    x, w = _x(16400, K), ops.fp8_quantize(_x(N, K, seed=1).cuda(), 128)
+    x[33, K - 1], x[16399, 0] = float("nan"), float("-inf")
+    out = ops.fp8_linear(x.cuda(), w).cpu()
+    rows = torch.zeros(16400, dtype=torch.bool)
+    rows[[33, 16399]] = True
+    assert bool(torch.isnan(out[rows]).all()) and bool(torch.isfinite(out[~rows]).all())
+
+
 def _check_product(a, va, b, vb, dtype=torch.float32, what="", **kw):
     out = ops.fp8_matmul(a, b, dtype, **kw)
     r, bound = ref.product(va, vb, dtype)
@@ -160,6 +170,20 @@ def test_long_sums(M, N, K):
     base = torch.randn(M, N, generator=torch.Generator().manual_seed(1)).cuda()
     got = ops.fp8_matmul(a, b, out=base.clone(), accumulate=True)
     assert torch.equal(got, base + first)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(5, 40, 256), (100, 201, 300), (300, 515, 9000), (2000, 2050, 200)])
+def test_accumulate(M, N, K, dtype):
+    a, va = _random(M, K, 1, 5, spread=1)
+    b, vb = _random(N, K, 128, 6, spread=1)
+    a._scale.view(torch.uint8).sub_(8)
+    va = va / 256
+    base = torch.randn(M, N, generator=torch.Generator().manual_seed(1)).to(dtype)
+    got = ops.fp8_matmul(a, b, out=base.cuda(), accumulate=True)
+    r, bound = ref.product(va, vb, dtype)
+    # one more rounding of the sum in fp32, and the one to the type
+    assert_within(got, r + base.double(), bound + ref.U * (r.abs() + base.double().abs()), dtype)
 
 
 @pytest.mark.parametrize("M,N,K", [(0, 5, 64), (5, 0, 64), (5, 7, 0)])
