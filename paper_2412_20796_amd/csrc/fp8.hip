@@ -933,12 +933,15 @@ __global__ void __launch_bounds__(512, 2) k_fp8_rows_resident(ProductArgs p, con
       }
     }
   }
-  // b's scales: a word has the bytes of the four blocks of K
-  unsigned eb[TN];
+  // b's scales: a word has the bytes of the four blocks of K (there are none, and may be
+  // no memory, where K = 0)
+  unsigned eb[TN] = {};
+  if (nkb) {
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int n = wn + column(r16, j);
-    eb[j] = *reinterpret_cast<const unsigned*>(p.b.scale + ((n < N ? n : N - 1) >> p.b.shift) * p.b.lds);
+    for (int j = 0; j < TN; ++j) {
+      const int n = wn + column(r16, j);
+      eb[j] = *reinterpret_cast<const unsigned*>(p.b.scale + ((n < N ? n : N - 1) >> p.b.shift) * p.b.lds);
+    }
   }
   // rows of x: row xr + 32 i of a tile, values 8 xc .. of a block of K
   const int xr = threadIdx.x >> 4, xc = threadIdx.x & 15;
