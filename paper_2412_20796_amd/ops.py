@@ -402,8 +402,21 @@ def norm_backward(x, w, dh, kind="rms", eps=1e-5, dx=None, dw=None, accumulate=F
     return dx, dw
 
 
+def _number(name, v):
+    """A factor's value as it is now (of a tensor, too, which may hold another one at the next call)."""
+    if type(v) is float:
+        return v
+    if isinstance(v, torch.Tensor) and v.requires_grad and torch.is_grad_enabled():
+        _followed(name)
+    try:
+        return float(v)
+    except (TypeError, ValueError, RuntimeError):
+        _bad("%s must be a number, not %r" % (name, v))
+
+
 @lru_cache(maxsize=64)
 def _residual_cfg(*fields):
+    """Of Python's own numbers only: an object of another type may be its own key and change its value."""
     return _Residual(*fields)
 
 
@@ -428,7 +441,8 @@ def _residual(f, post, post_kind, gate, pre, pre_kind, alpha, beta, p, seed, cal
     at = _draw(seed, call, step, gpu)
     # (by values, never for a step: a cached struct holds no address)
     make = _residual_cfg if at is None else _Residual
-    cfg = make(post_n, post_rows, pre_n, pre_rows, cols, alpha, beta, eps, p, seed, call, at)
+    cfg = make(post_n, post_rows, pre_n, pre_rows, cols, _number("alpha", alpha), _number("beta", beta), _number("eps", eps),
+               _number("p", p), seed, call, at)
     return cfg, (f.data_ptr(), ldf, gate.data_ptr() if cols else None, ldg, post.data_ptr() if post_rows else None,
                  pre.data_ptr() if pre_rows else None), post_rows + pre_rows, cols
 
