@@ -17,6 +17,7 @@ are written so that they add little to that (a dozen attribute reads).
 from __future__ import annotations
 
 import ctypes
+import math
 from collections import namedtuple
 from functools import lru_cache
 
@@ -360,14 +361,36 @@ def _draw(seed, call, step, gpu):
     return step.data_ptr()
 
 
+def _number(name, v):
+    """A factor's value as it is now (of a tensor, too, which may hold another one at the next call)."""
+    if type(v) is float:
+        return v
+    if isinstance(v, torch.Tensor) and v.requires_grad and torch.is_grad_enabled():
+        _followed(name)
+    try:
+        if not isinstance(v, (str, bytes)):
+            return float(v)
+    except (TypeError, ValueError, RuntimeError):
+        pass
+    _bad("%s must be a number, not %r" % (name, v))
+
+
+def _rate(p):
+    """p in steps of 2^-16, rounded from the number given: the call takes fp32, whose own rounding may pass a half step."""
+    p = _number("p", p)
+    if not 0.0 <= p <= 1.0:
+        _bad("p must be in 0 .. 1, not %r" % p)
+    return math.floor(p * 65536.0 + 0.5) / 65536.0
+
+
 def dropout(x, p, seed, call=0, step=None, out=None):
-    """x [rows, d] / (1 - p) where the counter-based generator keeps a value, else 0 (p counts in steps of 2^-16). The mask
+    """x [rows, d] / (1 - p) where the counter-based generator keeps a value, else 0 (p counts in steps of 2^-16, rounded once). The mask
     is that of (seed, call + step) whatever the type and strides, and is not stored: the same call on the upstream gradient is
     the backward pass. step: int64 [1] on the GPU, for graphs whose replays draw anew."""
     if x.requires_grad and torch.is_grad_enabled():
         _followed("x")
     rows, d, dtype, code, ldx, gpu = _start("x", x)
-    at = _draw(seed, call, step, gpu)
+    p, at = _rate(p), _draw(seed, call, step, gpu)
     out, ldo = _like("out", out, rows, d, dtype, gpu, x)
     _call(lib().chgnet_dropout, gpu, (rows, d, code, x.data_ptr(), ldx, p, seed, call, at, out.data_ptr(), ldo))
     return out
@@ -402,18 +425,6 @@ def norm_backward(x, w, dh, kind="rms", eps=1e-5, dx=None, dw=None, accumulate=F
     return dx, dw
 
 
-def _number(name, v):
-    """A factor's value as it is now (of a tensor, too, which may hold another one at the next call)."""
-    if type(v) is float:
-        return v
-    if isinstance(v, torch.Tensor) and v.requires_grad and torch.is_grad_enabled():
-        _followed(name)
-    try:
-        return float(v)
-    except (TypeError, ValueError, RuntimeError):
-        _bad("%s must be a number, not %r" % (name, v))
-
-
 @lru_cache(maxsize=64)
 def _residual_cfg(*fields):
     """Of Python's own numbers only: an object of another type may be its own key and change its value."""
@@ -442,7 +453,7 @@ def _residual(f, post, post_kind, gate, pre, pre_kind, alpha, beta, p, seed, cal
     # (by values, never for a step: a cached struct holds no address)
     make = _residual_cfg if at is None else _Residual
     cfg = make(post_n, post_rows, pre_n, pre_rows, cols, _number("alpha", alpha), _number("beta", beta), _number("eps", eps),
-               _number("p", p), seed, call, at)
+               _rate(p), seed, call, at)
     return cfg, (f.data_ptr(), ldf, gate.data_ptr() if cols else None, ldg, post.data_ptr() if post_rows else None,
                  pre.data_ptr() if pre_rows else None), post_rows + pre_rows, cols
 
