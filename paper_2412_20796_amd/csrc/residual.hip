@@ -284,6 +284,18 @@ struct ResArgs {
   int add;
 };
 
+// s(x) and its derivative s (1 - s), each to some last places of its own: with
+// e = exp(-|x|), s and 1 - s are 1 / (1 + e) and e times that. 1 - s formed from s is off
+// by half a last place of 1, which is all of it for x = 17.
+struct Sigmoid {
+  float s, slope;
+  __device__ __forceinline__ explicit Sigmoid(float x) {
+    const float e = __expf(-fabsf(x)), large = __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
+    s = x < 0.f ? small : large;
+    slope = small * large;
+  }
+};
+
 template <class T>
 __device__ __forceinline__ float stored(float v) {
   return (float)(T)v;
@@ -480,7 +492,7 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
     const int64_t r = first + threadIdx.x / TPR, at = row_of(first);
     const bool live = r < a.rows;
     float D[CPL] = {}, y[CPL] = {}, dh[CPL] = {}, f[CPL] = {}, g[CPL] = {};
-    float s1 = 1.f;
+    float g1 = 0.f;
     if constexpr (AHEAD) {
       if (a.dy) row.values(in.dy, D);
       if (a.pre) {
@@ -490,7 +502,7 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
       if constexpr (RES) {
         if (a.f) row.values(in.f, f);
         if (a.gate == 2) row.values(in.g, g);
-        if (a.gate == 1) s1 = sigm(in.g1);
+        if (a.gate == 1) g1 = in.g1;
       }
     } else {
       if (a.dy) row.load(static_cast<const T*>(a.dy) + at * a.lddy, a.rows - 1 - at, a.lddy, D);
@@ -501,7 +513,7 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
       if constexpr (RES) {
         if (a.f) row.load(static_cast<const T*>(a.f) + at * a.ldf, a.rows - 1 - at, a.ldf, f);
         if (a.gate == 2) row.load(static_cast<const T*>(a.g) + at * a.ldg, a.rows - 1 - at, a.ldg, g);
-        if (a.gate == 1) s1 = sigm((float)static_cast<const T*>(a.g)[at * a.ldg]);
+        if (a.gate == 1) g1 = (float)static_cast<const T*>(a.g)[at * a.ldg];
       }
     }
     if (AHEAD && first + stride < a.rows) load(row_of(first + stride));
@@ -565,11 +577,13 @@ __global__ void __launch_bounds__(bwd_threads<TPR>()) k_residual_bwd(ResArgs a) 
       }
       // y: the gradient of t
       if (a.gate) {
+        const Sigmoid one(g1);
 #pragma unroll
         for (int k = 0; k < CPL; ++k) {
-          const float du = beta * D[k], s = a.gate == 2 ? sigm(g[k]) : s1, dt = du * s;
-          g[k] = keep(k) ? dt * (1.0f - s) * fmaf(wp[k], f[k], bp[k]) : 0.f;
-          y[k] = keep(k) ? dt : 0.f;
+          const Sigmoid sg = a.gate == 2 ? Sigmoid(g[k]) : one;
+          const float du = beta * D[k];
+          g[k] = keep(k) ? du * sg.slope * fmaf(wp[k], f[k], bp[k]) : 0.f;
+          y[k] = keep(k) ? du * sg.s : 0.f;
         }
         if (a.gate == 2 && live) row.store(static_cast<T*>(a.o2) + r * a.ld2, g);
         if (a.gate == 1) {
