@@ -753,8 +753,10 @@ __global__ void __launch_bounds__(512) k_fp8_few(ProductArgs p, const T* __restr
 // a row's 128 values of a step; those of the next step arrive while this one's are
 // multiplied. Places in LDS and operands are k_fp8_product's. x's codes have one
 // buffer, which all read before they multiply: two blocks have room on a compute unit.
+// x is not `__restrict__`: a wait counts its loads, and so needs them where they are
+// written; the compiler may move loads of memory that nothing else can write past it.
 template <class T, bool EXACT, int BN>
-__global__ void __launch_bounds__(2 * BN, 4) k_fp8_rows_product(ProductArgs p, const T* __restrict__ x, int64_t ldx) {
+__global__ void __launch_bounds__(2 * BN, 4) k_fp8_rows_product(ProductArgs p, const T* x, int64_t ldx) {
   constexpr int BM = 64, WN = BN / 64, THREADS = 2 * BN, TM = 2, TN = 4, W = 16 / sizeof(T);
   constexpr int PIECES = BN * 8 / THREADS, XP = BM * 16 / THREADS, LOADS = XP * sizeof(T) / 2;
   __shared__ __align__(1024) uint8_t la[BM * kBlock], lb[2][BN * kBlock];
@@ -834,8 +836,8 @@ __global__ void __launch_bounds__(2 * BN, 4) k_fp8_rows_product(ProductArgs p, c
     for (int j = 0; j < TN; ++j) eb[j] = sb[j][kb];
     const bool more = kb + 1 < nkb;
     if (more) load_x(kb + 1);
-    // b's codes are there (the rows of x loaded after them may be under way), and
-    // all have written theirs of a
+    // b's codes are there (the LOADS loads of x's rows after them may be under way;
+    // others among them only lengthen the wait), and all have written theirs of a
     if (more && inside && (int64_t)(kb + 2) * kBlock <= K) wait_barrier<LOADS>();
     else wait_barrier<0>();
     if (more) load_b(kb + 1);
