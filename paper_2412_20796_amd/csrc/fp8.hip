@@ -1131,13 +1131,22 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
 
 // Columns of a block: twice as many where that leaves a block for each compute unit
 // (16 rows of 8,192 to 8,192 in bf16: 31 us in blocks of 16 columns, 24 of 32, 32 of
-// 64; one row of 4,096 to 4,096: 8.3, 8.4, 12)
+// 64; one row of 4,096 to 4,096: 8.3, 8.4, 12). A launch has fewer than 2^32 threads:
+// more columns than kLaunchCols, whole blocks of 128, are taken in turn.
+constexpr int64_t kLaunchCols = 1 << 26;
 template <class T, bool QUANT>
 int launch_few(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
   constexpr bool exact = std::is_same<T, float>::value;
   auto launch = [&](auto nt) -> int {
-    KLAUNCH(st, "k_fp8_few", k_fp8_few<T, exact, QUANT, nt.value>
-                             <<<(unsigned)cdiv(p.b.rows, 16 * nt.value), 512, 0, st>>>(p, x, ldx));
+    for (int64_t n = 0; n < p.b.rows; n += kLaunchCols) {
+      ProductArgs q = p;
+      q.b.codes += n * p.b.ldc;
+      q.b.scale += (n >> p.b.shift) * p.b.lds;
+      q.b.rows = std::min(kLaunchCols, p.b.rows - n);
+      q.out = static_cast<T*>(p.out) + n;
+      KLAUNCH(st, "k_fp8_few", k_fp8_few<T, exact, QUANT, nt.value>
+                               <<<(unsigned)cdiv(q.b.rows, 16 * nt.value), 512, 0, st>>>(q, x, ldx));
+    }
     return CHGNET_OK;
   };
   if (p.b.rows >= 32 * kUnits) return launch(std::integral_constant<int, 2>{});

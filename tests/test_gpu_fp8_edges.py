@@ -49,3 +49,28 @@ def test_many_rows_of_many_steps(rows, K, N, dtype):
         assert torch.equal(ops.fp8_linear(x, w), out)
     r, b = ref.product(_held(ops.fp8_quantize(x)), _held(w), dtype)
     assert_within(out, r, b, dtype)
+
+
+@pytest.mark.parametrize("br", [1, 128])
+@pytest.mark.parametrize("M", [1, 3])
+def test_more_columns_than_one_launch_has(M, br):
+    """2^28 columns and some for few rows: 2^32 threads and more in blocks of 32 columns."""
+    N, K, part = (1 << 28) + 37, 16, 1 << 20
+    g = torch.Generator().manual_seed(M)
+    few = ops.fp8_quantize(torch.randn(part, K, generator=g).cuda(), br)
+    codes = torch.empty(N, K, dtype=torch.uint8, device="cuda")
+    scale = torch.zeros(-(-N // br), 4, dtype=torch.uint8, device="cuda")
+    for n in range(0, N, part):
+        m = min(part, N - n)
+        codes[n:n + m] = few.codes.view(torch.uint8)[:m]
+        scale[n // br:-(-(n + m) // br), :1] = few.scale.view(torch.uint8)[:-(-m // br)]
+    w = ops.Fp8Matrix(codes.view(torch.float8_e4m3fn), scale.view(torch.float8_e8m0fnu)[:, :1], br)
+    x = torch.randn(M, K, generator=g).to(torch.bfloat16).cuda()
+    want = ops.fp8_linear(x, few)
+    r, b = ref.product(_held(ops.fp8_quantize(x)), _held(few), torch.bfloat16)
+    assert_within(want, r, b, torch.bfloat16)
+    for out in (ops.fp8_linear(x, w), ops.fp8_matmul(ops.fp8_quantize(x), w)):
+        assert out.shape == (M, N)
+        for n in range(0, N, part):
+            m = min(part, N - n)
+            assert torch.equal(out[:, n:n + m], want[:, :m]), n
