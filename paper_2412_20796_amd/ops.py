@@ -384,9 +384,9 @@ def _rate(p):
 
 
 def dropout(x, p, seed, call=0, step=None, out=None):
-    """x [rows, d] / (1 - p) where the counter-based generator keeps a value, else 0 (p counts in steps of 2^-16, rounded once). The mask
-    is that of (seed, call + step) whatever the type and strides, and is not stored: the same call on the upstream gradient is
-    the backward pass. step: int64 [1] on the GPU, for graphs whose replays draw anew."""
+    """x [rows, d] / (1 - p) where the counter-based generator keeps a value, else 0 (p counts in steps of 2^-16, to the
+    nearest of which it is rounded). The mask is that of (seed, call + step) whatever the type and strides, and is not stored: the
+    same call on the upstream gradient is the backward pass. step: int64 [1] on the GPU, for graphs whose replays draw anew."""
     if x.requires_grad and torch.is_grad_enabled():
         _followed("x")
     rows, d, dtype, code, ldx, gpu = _start("x", x)
@@ -557,7 +557,7 @@ class Fp8Matrix:
         """Row stride of bytes whose rows start on `unit` bytes and can be read up to the next multiple of it."""
         rows, cols = t.shape
         whole = -(-cols // unit) * unit
-        ld = t.stride(0) if rows > 1 else whole
+        ld = t.stride(0) if rows > 1 and cols else whole  # (of rows without bytes it says nothing)
         if (cols > 1 and t.stride(1) != 1) or ld % unit or ld < whole or t.data_ptr() % unit:
             _bad("%s must have contiguous columns, and rows that start on %d bytes and do not overlap" % (name, unit))
         if whole != cols and rows and t.storage_offset() + (rows - 1) * ld + whole > t.untyped_storage().nbytes():
