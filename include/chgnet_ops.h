@@ -184,7 +184,7 @@ typedef struct chgnet_fp8 {
  * the least power of two by which its largest magnitude is at most 448, but at
  * least 2^-126; codes are rounded to nearest, ties to even. A block with a value that
  * is not finite has the scale NaN. With block_rows = 128 both forms hold the same
- * values. rows <= 2^23. */
+ * values. rows <= 2^23; with t or block_rows = 128 fewer than 2^40 values. */
 int chgnet_fp8_quantize(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* q,
                         const chgnet_fp8* t, void* stream);
 

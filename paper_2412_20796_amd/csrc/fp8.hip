@@ -1131,8 +1131,9 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
 
 // Columns of a block: twice as many where that leaves a block for each compute unit
 // (16 rows of 8,192 to 8,192 in bf16: 31 us in blocks of 16 columns, 24 of 32, 32 of
-// 64; one row of 4,096 to 4,096: 8.3, 8.4, 12). A launch has fewer than 2^32 threads:
-// more columns than kLaunchCols, whole blocks of 128, are taken in turn.
+// 64; one row of 4,096 to 4,096: 8.3, 8.4, 12). A launch has fewer than 2^32 threads (of
+// more the runtime starts the number modulo 2^32, without an error): more columns than
+// kLaunchCols, whole blocks of 128, are taken in turn.
 constexpr int64_t kLaunchCols = 1 << 26;
 template <class T, bool QUANT>
 int launch_few(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
@@ -1210,7 +1211,8 @@ KLAUNCH(st, "k_fp8_rows",
     // 4,096 in bf16, both forms: 19 us in blocks of one tile, 22 of four)
     const int count = cdiv(rows, 512) * cdiv(cols, 128) >= 4 * kUnits ? 4 : 1;
     const int64_t tiles = cdiv(rows, 128 * count) * cdiv(cols, 128);
-    if (tiles >= (int64_t(1) << 31)) return bad(who, "more than 2^31 - 1 tiles of 128 x 128");
+    // (a launch has fewer than 2^32 threads, and the runtime does not say so)
+    if (tiles >= (int64_t(1) << 24)) return bad(who, "more than 2^40 values");
     const chgnet_fp8 none{}, &a = q ? *q : none, &b = t ? *t : none;
 #define CHG_TILE(S)                                                                                                     \
   KLAUNCH(st, "k_fp8_tile", k_fp8_tile<T, S><<<(unsigned)tiles, 256, 0, st>>>(                                          \
