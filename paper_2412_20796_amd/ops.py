@@ -617,6 +617,8 @@ def _fp8_quantize(x, block_rows, want, want_t, out, out_t):
         _bad("block_rows must be 1 or 128")
     q = _fp8_out("out", out, rows, cols, block_rows, gpu, x) if want else None
     t = _fp8_out("out_t", out_t, cols, rows, block_rows, gpu, x) if want_t else None
+    if q is not None and t is not None and q._c.codes == t._c.codes and q._c.codes:
+        _bad("out and out_t have the same codes")
     _call(lib().chgnet_fp8_quantize, gpu, (rows, cols, code, x.data_ptr(), ldx, ctypes.byref(q._c) if want else None,
                                            ctypes.byref(t._c) if want_t else None))
     return q, t
