@@ -168,8 +168,8 @@ int chgnet_dropout(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_
  * Codes of a row follow each other, rows are ld bytes apart (a multiple of 16, on
  * 16-byte boundaries); where cols is no multiple of 16 the bytes up to the next one
  * are 0 (chgnet_fp8_quantize writes them). Scale rows are ld_scale bytes apart (a
- * multiple of 4, on 4-byte boundaries). Strides are at most 2^23, rows < 2^31, 0 <=
- * cols <= 2^23. */
+ * multiple of 4, on 4-byte boundaries) and are read in words of 4. Strides are at most
+ * 2^23, rows < 2^31, 0 <= cols <= 2^23; without columns there is nothing to read. */
 typedef struct chgnet_fp8 {
   int64_t rows, cols;
   uint8_t* codes;
@@ -201,8 +201,10 @@ int chgnet_fp8_matmul(const chgnet_fp8* a, const chgnet_fp8* b, int32_t dtype, v
                       void* ws, size_t ws_bytes, void* stream);
 
 /* Linear layer: out [rows, N] = q(x) w^T for x [rows, K] and w [N, K], where q(x) is
- * x as chgnet_fp8_quantize has it with block_rows = 1; out has x's dtype. rows <=
- * 2^23. ws: at least chgnet_fp8_linear_workspace(rows, N, K) bytes, 16-byte aligned. */
+ * x as chgnet_fp8_quantize has it with block_rows = 1; out has x's dtype, summed
+ * as chgnet_fp8_matmul does for that type (to fp32's last place of 16-bit x: that call
+ * with fp32 results). rows <= 2^23. ws: at least chgnet_fp8_linear_workspace(rows, N, K)
+ * bytes, 16-byte aligned. */
 int chgnet_fp8_linear_workspace(int64_t rows, int64_t n, int64_t k, size_t* bytes);
 int chgnet_fp8_linear(int64_t rows, int32_t dtype, const void* x, int64_t ldx, const chgnet_fp8* w, void* out,
                       int64_t ldout, void* ws, size_t ws_bytes, void* stream);

@@ -170,9 +170,11 @@ __global__ void __launch_bounds__(256) k_fp8_rows(int64_t rows, int64_t cols, co
 // both share; else 1 x 128 of the rows of each. A thread has 8 x 8 values; the
 // transposed codes go through LDS, in units of the 8 bytes that a thread has of a
 // column, unit u of column c at u ^ (c / 8 % 16), so that 16 lanes write to 16
-// banks' pairs. Four tiles a block, so that the transpose's scales are written in
-// words: single bytes far from each other were a third of all writes, and took
-// twice the time (397,934 x 512 in bf16, both forms: 278 us).
+// banks' pairs. Blocks of four tiles write the transpose's scales in words; single
+// bytes far from each other were a third of all writes, as long as rows of codes
+// started anywhere. In whole lines of codes blocks of one tile are as fast or faster
+// (397,934 x 512 in bf16, both forms: 167 us of one, 180 of four; 16,384 x 16,384: 237
+// and 240).
 template <class T, bool SQUARE>
 __global__ void __launch_bounds__(256, 4) k_fp8_tile(int64_t rows, int64_t cols, const T* __restrict__ x, int64_t ldx,
                                                      uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scale,
@@ -388,7 +390,7 @@ __device__ __forceinline__ void put(T* p, float (&t)[W], int64_t left, bool add)
 // bits, are 16 bytes that follow each other, beside those of the other lane groups.
 // A row's 8 pieces of 16 bytes sit at piece ^ key(row), the keys such that the 16
 // rows of an operand meet in no bank: 16 lanes read 256 bytes, two rows, at a
-// time (with keys of row % 8 a load took twice as long: 8192^3 463 us).
+// time (with keys of row % 8 a load took twice as long: 8192^3 463 us in place of 420).
 // EXACT: products of bf16 values, 32 of a block's 128 at a time.
 template <class T, bool EXACT, int BM, int BN, int WM, int WN, int STAGES>
 __global__ void __launch_bounds__(64 * WM * WN, (WM * WN) / 4) k_fp8_product(ProductArgs p) {
@@ -909,7 +911,8 @@ __global__ void __launch_bounds__(2 * BN, 4) k_fp8_rows_product(ProductArgs p, c
 // 512 values. A block, one a compute unit, keeps them and walks the rows, 64 at a
 // time; the values of a step are loaded for the block's next rows as soon as they are
 // coded, a whole tile ahead, and a step waits for no load of codes. (397,934 rows of
-// 512 to 256 180 -> 152 us in bf16, 4.0 TB/s, 308 -> 245 in fp32, 5.0.)
+// 512 to 256 take 133 us in bf16, 4.6 TB/s, and 180 in k_fp8_rows_product, 241 and 306
+// in fp32.)
 template <class T, bool EXACT>
 __global__ void __launch_bounds__(512, 2) k_fp8_rows_resident(ProductArgs p, const T* __restrict__ x, int64_t ldx) {
   constexpr int BM = 64, BN = 256, WN = 4, THREADS = 512, TM = 2, TN = 4, W = 16 / sizeof(T), KB = 4, XP = 2;
@@ -1106,15 +1109,15 @@ struct Plan {
   int splits, kb_split;
 };
 // The tiles: the largest of which there is one for each compute unit, where K may
-// be divided into parts of kLeastSteps blocks or more. 256 x 512 x 397,934 took
-// 159 us in 2 tiles of 256 x 128 parts, 185 in 8 of 128 x 32, 190 in 32 of 64 x
-// 16; 512 x 4,096 x 4,096 19 us in 512 tiles of 64, 26 in 128 of 128, 24 in twice
-// as many halves; 128 x 8,192 x 8,192 25 us in 256 tiles of 64 and two parts, 29 in one,
-// 33 in 64 of 128 and two.
+// be divided into parts of kLeastSteps blocks or more. 256 x 512 x 397,934 takes
+// 135 us in 2 tiles of 256 x 128 parts, 158 in 8 of 128 x 32, 204 in 32 of 64 x
+// 16; 512 x 4,096 x 4,096 21 us in 512 tiles of 64, 28 in 128 of 128, 25 in twice
+// as many halves; 128 x 8,192 x 8,192 26 us in 256 tiles of 64 and two parts, 31 in one,
+// 34 in 64 of 128 and two.
 constexpr int64_t kLeastSteps = 24;
 // The smallest tiles, where there are fewer than compute units, take parts of 8
-// blocks (a linear layer of 1,938 rows of 8,192 to 128 in bf16 39 us with its 62 tiles
-// in 2 parts, 27 in 8).
+// blocks (a linear layer of 1,938 rows of 8,192 to 128 in bf16 30 us with its 62 tiles
+// in 2 parts, 24 in 8).
 constexpr int64_t kLeastSmallSteps = 8;
 Plan plan(int64_t M, int64_t N, int64_t K) {
   const int64_t nkb = std::max<int64_t>(1, cdiv(K, kBlock));
@@ -1130,8 +1133,8 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
 }
 
 // Columns of a block: twice as many where that leaves a block for each compute unit
-// (16 rows of 8,192 to 8,192 in bf16: 31 us in blocks of 16 columns, 24 of 32, 32 of
-// 64; one row of 4,096 to 4,096: 8.3, 8.4, 12). A launch has fewer than 2^32 threads (of
+// (16 rows of 8,192 to 8,192 in bf16: 33 us in blocks of 16 columns, 23 of 32, 26 of
+// 64; one row of 4,096 to 4,096: 7.6, 8.6, 12). A launch has fewer than 2^32 threads (of
 // more the runtime starts the number modulo 2^32, without an error): more columns than
 // kLaunchCols, whole blocks of 128, are taken in turn.
 constexpr int64_t kLaunchCols = 1 << 26;
@@ -1156,8 +1159,8 @@ int launch_few(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
 
 // Whether a linear layer quantises its rows on the way: where each is needed once
 // and the blocks fill the GPU (us of a call against quantiser and product, bf16: 397,934
-// rows of 512 to 256 152 and 227, to 128 115 and 211, 85,274 of 256 to 128 18 and 32; fp32 rows
-// 245 and 392, 189 and 354, 27 and 48; 5,000 of 512 to 256 9 and 11, in fp32 14 and 12)
+// rows of 512 to 256 133 and 227, to 128 116 and 211, 85,274 of 256 to 128 19 and 32; fp32 rows
+// 241 and 393, 192 and 353, 27 and 48; 5,000 of 512 to 256 9 and 10, in fp32 12 and 12)
 bool on_the_way(int64_t M, int64_t N) { return N <= 256 && cdiv(M, 64) >= kUnits; }
 template <class T>
 int launch_rows_product(const ProductArgs& p, const T* x, int64_t ldx, hipStream_t st) {
@@ -1207,8 +1210,8 @@ KLAUNCH(st, "k_fp8_rows",
               k_fp8_rows<T><<<blocks, 256, 0, st>>>(rows, cols, p, ldx, q->codes, q->ld, q->scale, q->ld_scale));
       return CHGNET_OK;
     }
-    // four tiles a block where that leaves four blocks for each compute unit (4,096 x
-    // 4,096 in bf16, both forms: 19 us in blocks of one tile, 22 of four)
+    // four tiles a block only where that leaves four blocks for each compute unit (4,096 x
+    // 4,096 in bf16, both forms: 16 us in blocks of one tile, 23 of four)
     const int count = cdiv(rows, 512) * cdiv(cols, 128) >= 4 * kUnits ? 4 : 1;
     const int64_t tiles = cdiv(rows, 128 * count) * cdiv(cols, 128);
     // (a launch has fewer than 2^32 threads, and the runtime does not say so)

@@ -16,9 +16,9 @@
 //
 // Bound by memory. Measured (kernel time, bytes that a pass cannot do without over
 // it; a copy reaches 4.7 TB/s): 16,384 rows of 8,192 in bf16 with RMS norms, gate and
-// dropout forward 268 us (5.0 TB/s), backward 425 (5.1); 397,934 rows of 128 in fp32
-// 200 and 331 us (5.1, 4.9), a LayerNorm alone 67 and 126; 65,536 rows of 512 in bf16 66
-// and 132 us (5.1, 4.1), where the backward pass has two wavefronts a SIMD for its
+// dropout forward 275 us (4.9 TB/s), backward 446 (4.8); 397,934 rows of 128 in fp32
+// 201 and 327 us (5.1, 5.0), a LayerNorm alone 66 and 125; 65,536 rows of 512 in bf16 66
+// and 140 us (5.1, 3.8), where the backward pass has two wavefronts a SIMD for its
 // 170 registers.
 #include <hip/hip_runtime.h>
 
@@ -56,9 +56,9 @@ struct Scale {
 // bytes) at columns (q TPR + j) VEC. ANY: rows at any value's address, and a last
 // group that is short; the hardware takes 16 bytes at any address. A short group is
 // loaded whole where the array goes on behind it (the next row's values), and what
-// is past the row is cleared; it is stored in 8, 4 and 2 bytes. (Single values took
-// 265 and 203 us forward and backward for 40,000 rows of 1,001 in bf16 with all parts;
-// short groups value by value 131 and 310.)
+// is past the row is cleared; it is stored in 8, 4 and 2 bytes. (40,000 rows of 1,001 in
+// bf16 with all parts take 96 and 268 us forward and backward; in single values 265 and
+// 475, with short groups value by value 131 and 310.)
 template <int VEC, int TPR, int NQ, bool ANY>
 struct Row {
   static constexpr int CPL = VEC * NQ, WAVES = TPR > 64 ? TPR / 64 : 1;

@@ -670,7 +670,8 @@ def fp8_matmul(a, b, dtype=torch.bfloat16, out=None, accumulate=False, ws=None):
 
 def fp8_linear(x, w, out=None, ws=None):
     """out [rows, N] = q(x) w^T of x [rows, K] in fp32, bf16 or fp16 and an Fp8Matrix w [N, K], where q(x) is fp8_quantize's
-    x; out is of x's type. ws: a Workspace of the caller's (one for each call that may run at the same time)."""
+    x; out is of x's type, summed as fp8_matmul does for that (for sums to fp32's last place of 16-bit x: fp8_matmul of
+    fp8_quantize(x) in fp32). ws: a Workspace of the caller's (one for each call that may run at the same time)."""
     if x.requires_grad and torch.is_grad_enabled():
         _followed("x")
     rows, k, dtype, code, ldx, gpu = _start("x", x)
